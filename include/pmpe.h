@@ -614,6 +614,160 @@ size_t pmpe_fingerprint_workspace_bytes(uint64_t nbytes);
 pmpe_status pmpe_fingerprint(const void* data, uint64_t nbytes, uint8_t* digest, void* ws,
                              size_t ws_bytes, pmpe_stream_t stream);
 
+/*
+ * pmpe_rmsnorm - residual add and RMS norm ahead of a layer, for T rows of H values.
+ * (The transformer around the layer, Fig. 1; no passage of the paper defines the norm.)
+ *
+ *   r = round(x + residual) to dtype (r = x without a residual)
+ *   y = r rstd weight, rstd = 1 / sqrt(mean(r^2) + eps), in fp32 from the rounded r
+ *   out = round(y) to dtype;  out_q = e4m3(y / s) with s = 2^ceil(log2(amax / 448)) of each
+ *   block of 32 consecutive values of a row (no value saturates), the format that
+ *   pmpe_expert_ffn_mx reads. out_scale holds s as its biased exponent (127 + log2 s, e8m0); a
+ *   block of zeros has scale 1, a block with a value that is not finite scale 1 and NaN
+ *   elements. Sums of squares are fp32 (rows of values beyond 1e19 overflow them).
+ *
+ *   T >= 0, H 1..16384 (a multiple of 32 with out_q); dtype PMPE_BF16 or PMPE_F32 of x,
+ *   residual, sum_out and out; w_dtype PMPE_F32 or PMPE_BF16; eps >= 0
+ *   x, residual  [T, H]; residual may be NULL
+ *   weight       [H]
+ *   sum_out      [T, H] out: r, required with a residual and NULL without; may be x or residual
+ *   out          [T, H] out or NULL; may be x when there is no residual
+ *   out_q        [T, H] uint8 out or NULL, out_scale [T, H / 32] uint8 out: both or neither
+ *   rstd         [T] fp32 out or NULL (pmpe_rmsnorm_backward reads it)
+ * Errors: PMPE_ERR_NULL (also when neither out nor out_q is given), PMPE_ERR_SHAPE,
+ * PMPE_ERR_DTYPE, PMPE_ERR_ALIGN (pointers to [T, H] arrays and the weight: 16 bytes).
+ */
+pmpe_status pmpe_rmsnorm(int32_t T, int32_t H, int32_t dtype, const void* x, const void* residual,
+                         const void* weight, int32_t w_dtype, float eps, void* sum_out, void* out,
+                         uint8_t* out_q, uint8_t* out_scale, float* rstd, pmpe_stream_t stream);
+
+/*
+ * pmpe_rmsnorm_backward - gradients of pmpe_rmsnorm's input and weight, for the upstream gradient
+ * dy of y and dres of r (the residual stream's own gradient):
+ *   dx = rstd (g - xhat mean(g xhat)) + dres, g = dy weight, xhat = r rstd
+ *   dweight = sum over the rows of dy xhat
+ * The gradient of x and of the residual are both dx. fp32 arithmetic; every sum has a fixed
+ * order (two calls give equal bits).
+ *
+ *   dy       [T, H] of dy_dtype: PMPE_F32 (what pmpe_backward returns) or dtype
+ *   dres     [T, H] dtype or NULL
+ *   r, rstd  pmpe_rmsnorm's sum_out (x without a residual) and rstd
+ *   dx       [T, H] dtype out; may be dres, or dy of the same type
+ *   dweight  [H] fp32 out or NULL (a frozen norm: no gradient of it is formed)
+ *   ws       pmpe_rmsnorm_backward_workspace_bytes(T, H) bytes, 16-byte aligned; unused without
+ *            dweight
+ * T = 0 writes zeros to dweight. Errors as pmpe_rmsnorm, and PMPE_ERR_WORKSPACE.
+ */
+size_t pmpe_rmsnorm_backward_workspace_bytes(int32_t T, int32_t H);
+
+pmpe_status pmpe_rmsnorm_backward(int32_t T, int32_t H, int32_t dtype, const void* dy,
+                                  int32_t dy_dtype, const void* dres, const void* r,
+                                  const void* weight, int32_t w_dtype, const float* rstd, void* dx,
+                                  float* dweight, void* ws, size_t ws_bytes, pmpe_stream_t stream);
+
+/*
+ * Routing by scores: an expert's score is the sigmoid of its logit, or the softmax over the
+ * permitted pool; the choice is made by score plus a balance bias (select_bias, which evens the
+ * experts' load and enters no gate), inside the best groups of experts. The policy mask comes
+ * before all of it, as in pmpe_route: a token has the scores, groups and choice of its permitted
+ * pool only. For token t with pool P, logits z and bias b:
+ *
+ *   s_e = 1 / (1 + exp(-z_e))  or  exp(z_e) / sum over P of exp(z);  u_e = s_e + b_e
+ *   P in n_group groups of consecutive ids; a group's rank is the sum of its group_top largest u;
+ *   the topk_group groups of the highest rank stay (equal ranks: the lower group)
+ *   the top_k largest u of the experts that stay are selected (equal u: the lower id)
+ *   gate_e = scale s_e / (sum over the selected of s + 1e-20)    d->gate_mode RENORM_TOPK, sigmoid
+ *   gate_e = scale softmax over the selected z                   RENORM_TOPK, softmax
+ *   gate_e = scale s_e                                           POOL_SOFTMAX: scores as they are
+ *
+ * s, u and the ranks are 64-bit: the selection is that of 64-bit arithmetic on the fp32 logits. A
+ * logit of -inf (or NaN) masks its expert: score and gate 0, no part in a group's rank, selected
+ * only when nothing else is left. +inf counts as the largest finite value. A bias of -inf (or NaN)
+ * ranks an expert with the masked ones, its score staying. With route_mode SOFT (the control arm)
+ * the pool is the concatenated one and neither pool may have groups.
+ */
+typedef enum { PMPE_SCORE_SOFTMAX = 0, PMPE_SCORE_SIGMOID = 1 } pmpe_score;
+#define PMPE_MAX_GROUPS 64
+typedef struct {
+  int32_t score;           /* pmpe_score */
+  int32_t group_top;       /* 1 or 2: best u of a group that make its rank */
+  int32_t n_group_pub;     /* groups of the public pool, 1..64, a divisor of n_pub (1: no groups) */
+  int32_t topk_group_pub;  /* of which stay, 1..n_group_pub; they hold at least top_k experts */
+  int32_t n_group_priv;    /* the same of the private pool (1 and 1 when n_priv == 0) */
+  int32_t topk_group_priv;
+  float scale;             /* factor of every gate, finite */
+} pmpe_score_rule;
+
+/*
+ * pmpe_select - policy decode, scores, selection and gates from given router logits.
+ *
+ *   logits       [T, n_pub + n_priv] of logits_dtype (PMPE_F32 or PMPE_BF16), any bias of the
+ *                router already added; a token's row is read in its permitted pool only
+ *   select_bias  [n_pub + n_priv] fp32 or NULL
+ *   policy_word  [T] uint32 or NULL (every token denies)
+ *   topk_idx     [T, k] int32 out, ascending; topk_gate [T, k] fp32 out
+ *   topk_logit   [T, k] fp32 out or NULL: the selected logits (pmpe_backward_scored reads them)
+ *   allow        [T] uint8 out: the resolved policy decision
+ *   margin       [T] fp32 out or NULL: u of the last selected expert minus the largest u that was
+ *                left among the groups that stayed; +inf when none, or only masked ones, were left
+ * d gives the pools, top_k, gate_mode and route_mode. No workspace.
+ * Errors: those of the descriptor, PMPE_ERR_SHAPE (a rule out of range), PMPE_ERR_NULL,
+ * PMPE_ERR_DTYPE. Pointers need the alignment of their elements only.
+ */
+pmpe_status pmpe_select(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int32_t T,
+                        const void* logits, int32_t logits_dtype, const float* select_bias,
+                        const uint32_t* policy_word, int32_t* topk_idx, float* topk_gate,
+                        float* topk_logit, uint8_t* allow, float* margin, pmpe_stream_t stream);
+
+/*
+ * pmpe_select_backward - gradient of pmpe_select's gates with respect to the logits; the selection
+ * is the forward's and has no gradient, nor has the balance bias.
+ *
+ *   topk_idx     [T, k] from pmpe_select (a token's pool is the one that its first id lies in;
+ *                ids outside that pool take no part)
+ *   dgate        [T, k] fp32
+ *   dlogits      [T, n_pub + n_priv] fp32 out: every element written, zeros outside the pool
+ * fp32 arithmetic; a masked logit has gradient 0.
+ */
+pmpe_status pmpe_select_backward(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int32_t T,
+                                 const void* logits, int32_t logits_dtype, const int32_t* topk_idx,
+                                 const float* dgate, float* dlogits, pmpe_stream_t stream);
+
+/*
+ * pmpe_route_scored - pmpe_route with the selection and gates of a score rule: the same logits of the
+ * same permitted pool (logit_bias included), then pmpe_select. Arguments, workspace and errors as
+ * pmpe_route, with rule, select_bias, topk_logit and margin as in pmpe_select.
+ */
+pmpe_status pmpe_route_scored(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int32_t T,
+                              const void* x, const float* wr_pub, const float* wr_priv,
+                              const float* logit_bias, const float* select_bias,
+                              const uint32_t* policy_word, int32_t* topk_idx, float* topk_gate,
+                              float* topk_logit, uint8_t* allow, float* margin, uint32_t* dev_status,
+                              void* ws, size_t ws_bytes, pmpe_stream_t stream);
+
+/*
+ * pmpe_backward_scored - pmpe_backward of a layer that routed by scores: the same gradients with the
+ * gates' own derivative,
+ *   sigmoid, RENORM_TOPK:  ds_j = scale / S (dg_j - sum_i g_i dg_i / scale), S = sum of s + 1e-20
+ *   sigmoid, POOL_SOFTMAX: ds_j = scale dg_j;  both: dz_j = ds_j s_j (1 - s_j) of the selected
+ *   softmax, RENORM_TOPK:  dz_j = g_j (dg_j - sum_i g_i dg_i / scale)
+ *   softmax, POOL_SOFTMAX: as pmpe_backward, times scale
+ * topk_logit [T, k] is the forward's (required with sigmoid, else it may be NULL); the other
+ * arguments, workspace and errors are pmpe_backward's. select_bias is frozen: no gradient.
+ */
+pmpe_status pmpe_backward_scored(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int32_t T,
+                                 const float* topk_logit, const void* x, const void* dout,
+                                 const int32_t* topk_idx, const float* topk_gate,
+                                 const int32_t* expert_count, const int32_t* expert_offset,
+                                 const int32_t* row_token, const int32_t* token_row, const void* y_perm,
+                                 const float* wr_pub, const float* wr_priv, const void* w13_pub,
+                                 const void* w2_pub, const void* w13_priv, const void* w2_priv,
+                                 const float* logit_bias, const void* w13_sh, const void* w2_sh,
+                                 const void* w2t_pub, const void* w13t_pub, const void* w2t_priv,
+                                 const void* w13t_priv, const float* ab, float* dx, float* dw13_priv,
+                                 float* dw2_priv, float* dwr_priv, uint32_t* grad_rows, void* ws,
+                                 size_t ws_bytes, pmpe_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,7 +15,10 @@ from ._native import (PMPE_BF16, PMPE_F32, PMPE_GATE_POOL_SOFTMAX, PMPE_GATE_REN
                       pmpe_adamw, pmpe_transpose_experts, PMPE_FP8_E4M3, pmpe_expert_ffn_fp8,
                       pmpe_audit, pmpe_check_desc, pmpe_combine, pmpe_dispatch, pmpe_expert_ffn,
                       pmpe_dispatch_noalloc, PMPE_ERR_SCRATCH, PMPE_NOALLOC_SCRATCH_BYTES,
-                      pmpe_route, pmpe_version, pmpe_workspace_bytes)
+                      pmpe_route, pmpe_version, pmpe_workspace_bytes,
+                      pmpe_rmsnorm, pmpe_rmsnorm_backward, pmpe_rmsnorm_backward_workspace_bytes, PMPE_SCORE_SIGMOID,
+                      PMPE_SCORE_SOFTMAX, ScoreRule, make_score_rule, pmpe_select, pmpe_select_backward,
+                      pmpe_route_scored, pmpe_backward_scored)
 from .layer import (AuditBuffers, GradBuffers, LayerBuffers, PolicyMaskedMoE,  # noqa: F401
                     PrivateAdamW)
 from .policy import policy_word, request_offsets, resolve_policy, token_policy_words  # noqa: F401

@@ -50,6 +50,8 @@ PMPE_LORA_GATE_ROW = 0
 PMPE_LORA_GATE_TILE = 1
 PMPE_LORA_GATE_POSTHOC = 2
 PMPE_LORA_TILE_ROWS = 64
+PMPE_SCORE_SOFTMAX = 0
+PMPE_SCORE_SIGMOID = 1
 PMPE_POOL_PUBLIC = 0
 PMPE_POOL_PRIVATE = 1
 PMPE_POOL_MIXED = 2
@@ -95,6 +97,18 @@ class ForwardArgs(ctypes.Structure):
         "deny_violations", "dev_status", "ws")
     _fields_ = [(n, ctypes.c_void_p) for n in POINTERS] + [
         ("ws_bytes", ctypes.c_size_t), ("R", ctypes.c_int32), ("ffn", ctypes.c_int32), ("failed", ctypes.c_int32)]
+
+
+class ScoreRule(ctypes.Structure):
+    """pmpe_score_rule: how pmpe_select and pmpe_route_scored choose and weight experts."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("score", "group_top", "n_group_pub", "topk_group_pub", "n_group_priv",
+                                              "topk_group_priv")] + [("scale", ctypes.c_float)]
+
+
+def make_score_rule(score: int = 1, groups=(1, 1), groups_priv=(1, 1), group_top: int = 2,
+                    scale: float = 1.0) -> ScoreRule:
+    """A score rule; groups and groups_priv are (groups, groups that stay) of the two pools."""
+    return ScoreRule(score, group_top, groups[0], groups[1], groups_priv[0], groups_priv[1], scale)
 
 
 _P = ctypes.c_void_p
@@ -152,12 +166,30 @@ _lib.pmpe_fingerprint_workspace_bytes.argtypes = [ctypes.c_uint64]
 _lib.pmpe_fingerprint.restype = _I32
 _lib.pmpe_fingerprint.argtypes = [_P, ctypes.c_uint64, _P, _P, _SZ, _P]
 
+_lib.pmpe_rmsnorm.restype = _I32
+_lib.pmpe_rmsnorm.argtypes = [_I32] * 3 + [_P] * 3 + [_I32, ctypes.c_float] + [_P] * 6
+_lib.pmpe_rmsnorm_backward_workspace_bytes.restype = _SZ
+_lib.pmpe_rmsnorm_backward_workspace_bytes.argtypes = [_I32, _I32]
+_lib.pmpe_rmsnorm_backward.restype = _I32
+_lib.pmpe_rmsnorm_backward.argtypes = [_I32] * 3 + [_P, _I32] + [_P] * 3 + [_I32] + [_P] * 4 + [_SZ, _P]
+_RULE = ctypes.POINTER(ScoreRule)
+_lib.pmpe_select.restype = _I32
+_lib.pmpe_select.argtypes = [_DESC, _RULE, _I32, _P, _I32] + [_P] * 8
+_lib.pmpe_select_backward.restype = _I32
+_lib.pmpe_select_backward.argtypes = [_DESC, _RULE, _I32, _P, _I32] + [_P] * 4
+_lib.pmpe_route_scored.restype = _I32
+_lib.pmpe_route_scored.argtypes = [_DESC, _RULE, _I32] + [_P] * 12 + [_P, _SZ, _P]
+_lib.pmpe_backward_scored.restype = _I32
+_lib.pmpe_backward_scored.argtypes = [_DESC, _RULE, _I32] + [_P] * 29 + [_P, _SZ, _P]
+
 EXPORTED = ["pmpe_version", "pmpe_status_string", "pmpe_workspace_bytes", "pmpe_check_desc",
             "pmpe_route", "pmpe_dispatch", "pmpe_expert_ffn", "pmpe_combine", "pmpe_audit",
             "pmpe_fingerprint_workspace_bytes", "pmpe_fingerprint", "pmpe_backward_workspace_bytes",
             "pmpe_backward", "pmpe_expert_ffn_train", "pmpe_route_record", "pmpe_cache_tag_check",
             "pmpe_expert_ffn_lora_workspace_bytes", "pmpe_expert_ffn_lora", "pmpe_adamw",
-            "pmpe_transpose_experts", "pmpe_expert_ffn_fp8", "pmpe_layer_forward"]
+            "pmpe_transpose_experts", "pmpe_expert_ffn_fp8", "pmpe_layer_forward",
+            "pmpe_rmsnorm", "pmpe_rmsnorm_backward_workspace_bytes", "pmpe_rmsnorm_backward",
+            "pmpe_select", "pmpe_select_backward", "pmpe_route_scored", "pmpe_backward_scored"]
 
 PMPE_FP_LEAF_BYTES = 1024
 PMPE_FP_FANOUT = 16
@@ -303,6 +335,20 @@ def pmpe_backward(desc, T, x, dout, topk_idx, topk_gate, expert_count, expert_of
         0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "pmpe_backward")
 
 
+def pmpe_backward_scored(desc, rule, T, topk_logit, x, dout, topk_idx, topk_gate, expert_count, expert_offset,
+                         row_token, token_row, y_perm, wr_pub, wr_priv, w13_pub, w2_pub, w13_priv, w2_priv,
+                         logit_bias, w13_sh, w2_sh, w2t_pub, w13t_pub, w2t_priv, w13t_priv, ab, dx, dw13_priv,
+                         dw2_priv, dwr_priv, grad_rows, ws, stream=None) -> None:
+    """pmpe_backward of a layer that routed by `rule` (pmpe_route_scored)."""
+    _check(_lib.pmpe_backward_scored(
+                ctypes.byref(desc), ctypes.byref(rule), T, _ptr(topk_logit), _ptr(x), _ptr(dout), _ptr(topk_idx),
+        _ptr(topk_gate), _ptr(expert_count), _ptr(expert_offset), _ptr(row_token), _ptr(token_row), _ptr(y_perm),
+        _ptr(wr_pub), _ptr(wr_priv), _ptr(w13_pub), _ptr(w2_pub), _ptr(w13_priv), _ptr(w2_priv), _ptr(logit_bias),
+        _ptr(w13_sh), _ptr(w2_sh), _ptr(w2t_pub), _ptr(w13t_pub), _ptr(w2t_priv), _ptr(w13t_priv), _ptr(ab),
+        _ptr(dx), _ptr(dw13_priv), _ptr(dw2_priv), _ptr(dwr_priv), _ptr(grad_rows), _ptr(ws),
+        0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "pmpe_backward_scored")
+
+
 def pmpe_fingerprint_workspace_bytes(nbytes: int) -> int:
     return int(_lib.pmpe_fingerprint_workspace_bytes(nbytes))
 
@@ -395,3 +441,117 @@ def pmpe_expert_ffn_fp8(desc, T, x_perm, x, expert_count, expert_offset, row_tok
         _ptr(w13s_pub), _ptr(w2s_pub), _ptr(w13s_priv), _ptr(w2s_priv), _ptr(y_perm),
         _ptr(audit_token_rows), _ptr(audit_priv_calls), _ptr(dev_status), _ptr(ws),
         0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "pmpe_expert_ffn_fp8")
+
+
+_DTYPES = {torch.float32: PMPE_F32, torch.bfloat16: PMPE_BF16}
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32 or bfloat16, not {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _here(t: torch.Tensor, name: str) -> torch.device:
+    """The device of `t`, which has to be the current one: the call's stream is one of its streams."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current HIP device")
+    return t.device
+
+
+def _need(t: Optional[torch.Tensor], name: str, shape, dtype, dev: torch.device) -> None:
+    """`t` is None or a tensor of this shape, one of these types and this device."""
+    if t is not None and (t.shape != shape or t.dtype not in dtype or t.device != dev):
+        raise ValueError(f"{name} must be {list(shape)} of {' or '.join(map(str, dtype))} on {dev}, "
+                         f"not {list(t.shape)} of {t.dtype} on {t.device}")
+
+
+def _need_len(t: Optional[torch.Tensor], name: str, n: int, dtype, dev: torch.device) -> None:
+    """`t` is None or a tensor of n elements (of any shape), one of these types and this device."""
+    if t is not None and (t.numel() != n or t.dtype not in dtype or t.device != dev):
+        raise ValueError(f"{name} must have {n} elements of {' or '.join(map(str, dtype))} on {dev}, "
+                         f"not {list(t.shape)} of {t.dtype} on {t.device}")
+
+
+def _need_bytes(ws: Optional[torch.Tensor], dev: torch.device) -> int:
+    """Bytes of a workspace on this device (0 for None)."""
+    if ws is None:
+        return 0
+    if ws.device != dev:
+        raise ValueError(f"the workspace is on {ws.device}, not on {dev}")
+    return ws.numel() * ws.element_size()
+
+
+def pmpe_rmsnorm(x, residual, weight, eps: float, sum_out, out, out_q, out_scale, rstd, stream=None) -> None:
+    """Residual add and RMS norm of x [T, H] (bf16 or fp32): r = x + residual into sum_out,
+    the norm of r into out and, in 8 bits, into out_q [T, H] with out_scale [T, H / 32]
+    (uint8); each output may be None."""
+    T, H = x.shape
+    dev = _here(x, "x")
+    for t, name in ((residual, "residual"), (sum_out, "sum_out"), (out, "out")):
+        _need(t, name, (T, H), (x.dtype,), dev)
+    _need(weight, "weight", (H,), tuple(_DTYPES), dev)
+    _need(out_q, "out_q", (T, H), (torch.uint8,), dev)
+    _need(out_scale, "out_scale", (T, H // 32), (torch.uint8,), dev)
+    _need(rstd, "rstd", (T,), (torch.float32,), dev)
+    _check(_lib.pmpe_rmsnorm(T, H, _dtype(x, "x"), _ptr(x), _ptr(residual), _ptr(weight), _dtype(weight, "weight"), eps,
+                             _ptr(sum_out), _ptr(out), _ptr(out_q), _ptr(out_scale), _ptr(rstd), _stream(stream)),
+           "pmpe_rmsnorm")
+
+
+def pmpe_rmsnorm_backward_workspace_bytes(T: int, H: int) -> int:
+    return int(_lib.pmpe_rmsnorm_backward_workspace_bytes(T, H))
+
+
+def pmpe_rmsnorm_backward(dy, dres, r, weight, rstd, dx, dweight, ws, stream=None) -> None:
+    """Gradients of pmpe_rmsnorm: dx [T, H] (of r's type) and dweight [H] fp32 or None."""
+    T, H = r.shape
+    dev = _here(r, "r")
+    _need(dy, "dy", (T, H), (torch.float32, r.dtype), dev)
+    _need(dres, "dres", (T, H), (r.dtype,), dev)
+    _need(dx, "dx", (T, H), (r.dtype,), dev)
+    _need(weight, "weight", (H,), tuple(_DTYPES), dev)
+    _need(rstd, "rstd", (T,), (torch.float32,), dev)
+    _need(dweight, "dweight", (H,), (torch.float32,), dev)
+    _check(_lib.pmpe_rmsnorm_backward(T, H, _dtype(r, "r"), _ptr(dy), _dtype(dy, "dy"), _ptr(dres), _ptr(r), _ptr(weight),
+                                      _dtype(weight, "weight"), _ptr(rstd), _ptr(dx), _ptr(dweight), _ptr(ws),
+                                      _need_bytes(ws, dev), _stream(stream)),
+           "pmpe_rmsnorm_backward")
+
+
+def pmpe_select(desc, rule, T, logits, select_bias, policy_word, topk_idx, topk_gate, topk_logit, allow, margin,
+                stream=None) -> None:
+    """Selection and gates by `rule` from router logits [T, n_pub + n_priv] (fp32 or bf16)."""
+    dev, E, k = _here(logits, "logits"), desc.n_pub + desc.n_priv, desc.top_k
+    _need(logits, "logits", (T, E), tuple(_DTYPES), dev)
+    _need(select_bias, "select_bias", (E,), (torch.float32,), dev)
+    for t, name, n, dt in ((policy_word, "policy_word", T, (torch.int32, torch.uint32)), (topk_idx, "topk_idx", T * k, (torch.int32,)),
+                           (topk_gate, "topk_gate", T * k, (torch.float32,)),
+                           (topk_logit, "topk_logit", T * k, (torch.float32,)), (allow, "allow", T, (torch.uint8,)),
+                           (margin, "margin", T, (torch.float32,))):
+        _need_len(t, name, n, dt, dev)
+    _check(_lib.pmpe_select(ctypes.byref(desc), ctypes.byref(rule), T, _ptr(logits), _dtype(logits, "logits"),
+                            _ptr(select_bias), _ptr(policy_word), _ptr(topk_idx), _ptr(topk_gate), _ptr(topk_logit),
+                            _ptr(allow), _ptr(margin), _stream(stream)), "pmpe_select")
+
+
+def pmpe_select_backward(desc, rule, T, logits, topk_idx, dgate, dlogits, stream=None) -> None:
+    """Gradient dlogits [T, n_pub + n_priv] fp32 of pmpe_select's gates for their gradient dgate."""
+    dev, E, k = _here(logits, "logits"), desc.n_pub + desc.n_priv, desc.top_k
+    _need(logits, "logits", (T, E), tuple(_DTYPES), dev)
+    _need(dlogits, "dlogits", (T, E), (torch.float32,), dev)
+    _need_len(topk_idx, "topk_idx", T * k, (torch.int32,), dev)
+    _need_len(dgate, "dgate", T * k, (torch.float32,), dev)
+    _check(_lib.pmpe_select_backward(ctypes.byref(desc), ctypes.byref(rule), T, _ptr(logits), _dtype(logits, "logits"),
+                                     _ptr(topk_idx), _ptr(dgate), _ptr(dlogits), _stream(stream)),
+           "pmpe_select_backward")
+
+
+def pmpe_route_scored(desc, rule, T, x, wr_pub, wr_priv, logit_bias, select_bias, policy_word, topk_idx, topk_gate,
+                      topk_logit, allow, margin, dev_status, ws, stream=None) -> None:
+    """pmpe_route with the selection and gates of a score rule."""
+    _check(_lib.pmpe_route_scored(ctypes.byref(desc), ctypes.byref(rule), T, _ptr(x), _ptr(wr_pub), _ptr(wr_priv),
+                                  _ptr(logit_bias), _ptr(select_bias), _ptr(policy_word), _ptr(topk_idx),
+                                  _ptr(topk_gate), _ptr(topk_logit), _ptr(allow), _ptr(margin), _ptr(dev_status), _ptr(ws),
+                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
+           "pmpe_route_scored")

@@ -69,7 +69,7 @@ def build(verbose: bool = False) -> str:
 # sanitizer runtime preloaded.
 SAN_DIR = os.path.join(BUILD_DIR, "san")
 SAN_LIB = os.path.join(SAN_DIR, "libpmpe_san.so")
-SAN_SRCS = ("pmpe_api.hip", "noalloc.hip")
+SAN_SRCS = ("pmpe_api.hip", "block_api.hip", "noalloc.hip")
 SAN_FLAGS = ["-O1", "-g",
              "-Xarch_host", "-fsanitize=address,undefined",
              "-Xarch_host", "-fno-sanitize-recover=all",

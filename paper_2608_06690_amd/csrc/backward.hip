@@ -104,9 +104,22 @@ __global__ __launch_bounds__(BT) void bwd_rows_kernel(BwdArgs a) {
       g[j] = a.topk_gate[t * k + j];
       sum += g[j] * v;
     }
-    // RENORM: the logit gradient lives on the k selected experts; POOL_SOFTMAX keeps
-    // dg (per slot) for the pool pass, which needs every pool logit
-    for (int j = 0; j < k; ++j) s_dz[j] = a.pool_gates ? dg[j] : g[j] * (dg[j] - sum);
+    if (a.sigmoid) {
+      // scores s = sigmoid(z) of the selected logits: dz = ds s (1 - s)
+      float total = 1e-20f;
+      for (int j = 0; j < k; ++j) {
+        const float z = a.topk_logit[t * k + j], e = z > -INFINITY ? expf(-fabsf(z)) : 0.f;
+        if (z > -INFINITY) total += (z < 0.f ? e : 1.f) / (1.f + e);
+        s_dz[j] = e / ((1.f + e) * (1.f + e));
+      }
+      for (int j = 0; j < k; ++j)
+        s_dz[j] *= a.renorm ? a.gate_scale / total * (dg[j] - sum / a.gate_scale) : a.gate_scale * dg[j];
+    } else {
+      // RENORM: the logit gradient lives on the k selected experts; POOL_SOFTMAX keeps
+      // dg (per slot) for the pool pass, which needs every pool logit
+      for (int j = 0; j < k; ++j)
+        s_dz[j] = a.pool_gates ? a.gate_scale * dg[j] : g[j] * (dg[j] - sum / a.gate_scale);
+    }
   }
   __syncthreads();
   if (tid < k) {

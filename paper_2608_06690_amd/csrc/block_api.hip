@@ -1,0 +1,152 @@
+// C ABI of the operators around the layer: argument validation (host only, before any launch)
+// and dispatch to the kernel launchers. No exception crosses this boundary; nothing is allocated.
+#include <cmath>
+
+#include "pmpe_internal.h"
+
+using namespace pmpe;
+
+namespace {
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+pmpe_status launched(hipError_t e) { return e == hipSuccess ? PMPE_OK : PMPE_ERR_LAUNCH; }
+
+bool float_type(int32_t t) { return t == PMPE_F32 || t == PMPE_BF16; }
+
+constexpr int32_t kNormMaxH = 16384;
+
+pmpe_status check_rows(int32_t T, int32_t H) {
+  return T < 0 || T > PMPE_MAX_TOKENS || H < 1 || H > kNormMaxH ? PMPE_ERR_SHAPE : PMPE_OK;
+}
+
+}  // namespace
+
+namespace pmpe {
+
+pmpe_status check_rule(const pmpe_layer_desc* d, const pmpe_score_rule* r) {
+  if (!r) return PMPE_ERR_NULL;
+  if (r->score != PMPE_SCORE_SOFTMAX && r->score != PMPE_SCORE_SIGMOID) return PMPE_ERR_SHAPE;
+  if (r->group_top != 1 && r->group_top != 2) return PMPE_ERR_SHAPE;
+  if (!std::isfinite(r->scale)) return PMPE_ERR_SHAPE;
+  const int32_t pool[2][3] = {{d->n_pub, r->n_group_pub, r->topk_group_pub}, {d->n_priv, r->n_group_priv, r->topk_group_priv}};
+  for (const auto& p : pool) {
+    if (p[1] < 1 || p[1] > PMPE_MAX_GROUPS || p[2] < 1 || p[2] > p[1]) return PMPE_ERR_SHAPE;
+    if (p[0] % p[1] != 0 || (p[0] > 0 && (int64_t)p[2] * (p[0] / p[1]) < d->top_k)) return PMPE_ERR_SHAPE;
+    if (d->route_mode == PMPE_ROUTE_SOFT && p[1] != 1) return PMPE_ERR_SHAPE;
+  }
+  return PMPE_OK;
+}
+
+SelectArgs select_args(const pmpe_layer_desc* d, const pmpe_score_rule* r, int T) {
+  SelectArgs a{};
+  a.T = T;
+  a.n_pub = d->n_pub;
+  a.n_priv = d->n_priv;
+  a.k = d->top_k;
+  a.sigmoid = r->score == PMPE_SCORE_SIGMOID;
+  a.renorm = d->gate_mode == PMPE_GATE_RENORM_TOPK;
+  a.soft = d->route_mode == PMPE_ROUTE_SOFT;
+  a.groups_pub = r->n_group_pub;
+  a.keep_pub = r->topk_group_pub;
+  a.groups_priv = r->n_group_priv;
+  a.keep_priv = r->topk_group_priv;
+  a.group_top = r->group_top;
+  a.scale = r->scale;
+  a.zstride = d->n_pub + d->n_priv;
+  a.zsplit = 1;
+  return a;
+}
+
+}  // namespace pmpe
+
+extern "C" {
+
+pmpe_status pmpe_rmsnorm(int32_t T, int32_t H, int32_t dtype, const void* x, const void* residual,
+                         const void* weight, int32_t w_dtype, float eps, void* sum_out, void* out,
+                         uint8_t* out_q, uint8_t* out_scale, float* rstd, pmpe_stream_t stream) {
+  const pmpe_status st = check_rows(T, H);
+  if (st != PMPE_OK) return st;
+  if (!float_type(dtype) || !float_type(w_dtype)) return PMPE_ERR_DTYPE;
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return PMPE_ERR_SHAPE;
+  if (out_q && H % 32 != 0) return PMPE_ERR_SHAPE;
+  if (T == 0) return PMPE_OK;  // (arrays without elements may be NULL)
+  if (!x || !weight || (!out && !out_q) || (out_q != nullptr) != (out_scale != nullptr) ||
+      (residual != nullptr) != (sum_out != nullptr))
+    return PMPE_ERR_NULL;
+  const void* al[] = {x, residual, weight, sum_out, out, out_q};
+  for (const void* p : al)
+    if (p && !aligned16(p)) return PMPE_ERR_ALIGN;
+  NormArgs a{T, H, dtype == PMPE_BF16, w_dtype == PMPE_BF16, eps, x, residual, weight, sum_out, out, out_q,
+             out_scale, rstd};
+  return launched(launch_rmsnorm(a, (hipStream_t)stream));
+}
+
+size_t pmpe_rmsnorm_backward_workspace_bytes(int32_t T, int32_t H) {
+  if (check_rows(T, H) != PMPE_OK || T == 0) return 0;
+  return (size_t)rmsnorm_bwd_parts(T, H) * H * 4;
+}
+
+pmpe_status pmpe_rmsnorm_backward(int32_t T, int32_t H, int32_t dtype, const void* dy,
+                                  int32_t dy_dtype, const void* dres, const void* r,
+                                  const void* weight, int32_t w_dtype, const float* rstd, void* dx,
+                                  float* dweight, void* ws, size_t ws_bytes, pmpe_stream_t stream) {
+  const pmpe_status st = check_rows(T, H);
+  if (st != PMPE_OK) return st;
+  if (!float_type(dtype) || !float_type(w_dtype)) return PMPE_ERR_DTYPE;
+  if (dy_dtype != PMPE_F32 && dy_dtype != dtype) return PMPE_ERR_DTYPE;
+  if (T > 0 && (!dy || !r || !weight || !rstd || !dx)) return PMPE_ERR_NULL;
+  const void* al[] = {dy, dres, r, weight, dx, dweight};
+  for (const void* p : al)
+    if (p && !aligned16(p)) return PMPE_ERR_ALIGN;
+  const size_t need = pmpe_rmsnorm_backward_workspace_bytes(T, H);
+  if (dweight && need > 0) {
+    if (!ws || ws_bytes < need) return PMPE_ERR_WORKSPACE;
+    if (!aligned16(ws)) return PMPE_ERR_ALIGN;
+  }
+  if (T == 0 && !dweight) return PMPE_OK;
+  NormBwdArgs a{T, H, dtype == PMPE_BF16, dy_dtype == PMPE_F32, w_dtype == PMPE_BF16, dy, dres, r, weight, rstd,
+                dx, dweight, dweight ? (float*)ws : nullptr};
+  return launched(launch_rmsnorm_bwd(a, (hipStream_t)stream));
+}
+
+pmpe_status pmpe_select(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int32_t T,
+                        const void* logits, int32_t logits_dtype, const float* select_bias,
+                        const uint32_t* policy_word, int32_t* topk_idx, float* topk_gate,
+                        float* topk_logit, uint8_t* allow, float* margin, pmpe_stream_t stream) {
+  pmpe_status st = pmpe_check_desc(d, T);
+  if (st == PMPE_OK) st = check_rule(d, rule);
+  if (st != PMPE_OK) return st;
+  if (!float_type(logits_dtype)) return PMPE_ERR_DTYPE;
+  if (T == 0) return PMPE_OK;
+  if (!logits || !topk_idx || !topk_gate || !allow) return PMPE_ERR_NULL;
+  SelectArgs a = select_args(d, rule, T);
+  a.z = logits;
+  a.z_bf16 = logits_dtype == PMPE_BF16;
+  a.select_bias = select_bias;
+  a.words = policy_word;
+  a.topk_idx = topk_idx;
+  a.topk_gate = topk_gate;
+  a.topk_logit = topk_logit;
+  a.allow = allow;
+  a.margin = margin;
+  return launched(launch_select(a, (hipStream_t)stream));
+}
+
+pmpe_status pmpe_select_backward(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int32_t T,
+                                 const void* logits, int32_t logits_dtype, const int32_t* topk_idx,
+                                 const float* dgate, float* dlogits, pmpe_stream_t stream) {
+  pmpe_status st = pmpe_check_desc(d, T);
+  if (st == PMPE_OK) st = check_rule(d, rule);
+  if (st != PMPE_OK) return st;
+  if (!float_type(logits_dtype)) return PMPE_ERR_DTYPE;
+  if (T == 0) return PMPE_OK;
+  if (!logits || !topk_idx || !dgate || !dlogits) return PMPE_ERR_NULL;
+  SelectBwdArgs a{select_args(d, rule, T), dgate, dlogits};
+  a.f.z = logits;
+  a.f.z_bf16 = logits_dtype == PMPE_BF16;
+  a.f.topk_idx = const_cast<int32_t*>(topk_idx);
+  return launched(launch_select_bwd(a, (hipStream_t)stream));
+}
+
+}  // extern "C"

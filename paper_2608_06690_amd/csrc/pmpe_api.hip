@@ -200,6 +200,66 @@ pmpe_status check_audit(const pmpe_layer_desc* d, const AuditArgs& a) {
   return PMPE_OK;
 }
 
+// pmpe_backward, or with a rule (checked here) pmpe_backward_scored
+pmpe_status backward_impl(const pmpe_layer_desc* d, const pmpe_score_rule* rule, const float* topk_logit, int32_t T,
+                          const void* x, const void* dout,
+                          const int32_t* topk_idx, const float* topk_gate,
+                          const int32_t* expert_count, const int32_t* expert_offset,
+                          const int32_t* row_token, const int32_t* token_row, const void* y_perm,
+                          const float* wr_pub, const float* wr_priv, const void* w13_pub,
+                          const void* w2_pub, const void* w13_priv, const void* w2_priv,
+                          const float* logit_bias, const void* w13_sh, const void* w2_sh,
+                          const void* w2t_pub, const void* w13t_pub, const void* w2t_priv,
+                          const void* w13t_priv, const float* ab, float* dx, float* dw13_priv,
+                          float* dw2_priv, float* dwr_priv, uint32_t* grad_rows, void* ws,
+                          size_t ws_bytes, pmpe_stream_t stream) {
+  pmpe_status st = check_backward_desc(d, T);
+  if (st == PMPE_OK && rule) st = check_rule(d, rule);
+  if (st != PMPE_OK) return st;
+  const bool sigmoid = rule && rule->score == PMPE_SCORE_SIGMOID;
+  // a scale of 0 makes every gate 0: no gradient could be told from the gates
+  if (rule && rule->scale == 0.f) return PMPE_ERR_SHAPE;
+  if (sigmoid && !topk_logit) return PMPE_ERR_NULL;
+  if (!x || !dout || !topk_idx || !topk_gate || !expert_count || !expert_offset || !row_token ||
+      !token_row || !y_perm || !wr_pub || !w13_pub || !w2_pub || !dx)
+    return PMPE_ERR_NULL;
+  if (d->n_priv > 0 && (!wr_priv || !w13_priv || !w2_priv || !dw13_priv || !dw2_priv || !dwr_priv))
+    return PMPE_ERR_NULL;
+  if (d->n_shared > 0 && (!w13_sh || !w2_sh)) return PMPE_ERR_NULL;
+  // transposed weights: all of them (private ones when there is a private pool) or none
+  const bool any_t = w2t_pub || w13t_pub || w2t_priv || w13t_priv;
+  if (any_t && (!w2t_pub || !w13t_pub || (d->n_priv > 0 && (!w2t_priv || !w13t_priv))))
+    return PMPE_ERR_NULL;
+  const void* al[] = {x, dout, y_perm, w13_pub, w2_pub, w13_priv, w2_priv, ab, w13_sh, w2_sh,
+                      w2t_pub, w13t_pub, w2t_priv, w13t_priv, dx, dw13_priv, dw2_priv, dwr_priv};
+  for (const void* p : al)
+    if (p && !aligned16(p)) return PMPE_ERR_ALIGN;
+  if (T == 0) return PMPE_OK;
+  const BwdLayout L = bwd_layout(d, T);
+  if (!ws || ws_bytes < L.total) return PMPE_ERR_WORKSPACE;
+  if (!aligned16(ws)) return PMPE_ERR_ALIGN;
+  char* w = (char*)ws;
+  BwdArgs a{T, d->hidden, d->inter, d->top_k, d->n_pub, d->n_priv, x, dout, topk_idx, topk_gate,
+            expert_count, expert_offset, row_token, token_row, y_perm, wr_pub, wr_priv, w13_pub,
+            w2_pub, w13_priv, w2_priv, ab, dx, dw13_priv, dw2_priv, dwr_priv, grad_rows,
+            (uint16_t*)(w + L.xp), (uint16_t*)(w + L.dy), (float*)(w + L.ab), (uint16_t*)(w + L.hh),
+            (uint16_t*)(w + L.da), (float*)(w + L.dxr), (float*)(w + L.dz), (float*)(w + L.part),
+            d->gate_mode == PMPE_GATE_POOL_SOFTMAX && !sigmoid ? 1 : 0, d->route_mode == PMPE_ROUTE_SOFT ? 1 : 0,
+            bwd_pool_stride(d), logit_bias, (float*)(w + L.dzp),
+            d->n_shared > 0 ? d->n_shared * d->shared_inter : 0, w13_sh, w2_sh,
+            (float*)(w + L.absh), (uint16_t*)(w + L.dash),
+            d->n_shared > 0 ? (float*)(w + L.dxsh) : nullptr,
+            any_t ? w2t_pub : nullptr, w13t_pub, w2t_priv, w13t_priv, (uint16_t*)(w + L.dh),
+            L.P > 0 ? (uint16_t*)(w + L.tr) : nullptr, L.P, (float*)(w + L.grow)};
+  if (rule) {
+    a.gate_scale = rule->scale;
+    a.sigmoid = sigmoid;
+    a.renorm = d->gate_mode == PMPE_GATE_RENORM_TOPK;
+    a.topk_logit = topk_logit;
+  }
+  return launched(launch_backward(a, (hipStream_t)stream));
+}
+
 }  // namespace
 
 namespace pmpe {
@@ -228,6 +288,44 @@ const char* pmpe_status_string(int32_t status) {
 }
 
 pmpe_status pmpe_check_desc(const pmpe_layer_desc* d, int32_t T) { return check_desc(d, T); }
+
+pmpe_status pmpe_route_scored(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int32_t T,
+                              const void* x, const float* wr_pub, const float* wr_priv,
+                              const float* logit_bias, const float* select_bias,
+                              const uint32_t* policy_word, int32_t* topk_idx, float* topk_gate,
+                              float* topk_logit, uint8_t* allow, float* margin, uint32_t* dev_status,
+                              void* ws, size_t ws_bytes, pmpe_stream_t stream) {
+  pmpe_status st = check_desc(d, T);
+  if (st == PMPE_OK) st = check_rule(d, rule);
+  if (st != PMPE_OK) return st;
+  if (T == 0) return PMPE_OK;
+  if (!x || !wr_pub || !topk_idx || !topk_gate || !allow) return PMPE_ERR_NULL;
+  if (d->route_mode == PMPE_ROUTE_SOFT && !wr_priv) return PMPE_ERR_NULL;
+  if (!aligned16(x) || !aligned16(wr_pub) || (wr_priv && !aligned16(wr_priv))) return PMPE_ERR_ALIGN;
+  if (!ws || ws_bytes < route_ws(d, T)) return PMPE_ERR_WORKSPACE;
+  if (!aligned16(ws)) return PMPE_ERR_ALIGN;
+  RouteArgs r{T, d->hidden, d->n_pub, d->n_priv, d->top_k, d->gate_mode, d->act_dtype == PMPE_BF16, x, wr_pub, wr_priv,
+              logit_bias, policy_word, topk_idx, topk_gate, allow, margin, dev_status, (float*)ws, route_zstride(d),
+              d->route_mode == PMPE_ROUTE_SOFT ? 1 : 0,
+              route_ksplit(T, d->hidden, d->n_pub, d->n_priv, d->act_dtype == PMPE_BF16)};
+  SelectArgs a = select_args(d, rule, T);
+  a.z = ws;
+  a.zstride = r.zstride;
+  a.zpool = 1;
+  a.zsplit = r.zsplit;
+  a.select_bias = select_bias;
+  a.words = policy_word;
+  a.no_private = wr_priv == nullptr;
+  a.topk_idx = topk_idx;
+  a.topk_gate = topk_gate;
+  a.topk_logit = topk_logit;
+  a.allow = allow;
+  a.margin = margin;
+  a.dev_status = dev_status;
+  hipError_t e = launch_route_logits(r, (hipStream_t)stream);
+  if (e == hipSuccess) e = launch_select(a, (hipStream_t)stream);
+  return launched(e);
+}
 
 size_t pmpe_workspace_bytes(const pmpe_layer_desc* d, int32_t T) {
   if (check_desc(d, T) != PMPE_OK) return 0;
@@ -451,40 +549,23 @@ pmpe_status pmpe_backward(const pmpe_layer_desc* d, int32_t T, const void* x, co
                           const void* w13t_priv, const float* ab, float* dx, float* dw13_priv,
                           float* dw2_priv, float* dwr_priv, uint32_t* grad_rows, void* ws,
                           size_t ws_bytes, pmpe_stream_t stream) {
-  pmpe_status st = check_backward_desc(d, T);
-  if (st != PMPE_OK) return st;
-  if (!x || !dout || !topk_idx || !topk_gate || !expert_count || !expert_offset || !row_token ||
-      !token_row || !y_perm || !wr_pub || !w13_pub || !w2_pub || !dx)
-    return PMPE_ERR_NULL;
-  if (d->n_priv > 0 && (!wr_priv || !w13_priv || !w2_priv || !dw13_priv || !dw2_priv || !dwr_priv))
-    return PMPE_ERR_NULL;
-  if (d->n_shared > 0 && (!w13_sh || !w2_sh)) return PMPE_ERR_NULL;
-  // transposed weights: all of them (private ones when there is a private pool) or none
-  const bool any_t = w2t_pub || w13t_pub || w2t_priv || w13t_priv;
-  if (any_t && (!w2t_pub || !w13t_pub || (d->n_priv > 0 && (!w2t_priv || !w13t_priv))))
-    return PMPE_ERR_NULL;
-  const void* al[] = {x, dout, y_perm, w13_pub, w2_pub, w13_priv, w2_priv, ab, w13_sh, w2_sh,
-                      w2t_pub, w13t_pub, w2t_priv, w13t_priv, dx, dw13_priv, dw2_priv, dwr_priv};
-  for (const void* p : al)
-    if (p && !aligned16(p)) return PMPE_ERR_ALIGN;
-  if (T == 0) return PMPE_OK;
-  const BwdLayout L = bwd_layout(d, T);
-  if (!ws || ws_bytes < L.total) return PMPE_ERR_WORKSPACE;
-  if (!aligned16(ws)) return PMPE_ERR_ALIGN;
-  char* w = (char*)ws;
-  BwdArgs a{T, d->hidden, d->inter, d->top_k, d->n_pub, d->n_priv, x, dout, topk_idx, topk_gate,
-            expert_count, expert_offset, row_token, token_row, y_perm, wr_pub, wr_priv, w13_pub,
-            w2_pub, w13_priv, w2_priv, ab, dx, dw13_priv, dw2_priv, dwr_priv, grad_rows,
-            (uint16_t*)(w + L.xp), (uint16_t*)(w + L.dy), (float*)(w + L.ab), (uint16_t*)(w + L.hh),
-            (uint16_t*)(w + L.da), (float*)(w + L.dxr), (float*)(w + L.dz), (float*)(w + L.part),
-            d->gate_mode == PMPE_GATE_POOL_SOFTMAX ? 1 : 0, d->route_mode == PMPE_ROUTE_SOFT ? 1 : 0,
-            bwd_pool_stride(d), logit_bias, (float*)(w + L.dzp),
-            d->n_shared > 0 ? d->n_shared * d->shared_inter : 0, w13_sh, w2_sh,
-            (float*)(w + L.absh), (uint16_t*)(w + L.dash),
-            d->n_shared > 0 ? (float*)(w + L.dxsh) : nullptr,
-            any_t ? w2t_pub : nullptr, w13t_pub, w2t_priv, w13t_priv, (uint16_t*)(w + L.dh),
-            L.P > 0 ? (uint16_t*)(w + L.tr) : nullptr, L.P, (float*)(w + L.grow)};
-  return launched(launch_backward(a, (hipStream_t)stream));
+  return backward_impl(d, nullptr, nullptr, T, x, dout, topk_idx, topk_gate, expert_count, expert_offset, row_token, token_row, y_perm, wr_pub, wr_priv, w13_pub, w2_pub, w13_priv, w2_priv, logit_bias, w13_sh, w2_sh, w2t_pub, w13t_pub, w2t_priv, w13t_priv, ab, dx, dw13_priv, dw2_priv, dwr_priv, grad_rows, ws, ws_bytes, stream);
+}
+
+pmpe_status pmpe_backward_scored(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int32_t T,
+                                 const float* topk_logit, const void* x, const void* dout,
+                                 const int32_t* topk_idx, const float* topk_gate,
+                                 const int32_t* expert_count, const int32_t* expert_offset,
+                                 const int32_t* row_token, const int32_t* token_row, const void* y_perm,
+                                 const float* wr_pub, const float* wr_priv, const void* w13_pub,
+                                 const void* w2_pub, const void* w13_priv, const void* w2_priv,
+                                 const float* logit_bias, const void* w13_sh, const void* w2_sh,
+                                 const void* w2t_pub, const void* w13t_pub, const void* w2t_priv,
+                                 const void* w13t_priv, const float* ab, float* dx, float* dw13_priv,
+                                 float* dw2_priv, float* dwr_priv, uint32_t* grad_rows, void* ws,
+                                 size_t ws_bytes, pmpe_stream_t stream) {
+  if (!rule) return PMPE_ERR_NULL;
+  return backward_impl(d, rule, topk_logit, T, x, dout, topk_idx, topk_gate, expert_count, expert_offset, row_token, token_row, y_perm, wr_pub, wr_priv, w13_pub, w2_pub, w13_priv, w2_priv, logit_bias, w13_sh, w2_sh, w2t_pub, w13t_pub, w2t_priv, w13t_priv, ab, dx, dw13_priv, dw2_priv, dwr_priv, grad_rows, ws, ws_bytes, stream);
 }
 
 pmpe_status pmpe_layer_forward(const pmpe_layer_desc* d, int32_t T, pmpe_forward_args* args,

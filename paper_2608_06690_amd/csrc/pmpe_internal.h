@@ -323,6 +323,10 @@ struct BwdArgs {
   uint16_t* tr;
   int P;
   float* g_row;           // [T*k]: the gate of each row (its upstream rows are g_row[r] dout[t])
+  // routing by scores: the gates' scale, and with sigmoid scores the selected logits
+  float gate_scale = 1.f;
+  int sigmoid = 0, renorm = 0;
+  const float* topk_logit = nullptr;  // [T*k]
 };
 constexpr int BWD_DWR_SPLIT = 16;  // row chunks per private expert in the router-row gradient
 
@@ -353,6 +357,64 @@ struct WgradArgs {
   float* C;
 };
 hipError_t launch_wgrad(const WgradArgs& a, hipStream_t s);
+
+struct NormArgs {
+  int T, H, bf16, w_bf16;
+  float eps;
+  const void* x;
+  const void* residual;  // or NULL: r = x
+  const void* weight;
+  void* sum_out;         // r, with a residual
+  void* out;             // or NULL
+  uint8_t* out_q;        // or NULL: e4m3 [T, H] and their scales [T, H / 32]
+  uint8_t* out_scale;
+  float* rstd;           // [T] or NULL
+};
+hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s);
+
+struct NormBwdArgs {
+  int T, H, bf16, dy32, w_bf16;
+  const void* dy;
+  const void* dres;  // or NULL
+  const void* r;
+  const void* weight;
+  const float* rstd;
+  void* dx;
+  float* dw;         // [H] or NULL
+  float* dw_part;    // workspace [rmsnorm_bwd_parts(T, H), H], NULL without dw
+};
+int rmsnorm_bwd_parts(int T, int H);
+hipError_t launch_rmsnorm_bwd(const NormBwdArgs& a, hipStream_t s);
+
+struct SelectArgs {
+  int T, n_pub, n_priv, k, sigmoid, renorm, soft;
+  int groups_pub, keep_pub, groups_priv, keep_priv, group_top;
+  float scale;
+  const void* z;             // logits: [T, zstride], columns as experts, or (zpool) those of the token's pool
+  int z_bf16, zstride, zpool;
+  int zsplit;                // partial arrays [T, zstride] that are added in order
+  const float* select_bias;  // [E] or NULL
+  const uint32_t* words;
+  int no_private;            // no private router: every token routes as deny
+  int32_t* topk_idx;
+  float* topk_gate;
+  float* topk_logit;         // or NULL
+  uint8_t* allow;
+  float* margin;             // or NULL
+  uint32_t* dev_status;
+};
+// PMPE_OK if the rule fits a valid descriptor
+pmpe_status check_rule(const pmpe_layer_desc* d, const pmpe_score_rule* rule);
+// the rule's fields of SelectArgs
+SelectArgs select_args(const pmpe_layer_desc* d, const pmpe_score_rule* rule, int T);
+hipError_t launch_select(const SelectArgs& a, hipStream_t s);
+
+struct SelectBwdArgs {
+  SelectArgs f;        // the forward's rule, logits and selection (topk_idx is read)
+  const float* dgate;  // [T, k]
+  float* dlogits;      // [T, E]
+};
+hipError_t launch_select_bwd(const SelectBwdArgs& a, hipStream_t s);
 
 // Fingerprint tree: 1 KiB leaves, 16 digests per inner node.
 constexpr uint32_t kFpLeafBytes = 1024;

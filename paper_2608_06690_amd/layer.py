@@ -29,6 +29,7 @@ class LayerBuffers:
     ws: torch.Tensor
     dev_status: torch.Tensor
     ab: Optional[torch.Tensor] = None   # [T*k, 2I] fp32, filled by a training forward
+    topk_logit: Optional[torch.Tensor] = None  # [T*k] fp32, filled by routing with a score rule
 
 
 @dataclasses.dataclass
@@ -77,16 +78,24 @@ class PolicyMaskedMoE:
     Weights: wr_pub [n_pub, H] fp32, wr_priv [n_priv, H] fp32 (or None), bias [E] fp32 or
     None, w13_* [n, 2I, H], w2_* [n, H, I] in the activation dtype, shared group
     w13_sh [2 Is, H], w2_sh [H, Is] or None.
+
+    With a score rule (make_score_rule) the layer routes by scores: `rule` chooses and weights
+    the experts, select_bias [E] fp32 or None evens their load; kgap is then the margin
+    between the last selected expert and the next.
     """
 
     def __init__(self, desc: N.LayerDesc, wr_pub, wr_priv, bias, w13_pub, w2_pub, w13_priv,
-                 w2_priv, w13_sh=None, w2_sh=None, gather_in_dispatch: bool = False):
+                 w2_priv, w13_sh=None, w2_sh=None, gather_in_dispatch: bool = False,
+                 rule: Optional[N.ScoreRule] = None, select_bias: Optional[torch.Tensor] = None):
         self.desc = desc
         self.wr_pub, self.wr_priv, self.bias = wr_pub, wr_priv, bias
         self.w13_pub, self.w2_pub = w13_pub, w2_pub
         self.w13_priv, self.w2_priv = w13_priv, w2_priv
         self.w13_sh, self.w2_sh = w13_sh, w2_sh
         self.gather_in_dispatch = gather_in_dispatch
+        if select_bias is not None and rule is None:
+            raise ValueError("select_bias needs a score rule")
+        self.rule, self.select_bias = rule, select_bias
         self._bufs = {}
 
     @property
@@ -128,6 +137,12 @@ class PolicyMaskedMoE:
 
     def route(self, x, words, b: LayerBuffers, stream=None):
         T = x.shape[0]
+        if self.rule is not None:
+            if b.topk_logit is None:
+                b.topk_logit = torch.empty_like(b.topk_gate)
+            N.pmpe_route_scored(self.desc, self.rule, T, x, self.wr_pub, self.wr_priv, self.bias, self.select_bias, words,
+                                b.topk_idx, b.topk_gate, b.topk_logit, b.allow, b.kgap, b.dev_status, b.ws, stream)
+            return
         N.pmpe_route(self.desc, T, x, self.wr_pub, self.wr_priv, self.bias, words, b.topk_idx,
                      b.topk_gate, b.allow, b.kgap, b.dev_status, b.ws, stream)
 
@@ -159,8 +174,9 @@ class PolicyMaskedMoE:
     def _plain_steps(self) -> bool:
         # the steps and their library calls are the ones written here: where a subclass, an object,
         # the class or the binding has one replaced, the calls are made one by one
+        # (routing by scores has a call of its own)
         d = self.__dict__
-        return (type(self) is PolicyMaskedMoE and "route" not in d and "dispatch" not in d and "expert_ffn" not in d
+        return (self.rule is None and type(self) is PolicyMaskedMoE and "route" not in d and "dispatch" not in d and "expert_ffn" not in d
                 and "combine" not in d and "audit" not in d and _steps_of(PolicyMaskedMoE.__dict__) == _OWN_STEPS
                 and _calls_of(N.__dict__) == _OWN_CALLS)
 
@@ -302,6 +318,13 @@ class PolicyMaskedMoE:
         T = x.shape[0]
         g = g or self.grad_buffers(T)
         wt = self.transposed_weights(stream) if transposed else (None, None, None, None)
+        if self.rule is not None:
+            N.pmpe_backward_scored(self.desc, self.rule, T, b.topk_logit, x, dout, b.topk_idx, b.topk_gate,
+                                   b.expert_count, b.expert_offset, b.row_token, b.token_row, b.y_perm, self.wr_pub,
+                                   self.wr_priv, self.w13_pub, self.w2_pub, self.w13_priv, self.w2_priv, self.bias,
+                                   self.w13_sh, self.w2_sh, *wt, b.ab if use_saved else None, g.dx, g.dw13_priv,
+                                   g.dw2_priv, g.dwr_priv, g.grad_rows, g.ws, stream)
+            return g
         N.pmpe_backward(self.desc, T, x, dout, b.topk_idx, b.topk_gate, b.expert_count,
                         b.expert_offset, b.row_token, b.token_row, b.y_perm, self.wr_pub,
                         self.wr_priv, self.w13_pub, self.w2_pub, self.w13_priv, self.w2_priv,
