@@ -768,6 +768,52 @@ pmpe_status pmpe_backward_scored(const pmpe_layer_desc* d, const pmpe_score_rule
                                  float* dw2_priv, float* dwr_priv, uint32_t* grad_rows, void* ws,
                                  size_t ws_bytes, pmpe_stream_t stream);
 
+/*
+ * pmpe_grad_norm - global norm of a list of gradients, for clipping (the optimizer step of the
+ * private parameters, Sec. 3.2 and App. C.1; the paper does not say whether it clips).
+ *
+ *   norm[0] = sqrt(sum over the list of g^2)             summed in 64 bits, in a fixed order
+ *   norm[1] = min(1, max_norm / (norm[0] + 1e-6))        the factor that pmpe_clip_grads and
+ *                                                        pmpe_adamw_clipped apply
+ * A gradient with inf or NaN gives a norm of inf or NaN, and a factor of 0 or NaN.
+ *
+ *   grads, n, dtype   HOST arrays of `count` device pointers, element counts and types (PMPE_F32
+ *                     or PMPE_BF16), read during the call only; a tensor of 0 elements may have a
+ *                     NULL pointer; pointers need the alignment of their elements only
+ *   count             0 .. PMPE_MAX_GRADS; each n below 2^43
+ *   max_norm          > 0; +inf: no clipping (the factor is 1 for a finite norm)
+ *   norm              [2] fp32 out
+ *   ws                pmpe_grad_norm_workspace_bytes(n, count) bytes, 16-byte aligned
+ * Errors: PMPE_ERR_NULL, PMPE_ERR_SHAPE, PMPE_ERR_DTYPE, PMPE_ERR_ALIGN, PMPE_ERR_WORKSPACE.
+ */
+#define PMPE_MAX_GRADS (1 << 20)
+size_t pmpe_grad_norm_workspace_bytes(const uint64_t* n, int32_t count);
+
+pmpe_status pmpe_grad_norm(const void* const* grads, const uint64_t* n, const int32_t* dtype,
+                           int32_t count, double max_norm, float* norm, void* ws, size_t ws_bytes,
+                           pmpe_stream_t stream);
+
+/*
+ * pmpe_clip_grads - outs[i] = round(norm[1] * grads[i]) for every tensor of the list, with the norm
+ * that pmpe_grad_norm wrote. outs: HOST array of device pointers (tensors of the gradients' sizes
+ * and types), or NULL: in place. outs[i] may be grads[i] but must not overlap it otherwise; with a
+ * factor of 1, tensors clipped in place are not touched.
+ */
+pmpe_status pmpe_clip_grads(const void* const* grads, void* const* outs, const uint64_t* n,
+                            const int32_t* dtype, int32_t count, const float* norm,
+                            pmpe_stream_t stream);
+
+/*
+ * pmpe_adamw_clipped - pmpe_adamw on the gradient norm[1] * grad, with the norm that pmpe_grad_norm
+ * wrote (device, [2] fp32): the clipped gradients are never stored. A norm that is not finite makes
+ * the step leave param, master, m and v as they are. Other arguments and errors as pmpe_adamw, and
+ * PMPE_ERR_NULL without norm.
+ */
+pmpe_status pmpe_adamw_clipped(void* param, int32_t param_dtype, float* master, const float* grad,
+                               float* m, float* v, uint64_t n, int32_t step, float lr, float beta1,
+                               float beta2, float eps, float weight_decay, const float* norm,
+                               pmpe_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

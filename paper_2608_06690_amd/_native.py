@@ -181,6 +181,14 @@ _lib.pmpe_route_scored.restype = _I32
 _lib.pmpe_route_scored.argtypes = [_DESC, _RULE, _I32] + [_P] * 12 + [_P, _SZ, _P]
 _lib.pmpe_backward_scored.restype = _I32
 _lib.pmpe_backward_scored.argtypes = [_DESC, _RULE, _I32] + [_P] * 29 + [_P, _SZ, _P]
+_lib.pmpe_grad_norm_workspace_bytes.restype = _SZ
+_lib.pmpe_grad_norm_workspace_bytes.argtypes = [_P, _I32]
+_lib.pmpe_grad_norm.restype = _I32
+_lib.pmpe_grad_norm.argtypes = [_P, _P, _P, _I32, ctypes.c_double, _P, _P, _SZ, _P]
+_lib.pmpe_clip_grads.restype = _I32
+_lib.pmpe_clip_grads.argtypes = [_P, _P, _P, _P, _I32, _P, _P]
+_lib.pmpe_adamw_clipped.restype = _I32
+_lib.pmpe_adamw_clipped.argtypes = [_P, _I32, _P, _P, _P, _P, ctypes.c_uint64, _I32] + [ctypes.c_float] * 5 + [_P, _P]
 
 EXPORTED = ["pmpe_version", "pmpe_status_string", "pmpe_workspace_bytes", "pmpe_check_desc",
             "pmpe_route", "pmpe_dispatch", "pmpe_expert_ffn", "pmpe_combine", "pmpe_audit",
@@ -189,7 +197,8 @@ EXPORTED = ["pmpe_version", "pmpe_status_string", "pmpe_workspace_bytes", "pmpe_
             "pmpe_expert_ffn_lora_workspace_bytes", "pmpe_expert_ffn_lora", "pmpe_adamw",
             "pmpe_transpose_experts", "pmpe_expert_ffn_fp8", "pmpe_layer_forward",
             "pmpe_rmsnorm", "pmpe_rmsnorm_backward_workspace_bytes", "pmpe_rmsnorm_backward",
-            "pmpe_select", "pmpe_select_backward", "pmpe_route_scored", "pmpe_backward_scored"]
+            "pmpe_select", "pmpe_select_backward", "pmpe_route_scored", "pmpe_backward_scored",
+            "pmpe_grad_norm_workspace_bytes", "pmpe_grad_norm", "pmpe_clip_grads", "pmpe_adamw_clipped"]
 
 PMPE_FP_LEAF_BYTES = 1024
 PMPE_FP_FANOUT = 16
@@ -555,3 +564,76 @@ def pmpe_route_scored(desc, rule, T, x, wr_pub, wr_priv, logit_bias, select_bias
                                   _ptr(topk_gate), _ptr(topk_logit), _ptr(allow), _ptr(margin), _ptr(dev_status), _ptr(ws),
                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
            "pmpe_route_scored")
+
+
+class GradList:
+    """A list of gradients (fp32 or bf16 tensors of one device) with the arrays that
+    pmpe_grad_norm and pmpe_clip_grads take; a program whose gradients stay in the same
+    tensors makes it once. The tensors are kept alive."""
+
+    def __init__(self, tensors) -> None:
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        for i, t in enumerate(self.tensors):
+            _dtype(t, f"gradient {i}")
+            if t.device != self.tensors[0].device:
+                raise ValueError("the gradients of a list are on one device")
+        self.ptrs = (ctypes.c_void_p * n)(*[_ptr(t) for t in self.tensors])
+        self.sizes = (ctypes.c_uint64 * n)(*[t.numel() for t in self.tensors])
+        self.dtypes = (_I32 * n)(*[_DTYPES[t.dtype] for t in self.tensors])
+
+    def __len__(self) -> int:
+        return len(self.tensors)
+
+    @classmethod
+    def of(cls, grads) -> "GradList":
+        return grads if isinstance(grads, cls) else cls(grads)
+
+
+def pmpe_grad_norm_workspace_bytes(grads) -> int:
+    g = GradList.of(grads)
+    return int(_lib.pmpe_grad_norm_workspace_bytes(g.sizes, len(g)))
+
+
+def _norm_of(norm: torch.Tensor) -> torch.device:
+    dev = _here(norm, "norm")
+    _need_len(norm, "norm", 2, (torch.float32,), dev)
+    return dev
+
+
+def pmpe_grad_norm(grads, max_norm: float, norm: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """Global norm of the gradients (a GradList or tensors) and the factor that clips them to
+    max_norm, into norm [2] fp32."""
+    g, dev = GradList.of(grads), _norm_of(norm)
+    if len(g) and g.tensors[0].device != dev:
+        raise ValueError(f"the gradients are on {g.tensors[0].device}, not on {dev}")
+    _check(_lib.pmpe_grad_norm(g.ptrs, g.sizes, g.dtypes, len(g), max_norm, _ptr(norm), _ptr(ws), _need_bytes(ws, dev),
+                               _stream(stream)), "pmpe_grad_norm")
+
+
+def pmpe_clip_grads(grads, outs, norm: torch.Tensor, stream=None) -> None:
+    """The gradients times the factor of pmpe_grad_norm, into `outs` (None: in place)."""
+    g, dev = GradList.of(grads), _norm_of(norm)
+    if len(g) and g.tensors[0].device != dev:
+        raise ValueError(f"the gradients are on {g.tensors[0].device}, not on {dev}")
+    o = None
+    if outs is not None:
+        o = GradList.of(outs)
+        if len(o) != len(g) or bytes(o.sizes) != bytes(g.sizes) or bytes(o.dtypes) != bytes(g.dtypes) \
+                or (len(o) and o.tensors[0].device != dev):
+            raise ValueError("outs must be tensors of the gradients' sizes and types on their device")
+    _check(_lib.pmpe_clip_grads(g.ptrs, None if o is None else o.ptrs, g.sizes, g.dtypes, len(g), _ptr(norm),
+                                _stream(stream)), "pmpe_clip_grads")
+
+
+def pmpe_adamw_clipped(param: torch.Tensor, master: Optional[torch.Tensor], grad: torch.Tensor,
+                       m: torch.Tensor, v: torch.Tensor, step: int, lr: float, beta1: float, beta2: float,
+                       eps: float, weight_decay: float, norm: torch.Tensor, stream=None) -> None:
+    """pmpe_adamw on the gradient times the factor that pmpe_grad_norm wrote to `norm`."""
+    dev = _norm_of(norm)
+    for t, name in ((master, "master"), (grad, "grad"), (m, "m"), (v, "v")):
+        _need_len(t, name, param.numel(), (torch.float32,), dev)
+    _need_len(param, "param", param.numel(), tuple(_DTYPES), dev)
+    _check(_lib.pmpe_adamw_clipped(_ptr(param), _DTYPES[param.dtype], _ptr(master), _ptr(grad), _ptr(m), _ptr(v),
+                                   param.numel(), step, lr, beta1, beta2, eps, weight_decay, _ptr(norm), _stream(stream)),
+           "pmpe_adamw_clipped")

@@ -20,6 +20,19 @@ pmpe_status check_rows(int32_t T, int32_t H) {
   return T < 0 || T > PMPE_MAX_TOKENS || H < 1 || H > kNormMaxH ? PMPE_ERR_SHAPE : PMPE_OK;
 }
 
+// sizes, types and pointers of a list of gradients
+pmpe_status check_grads(const void* const* grads, const uint64_t* n, const int32_t* dtype, int32_t count) {
+  if (count < 0 || count > PMPE_MAX_GRADS) return PMPE_ERR_SHAPE;
+  if (count > 0 && (!grads || !n || !dtype)) return PMPE_ERR_NULL;
+  for (int32_t i = 0; i < count; ++i) {
+    if (!float_type(dtype[i])) return PMPE_ERR_DTYPE;
+    if (n[i] >= ((uint64_t)1 << 43)) return PMPE_ERR_SHAPE;
+    if (n[i] > 0 && !grads[i]) return PMPE_ERR_NULL;
+    if (((uintptr_t)grads[i] & (dtype[i] == PMPE_BF16 ? 1u : 3u)) != 0) return PMPE_ERR_ALIGN;
+  }
+  return PMPE_OK;
+}
+
 }  // namespace
 
 namespace pmpe {
@@ -147,6 +160,50 @@ pmpe_status pmpe_select_backward(const pmpe_layer_desc* d, const pmpe_score_rule
   a.f.z_bf16 = logits_dtype == PMPE_BF16;
   a.f.topk_idx = const_cast<int32_t*>(topk_idx);
   return launched(launch_select_bwd(a, (hipStream_t)stream));
+}
+
+size_t pmpe_grad_norm_workspace_bytes(const uint64_t* n, int32_t count) {
+  if (count < 0 || count > PMPE_MAX_GRADS || (count > 0 && !n)) return 0;
+  // launches of GRAD_LIST tensors, and one more wherever the chunks of a launch would pass 2^31
+  uint64_t elements = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (n[i] >= ((uint64_t)1 << 43)) return 0;
+    elements += n[i];
+  }
+  const uint64_t launches = (uint64_t)count / GRAD_LIST + 1 + 2 * (elements >> 43);
+  return (size_t)launches * GRAD_BLOCKS * sizeof(double);
+}
+
+pmpe_status pmpe_grad_norm(const void* const* grads, const uint64_t* n, const int32_t* dtype,
+                           int32_t count, double max_norm, float* norm, void* ws, size_t ws_bytes,
+                           pmpe_stream_t stream) {
+  const pmpe_status st = check_grads(grads, n, dtype, count);
+  if (st != PMPE_OK) return st;
+  if (!(max_norm > 0.0)) return PMPE_ERR_SHAPE;
+  if (!norm) return PMPE_ERR_NULL;
+  if (((uintptr_t)norm & 3u) != 0) return PMPE_ERR_ALIGN;
+  if (!ws || ws_bytes < pmpe_grad_norm_workspace_bytes(n, count)) return PMPE_ERR_WORKSPACE;
+  if (!aligned16(ws)) return PMPE_ERR_ALIGN;
+  return launched(launch_grad_norm(GradListArgs{grads, nullptr, n, dtype, count}, max_norm, norm, (double*)ws,
+                                   (hipStream_t)stream));
+}
+
+pmpe_status pmpe_clip_grads(const void* const* grads, void* const* outs, const uint64_t* n,
+                            const int32_t* dtype, int32_t count, const float* norm,
+                            pmpe_stream_t stream) {
+  const pmpe_status st = check_grads(grads, n, dtype, count);
+  if (st != PMPE_OK) return st;
+  if (!norm) return PMPE_ERR_NULL;
+  if (((uintptr_t)norm & 3u) != 0) return PMPE_ERR_ALIGN;
+  for (int32_t i = 0; outs && i < count; ++i) {
+    if (n[i] == 0) continue;
+    if (!outs[i]) return PMPE_ERR_NULL;
+    const uint64_t el = dtype[i] == PMPE_BF16 ? 2 : 4;
+    if (((uintptr_t)outs[i] & (el - 1)) != 0) return PMPE_ERR_ALIGN;
+    const uintptr_t g = (uintptr_t)grads[i], o = (uintptr_t)outs[i];
+    if (g != o && g < o + n[i] * el && o < g + n[i] * el) return PMPE_ERR_SHAPE;  // overlapping
+  }
+  return launched(launch_clip_grads(GradListArgs{grads, outs, n, dtype, count}, norm, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -11,12 +11,19 @@
 namespace pmpe {
 namespace {
 
-template <bool BF16>
+// CLIP: the gradient is norm[1] * grad, and a norm that is not finite ends the step (one more scalar
+// load per block: the step's time is the same).
+template <bool BF16, bool CLIP>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
   // 8 consecutive elements per thread and iteration: two 16-byte vectors of each of the
   // four input streams in flight per thread (non-temporal loads and stores measured slower)
   const uint64_t stride = (uint64_t)gridDim.x * 256 * 8;
   float* master = BF16 ? a.master : (float*)a.param;
+  float coef = 1.0f;
+  if constexpr (CLIP) {
+    if (!(a.norm[0] < INFINITY)) return;
+    coef = a.norm[1];
+  }
   for (uint64_t i0 = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8; i0 < a.n; i0 += stride) {
     const int cnt = (int)min((uint64_t)8, a.n - i0);
     float p[8], g[8], m[8], v[8];
@@ -41,6 +48,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
+      if constexpr (CLIP) g[j] *= coef;
       p[j] *= a.decay;
       m[j] = a.beta1 * m[j] + (1.0f - a.beta1) * g[j];
       v[j] = a.beta2 * v[j] + (1.0f - a.beta2) * g[j] * g[j];
@@ -73,10 +81,14 @@ hipError_t launch_adamw(const AdamwArgs& a, hipStream_t s) {
   if (a.n == 0) return hipSuccess;
   const uint64_t blocks = (a.n + 2047) / 2048;
   const unsigned grid = (unsigned)(blocks < 65536 ? blocks : 65536);
-  if (a.master)
-    adamw_kernel<true><<<grid, 256, 0, s>>>(a);
+  if (a.master && a.norm)
+    adamw_kernel<true, true><<<grid, 256, 0, s>>>(a);
+  else if (a.master)
+    adamw_kernel<true, false><<<grid, 256, 0, s>>>(a);
+  else if (a.norm)
+    adamw_kernel<false, true><<<grid, 256, 0, s>>>(a);
   else
-    adamw_kernel<false><<<grid, 256, 0, s>>>(a);
+    adamw_kernel<false, false><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -260,6 +260,26 @@ pmpe_status backward_impl(const pmpe_layer_desc* d, const pmpe_score_rule* rule,
   return launched(launch_backward(a, (hipStream_t)stream));
 }
 
+// pmpe_adamw, with a norm pmpe_adamw_clipped
+pmpe_status adamw_impl(void* param, int32_t param_dtype, float* master, const float* grad,
+                       float* m, float* v, uint64_t n, int32_t step, float lr, float beta1,
+                       float beta2, float eps, float weight_decay, const float* norm, pmpe_stream_t stream) {
+  if (param_dtype != PMPE_F32 && param_dtype != PMPE_BF16) return PMPE_ERR_DTYPE;
+  if ((param_dtype == PMPE_BF16) != (master != nullptr)) return PMPE_ERR_DTYPE;
+  if (step < 1 || !std::isfinite(lr) || !std::isfinite(eps) || !std::isfinite(weight_decay) ||
+      !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f))
+    return PMPE_ERR_SHAPE;
+  if (n == 0) return PMPE_OK;
+  if (!param || !grad || !m || !v) return PMPE_ERR_NULL;
+  const void* al[] = {param, master, grad, m, v};
+  for (const void* p : al)
+    if (p && !aligned16(p)) return PMPE_ERR_ALIGN;
+  const float c1 = (float)(1.0 - std::pow((double)beta1, (double)step));
+  const float c2 = (float)(1.0 - std::pow((double)beta2, (double)step));
+  AdamwArgs a{param, master, grad, m, v, n, lr, beta1, beta2, eps, 1.0f - lr * weight_decay, c1, c2, norm};
+  return launched(launch_adamw(a, (hipStream_t)stream));
+}
+
 }  // namespace
 
 namespace pmpe {
@@ -623,20 +643,16 @@ pmpe_status pmpe_layer_forward(const pmpe_layer_desc* d, int32_t T, pmpe_forward
 pmpe_status pmpe_adamw(void* param, int32_t param_dtype, float* master, const float* grad,
                        float* m, float* v, uint64_t n, int32_t step, float lr, float beta1,
                        float beta2, float eps, float weight_decay, pmpe_stream_t stream) {
-  if (param_dtype != PMPE_F32 && param_dtype != PMPE_BF16) return PMPE_ERR_DTYPE;
-  if ((param_dtype == PMPE_BF16) != (master != nullptr)) return PMPE_ERR_DTYPE;
-  if (step < 1 || !std::isfinite(lr) || !std::isfinite(eps) || !std::isfinite(weight_decay) ||
-      !(beta1 >= 0.f && beta1 < 1.f) || !(beta2 >= 0.f && beta2 < 1.f))
-    return PMPE_ERR_SHAPE;
-  if (n == 0) return PMPE_OK;
-  if (!param || !grad || !m || !v) return PMPE_ERR_NULL;
-  const void* al[] = {param, master, grad, m, v};
-  for (const void* p : al)
-    if (p && !aligned16(p)) return PMPE_ERR_ALIGN;
-  const float c1 = (float)(1.0 - std::pow((double)beta1, (double)step));
-  const float c2 = (float)(1.0 - std::pow((double)beta2, (double)step));
-  AdamwArgs a{param, master, grad, m, v, n, lr, beta1, beta2, eps, 1.0f - lr * weight_decay, c1, c2};
-  return launched(launch_adamw(a, (hipStream_t)stream));
+  return adamw_impl(param, param_dtype, master, grad, m, v, n, step, lr, beta1, beta2, eps, weight_decay, nullptr,
+                    stream);
+}
+
+pmpe_status pmpe_adamw_clipped(void* param, int32_t param_dtype, float* master, const float* grad,
+                               float* m, float* v, uint64_t n, int32_t step, float lr, float beta1,
+                               float beta2, float eps, float weight_decay, const float* norm,
+                               pmpe_stream_t stream) {
+  if (!norm) return PMPE_ERR_NULL;
+  return adamw_impl(param, param_dtype, master, grad, m, v, n, step, lr, beta1, beta2, eps, weight_decay, norm, stream);
 }
 
 pmpe_status pmpe_transpose_experts(const void* src, void* dst, int32_t n, int32_t rows,

@@ -256,6 +256,7 @@ struct AdamwArgs {
   float* v;
   uint64_t n;
   float lr, beta1, beta2, eps, decay, c1, c2;  // decay = 1 - lr wd; c = bias corrections
+  const float* norm = nullptr;  // clipped step: the gradients' norm and factor
 };
 hipError_t launch_adamw(const AdamwArgs& a, hipStream_t s);
 
@@ -415,6 +416,21 @@ struct SelectBwdArgs {
   float* dlogits;      // [T, E]
 };
 hipError_t launch_select_bwd(const SelectBwdArgs& a, hipStream_t s);
+
+// A list of gradients (host arrays, read during the call).
+struct GradListArgs {
+  const void* const* src;
+  void* const* dst;  // NULL: in place
+  const uint64_t* n;
+  const int32_t* dtype;
+  int count;
+};
+constexpr int GRAD_LIST = 96;      // tensors of a launch
+constexpr int GRAD_BLOCKS = 2048;  // blocks of a launch of the norm
+constexpr uint64_t GRAD_MAX_CHUNKS = (uint64_t)1 << 31;
+// part: GRAD_BLOCKS doubles per launch
+hipError_t launch_grad_norm(const GradListArgs& a, double max_norm, float* norm, double* part, hipStream_t s);
+hipError_t launch_clip_grads(const GradListArgs& a, const float* norm, hipStream_t s);
 
 // Fingerprint tree: 1 KiB leaves, 16 digests per inner node.
 constexpr uint32_t kFpLeafBytes = 1024;

@@ -357,10 +357,17 @@ _OWN_STEPS, _OWN_CALLS = _steps_of(PolicyMaskedMoE.__dict__), _calls_of(N.__dict
 class PrivateAdamW:
     """AdamW over a layer's private parameters only: the private router rows (fp32) and
     the private expert weights (bf16 with fp32 master copies). Public tensors are never
-    handed to the optimizer (they are not arguments of any call here)."""
+    handed to the optimizer (they are not arguments of any call here).
+
+    With max_norm the gradients of a step are clipped to that global norm; `norm` [2] then
+    holds the norm and the factor of the last step, and a step whose norm is not finite changes
+    nothing. Several layers are clipped together by step_clipped: their norm is taken over all
+    their gradients."""
 
     def __init__(self, layer: PolicyMaskedMoE, lr: float = 1e-4, betas=(0.9, 0.999),
-                 eps: float = 1e-8, weight_decay: float = 0.0):
+                 eps: float = 1e-8, weight_decay: float = 0.0, max_norm: Optional[float] = None):
+        if max_norm is not None and not max_norm > 0:
+            raise ValueError("max_norm must be above 0")
         self.layer = layer
         self.lr, self.betas, self.eps, self.wd = lr, betas, eps, weight_decay
         self.params = [layer.wr_priv, layer.w13_priv, layer.w2_priv]
@@ -368,14 +375,49 @@ class PrivateAdamW:
         self.m = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in self.params]
         self.v = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in self.params]
         self.t = 0
+        self.max_norm, self.norm, self._ws = max_norm, None, None
+
+    @staticmethod
+    def _grads(g: GradBuffers):
+        return [g.dwr_priv, g.dw13_priv, g.dw2_priv]
 
     def step(self, g: GradBuffers, stream=None) -> None:
+        if self.max_norm is not None:
+            step_clipped([(self, g)], self.max_norm, stream)
+            return
         self.t += 1
-        grads = [g.dwr_priv, g.dw13_priv, g.dw2_priv]
+        grads = self._grads(g)
         for p, mp, gr, m, v in zip(self.params, self.master, grads, self.m, self.v):
             N.pmpe_adamw(p, mp, gr, m, v, self.t, self.lr, self.betas[0], self.betas[1], self.eps,
                          self.wd, stream)
+        self._follow(stream)
+
+    def _follow(self, stream) -> None:
         # the backward's transposed copies of the private experts follow the update (once
         # per step, on the same stream), if the layer keeps them
         if getattr(self.layer, "_wt_priv", None) is not None:
             self.layer.refresh_private_transposes(stream)
+
+
+def step_clipped(steps, max_norm: float, stream=None) -> torch.Tensor:
+    """One optimizer step of several layers whose gradients are clipped together: steps are pairs
+    (PrivateAdamW, GradBuffers). Returns norm [2]: the global norm of all their private gradients
+    and the factor they were multiplied with (kept by the first optimizer, overwritten by its
+    next step)."""
+    steps = list(steps)
+    grads = N.GradList([t for opt, g in steps for t in opt._grads(g)])
+    first = steps[0][0]
+    need = N.pmpe_grad_norm_workspace_bytes(grads)
+    if first._ws is None or first._ws.numel() < need:
+        first._ws = torch.empty(need, dtype=torch.uint8, device=first.m[0].device)
+    if first.norm is None:
+        first.norm = torch.empty(2, dtype=torch.float32, device=first.m[0].device)
+    N.pmpe_grad_norm(grads, max_norm, first.norm, first._ws, stream)
+    for opt, g in steps:
+        opt.t += 1
+        for p, mp, gr, m, v in zip(opt.params, opt.master, opt._grads(g), opt.m, opt.v):
+            N.pmpe_adamw_clipped(p, mp, gr, m, v, opt.t, opt.lr, opt.betas[0], opt.betas[1], opt.eps, opt.wd,
+                                 first.norm, stream)
+        opt.norm = first.norm
+        opt._follow(stream)
+    return first.norm

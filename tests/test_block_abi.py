@@ -134,3 +134,54 @@ def test_a_balance_bias_needs_a_rule():
     w = torch.zeros(1)
     with pytest.raises(ValueError):
         P.PolicyMaskedMoE(P.make_desc(256, 128, 16, 8, 4), w, w, None, w, w, w, w, select_bias=w)
+
+
+def arrays(ptrs=(A, B), sizes=(10, 20), types=(F32, BF16)):
+    n = len(ptrs)
+    return (ctypes.c_void_p * n)(*ptrs), (ctypes.c_uint64 * n)(*sizes), (ctypes.c_int32 * n)(*types), n
+
+
+def grad_norm(a=None, max_norm=1.0, norm=C, ws=D, n=1 << 20):
+    p, s, t, c = a or arrays()
+    return N.lib().pmpe_grad_norm(p, s, t, c, max_norm, norm, ws, n, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(a=arrays((A, None))), NULL), (dict(norm=None), NULL), (dict(a=(None, None, None, 1)), NULL),
+    (dict(a=arrays(types=(F32, 2))), DTYPE), (dict(a=arrays(sizes=(1 << 43, 1))), SHAPE), (dict(a=(None, None, None, -1)), SHAPE),
+    (dict(a=(None, None, None, (1 << 20) + 1)), SHAPE), (dict(max_norm=0.0), SHAPE), (dict(max_norm=-1.0), SHAPE),
+    (dict(max_norm=float("nan")), SHAPE), (dict(a=arrays((A + 2, B))), ALIGN), (dict(a=arrays((A, B + 1))), ALIGN),
+    (dict(norm=C + 2), ALIGN), (dict(ws=None), WORKSPACE), (dict(n=16), WORKSPACE), (dict(ws=D + 8), ALIGN)])
+def test_grad_norm(kw, status):
+    assert grad_norm(**kw) == status
+
+
+def clip_grads(a=None, outs=None, norm=C):
+    p, s, t, c = a or arrays()
+    o = None if outs is None else (ctypes.c_void_p * len(outs))(*outs)
+    return N.lib().pmpe_clip_grads(p, o, s, t, c, norm, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(a=arrays((None, B))), NULL), (dict(norm=None), NULL), (dict(outs=(A, None)), NULL), (dict(outs=(D, E + 1)), ALIGN),
+    (dict(outs=(D + 2, E)), ALIGN), (dict(norm=C + 1), ALIGN), (dict(outs=(A + 4, B)), SHAPE), (dict(outs=(A, B - 2)), SHAPE),
+    (dict(a=(None, None, None, 0)), 0), (dict(a=arrays((None,), (0,), (F32,)), outs=(None,)), 0)])
+def test_clip_grads(kw, status):
+    assert clip_grads(**kw) == status
+
+
+def test_grad_norm_workspace():
+    size = lambda *n: N.lib().pmpe_grad_norm_workspace_bytes((ctypes.c_uint64 * len(n))(*n), len(n))  # noqa: E731
+    assert size() > 0 and size(5) == size(1 << 40) and size(*[1] * 96) == 2 * size(5)
+    assert size(1 << 43) == 0 and N.lib().pmpe_grad_norm_workspace_bytes(None, 1) == 0
+    assert N.lib().pmpe_grad_norm_workspace_bytes(None, -1) == 0
+
+
+def test_adamw_clipped():
+    f = N.lib().pmpe_adamw_clipped
+    hp = (1e-3, 0.9, 0.99, 1e-8, 0.0)
+    assert f(A, F32, None, B, C, D, 4, 1, *hp, None, None) == NULL
+    assert f(A, BF16, None, B, C, D, 4, 1, *hp, E, None) == DTYPE
+    assert f(A, F32, None, B, C, D, 4, 0, *hp, E, None) == SHAPE
+    assert f(A + 4, F32, None, B, C, D, 4, 1, *hp, E, None) == ALIGN
+    assert f(None, F32, None, B, C, D, 0, 1, *hp, E, None) == 0
