@@ -814,6 +814,36 @@ pmpe_status pmpe_adamw_clipped(void* param, int32_t param_dtype, float* master, 
                                float beta2, float eps, float weight_decay, const float* norm,
                                pmpe_stream_t stream);
 
+/*
+ * pmpe_expert_ffn_mx - pmpe_expert_ffn_fp8 with the activations in 8 bits too: the e4m3 values and
+ * block scales that pmpe_rmsnorm writes, h in the same format between the two products, products
+ * on the fp8 matrix instructions at twice the bf16 rate. A precision variant for serving (no
+ * backward), as pmpe_expert_ffn_fp8 is.
+ *
+ *   h = silu(X Wg^T) * (X Wu^T) in fp32, then e4m3(h / s) with s = 2^ceil(log2(amax / 448)) of every
+ *   32 consecutive values of a row;  y_perm[rows] = (s e4m3) Wd^T, rounded once to bf16
+ *
+ *   d            act_dtype PMPE_BF16 (of y_perm), w_dtype PMPE_FP8_E4M3, n_shared 0, inter a
+ *                multiple of 128
+ *   xq, xs       [T, H] e4m3 and [T, H / 32] e8m0 (uint8), not NULL; rows are gathered by token.
+ *                A scale of 255 (NaN) makes its block NaN
+ *   expert_count, expert_offset, row_token   pmpe_dispatch's
+ *   ws           pmpe_expert_ffn_mx_workspace_bytes(d, T) bytes
+ * Weights, their scales, the audit, missing private weights and errors as pmpe_expert_ffn_fp8; xq, xs,
+ * weights, y_perm and ws are 16-byte aligned.
+ */
+size_t pmpe_expert_ffn_mx_workspace_bytes(const pmpe_layer_desc* d, int32_t T);
+
+pmpe_status pmpe_expert_ffn_mx(const pmpe_layer_desc* d, int32_t T, const uint8_t* xq,
+                               const uint8_t* xs, const int32_t* expert_count,
+                               const int32_t* expert_offset, const int32_t* row_token,
+                               const void* w13_pub, const void* w2_pub, const void* w13_priv,
+                               const void* w2_priv, const float* w13s_pub, const float* w2s_pub,
+                               const float* w13s_priv, const float* w2s_priv, void* y_perm,
+                               uint32_t* audit_token_rows, uint32_t* audit_priv_calls,
+                               uint32_t* dev_status, void* ws, size_t ws_bytes,
+                               pmpe_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,7 +19,8 @@ from ._native import (PMPE_BF16, PMPE_F32, PMPE_GATE_POOL_SOFTMAX, PMPE_GATE_REN
                       pmpe_rmsnorm, pmpe_rmsnorm_backward, pmpe_rmsnorm_backward_workspace_bytes, PMPE_SCORE_SIGMOID,
                       PMPE_SCORE_SOFTMAX, ScoreRule, make_score_rule, pmpe_select, pmpe_select_backward,
                       pmpe_route_scored, pmpe_backward_scored, GradList, pmpe_grad_norm,
-                      pmpe_grad_norm_workspace_bytes, pmpe_clip_grads, pmpe_adamw_clipped)
-from .layer import (AuditBuffers, GradBuffers, LayerBuffers, PolicyMaskedMoE,  # noqa: F401
+                      pmpe_grad_norm_workspace_bytes, pmpe_clip_grads, pmpe_adamw_clipped, pmpe_expert_ffn_mx,
+                      pmpe_expert_ffn_mx_workspace_bytes)
+from .layer import (AuditBuffers, BlockBuffers, GradBuffers, LayerBuffers, NormedMoE, PolicyMaskedMoE,  # noqa: F401
                     PrivateAdamW, step_clipped)
 from .policy import policy_word, request_offsets, resolve_policy, token_policy_words  # noqa: F401

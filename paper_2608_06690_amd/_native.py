@@ -189,6 +189,10 @@ _lib.pmpe_clip_grads.restype = _I32
 _lib.pmpe_clip_grads.argtypes = [_P, _P, _P, _P, _I32, _P, _P]
 _lib.pmpe_adamw_clipped.restype = _I32
 _lib.pmpe_adamw_clipped.argtypes = [_P, _I32, _P, _P, _P, _P, ctypes.c_uint64, _I32] + [ctypes.c_float] * 5 + [_P, _P]
+_lib.pmpe_expert_ffn_mx_workspace_bytes.restype = _SZ
+_lib.pmpe_expert_ffn_mx_workspace_bytes.argtypes = [_DESC, _I32]
+_lib.pmpe_expert_ffn_mx.restype = _I32
+_lib.pmpe_expert_ffn_mx.argtypes = [_DESC, _I32] + [_P] * 17 + [_P, _SZ, _P]
 
 EXPORTED = ["pmpe_version", "pmpe_status_string", "pmpe_workspace_bytes", "pmpe_check_desc",
             "pmpe_route", "pmpe_dispatch", "pmpe_expert_ffn", "pmpe_combine", "pmpe_audit",
@@ -198,7 +202,8 @@ EXPORTED = ["pmpe_version", "pmpe_status_string", "pmpe_workspace_bytes", "pmpe_
             "pmpe_transpose_experts", "pmpe_expert_ffn_fp8", "pmpe_layer_forward",
             "pmpe_rmsnorm", "pmpe_rmsnorm_backward_workspace_bytes", "pmpe_rmsnorm_backward",
             "pmpe_select", "pmpe_select_backward", "pmpe_route_scored", "pmpe_backward_scored",
-            "pmpe_grad_norm_workspace_bytes", "pmpe_grad_norm", "pmpe_clip_grads", "pmpe_adamw_clipped"]
+            "pmpe_grad_norm_workspace_bytes", "pmpe_grad_norm", "pmpe_clip_grads", "pmpe_adamw_clipped",
+            "pmpe_expert_ffn_mx_workspace_bytes", "pmpe_expert_ffn_mx"]
 
 PMPE_FP_LEAF_BYTES = 1024
 PMPE_FP_FANOUT = 16
@@ -637,3 +642,23 @@ def pmpe_adamw_clipped(param: torch.Tensor, master: Optional[torch.Tensor], grad
     _check(_lib.pmpe_adamw_clipped(_ptr(param), _DTYPES[param.dtype], _ptr(master), _ptr(grad), _ptr(m), _ptr(v),
                                    param.numel(), step, lr, beta1, beta2, eps, weight_decay, _ptr(norm), _stream(stream)),
            "pmpe_adamw_clipped")
+
+
+def pmpe_expert_ffn_mx_workspace_bytes(desc: LayerDesc, T: int) -> int:
+    return int(_lib.pmpe_expert_ffn_mx_workspace_bytes(ctypes.byref(desc), T))
+
+
+def pmpe_expert_ffn_mx(desc, T, xq, xs, expert_count, expert_offset, row_token, w13_pub, w2_pub, w13_priv, w2_priv,
+                       w13s_pub, w2s_pub, w13s_priv, w2s_priv, y_perm, audit_token_rows, audit_priv_calls,
+                       dev_status, ws, stream=None) -> None:
+    """Expert FFN on 8-bit activations xq [T, H] with block scales xs [T, H / 32] (both uint8,
+    as pmpe_rmsnorm writes them) and 8-bit weights with row scales."""
+    dev, H = _here(xq, "xq"), desc.hidden
+    _need(xq, "xq", (T, H), (torch.uint8,), dev)
+    _need(xs, "xs", (T, H // 32), (torch.uint8,), dev)
+    _need_len(y_perm, "y_perm", T * desc.top_k * H, (torch.bfloat16,), dev)
+    _check(_lib.pmpe_expert_ffn_mx(
+        ctypes.byref(desc), T, _ptr(xq), _ptr(xs), _ptr(expert_count), _ptr(expert_offset), _ptr(row_token),
+        _ptr(w13_pub), _ptr(w2_pub), _ptr(w13_priv), _ptr(w2_priv), _ptr(w13s_pub), _ptr(w2s_pub), _ptr(w13s_priv),
+        _ptr(w2s_priv), _ptr(y_perm), _ptr(audit_token_rows), _ptr(audit_priv_calls), _ptr(dev_status), _ptr(ws),
+        _need_bytes(ws, dev), _stream(stream)), "pmpe_expert_ffn_mx")

@@ -20,6 +20,19 @@ pmpe_status check_rows(int32_t T, int32_t H) {
   return T < 0 || T > PMPE_MAX_TOKENS || H < 1 || H > kNormMaxH ? PMPE_ERR_SHAPE : PMPE_OK;
 }
 
+size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
+
+// the descriptor of the 8-bit experts: the bf16 path's checks, with the weight type read as bf16
+pmpe_status check_mx(const pmpe_layer_desc* d, int32_t T) {
+  if (!d) return PMPE_ERR_NULL;
+  if (d->act_dtype != PMPE_BF16 || d->w_dtype != PMPE_FP8_E4M3) return PMPE_ERR_DTYPE;
+  pmpe_layer_desc db = *d;
+  db.w_dtype = PMPE_BF16;
+  const pmpe_status st = pmpe_check_desc(&db, T);
+  if (st != PMPE_OK) return st;
+  return d->n_shared != 0 || d->inter % 128 != 0 ? PMPE_ERR_SHAPE : PMPE_OK;
+}
+
 // sizes, types and pointers of a list of gradients
 pmpe_status check_grads(const void* const* grads, const uint64_t* n, const int32_t* dtype, int32_t count) {
   if (count < 0 || count > PMPE_MAX_GRADS) return PMPE_ERR_SHAPE;
@@ -204,6 +217,41 @@ pmpe_status pmpe_clip_grads(const void* const* grads, void* const* outs, const u
     if (g != o && g < o + n[i] * el && o < g + n[i] * el) return PMPE_ERR_SHAPE;  // overlapping
   }
   return launched(launch_clip_grads(GradListArgs{grads, outs, n, dtype, count}, norm, (hipStream_t)stream));
+}
+
+size_t pmpe_expert_ffn_mx_workspace_bytes(const pmpe_layer_desc* d, int32_t T) {
+  if (check_mx(d, T) != PMPE_OK) return 0;
+  const size_t n = (size_t)T * d->top_k * d->inter;
+  return round_up(n) + round_up(n / 32);
+}
+
+pmpe_status pmpe_expert_ffn_mx(const pmpe_layer_desc* d, int32_t T, const uint8_t* xq,
+                               const uint8_t* xs, const int32_t* expert_count,
+                               const int32_t* expert_offset, const int32_t* row_token,
+                               const void* w13_pub, const void* w2_pub, const void* w13_priv,
+                               const void* w2_priv, const float* w13s_pub, const float* w2s_pub,
+                               const float* w13s_priv, const float* w2s_priv, void* y_perm,
+                               uint32_t* audit_token_rows, uint32_t* audit_priv_calls,
+                               uint32_t* dev_status, void* ws, size_t ws_bytes,
+                               pmpe_stream_t stream) {
+  const pmpe_status st = check_mx(d, T);
+  if (st != PMPE_OK) return st;
+  if (T == 0) return PMPE_OK;
+  if (!xq || !xs || !expert_count || !expert_offset || !row_token || !w13_pub || !w2_pub || !w13s_pub || !w2s_pub ||
+      !y_perm || !audit_token_rows)
+    return PMPE_ERR_NULL;
+  if ((w13_priv != nullptr) != (w13s_priv != nullptr) || (w2_priv != nullptr) != (w2s_priv != nullptr))
+    return PMPE_ERR_NULL;
+  const void* al[] = {xq, xs, w13_pub, w2_pub, w13_priv, w2_priv, y_perm};
+  for (const void* p : al)
+    if (p && !aligned16(p)) return PMPE_ERR_ALIGN;
+  if (!ws || ws_bytes < pmpe_expert_ffn_mx_workspace_bytes(d, T)) return PMPE_ERR_WORKSPACE;
+  if (!aligned16(ws)) return PMPE_ERR_ALIGN;
+  uint8_t* hq = (uint8_t*)ws;
+  MxFfnArgs a{T, d->hidden, d->inter, d->n_pub, d->n_priv, d->top_k, xq, xs, expert_offset, row_token,
+              w13_pub, w2_pub, w13_priv, w2_priv, w13s_pub, w2s_pub, w13s_priv, w2s_priv, y_perm,
+              audit_token_rows, audit_priv_calls, dev_status, hq, hq + round_up((size_t)T * d->top_k * d->inter)};
+  return launched(launch_expert_ffn_mx(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

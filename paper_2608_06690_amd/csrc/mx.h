@@ -23,4 +23,26 @@ __device__ __forceinline__ uint32_t mx_pack4(float a, float b, float c, float d)
   return (uint32_t)v;
 }
 
+// Largest magnitude of 8 values of a block; +inf if one is not finite.
+__device__ __forceinline__ float mx_amax8(const float (&v)[8]) {
+  float m = 0.f;
+  bool fine = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    m = fmaxf(m, fabsf(v[i]));
+    fine = fine && fabsf(v[i]) < INFINITY;
+  }
+  return fine ? m : INFINITY;
+}
+// The block's 8 values as bytes, with amax of the whole block of 32; returns the scale's exponent.
+// A block with a value that is not finite holds NaN only.
+__device__ __forceinline__ int mx_pack8(const float (&v)[8], float amax, uint32_t& q0, uint32_t& q1) {
+  const int e = mx_exponent(amax);
+  const float inv = mx_pow2(-e);
+  q0 = mx_pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  q1 = mx_pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+  if (!(amax < INFINITY)) q0 = q1 = 0x7F7F7F7Fu;
+  return e;
+}
+
 }  // namespace pmpe

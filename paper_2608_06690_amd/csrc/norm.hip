@@ -133,24 +133,14 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_kernel(NormArgs
     for (int j = 0; j < 8; ++j) w[j] *= r[v][j] * rstd;
     if (a.out) store8<BF16>((char*)a.out + row * el, i, H, w);
     if (a.out_q) {  // (H is a multiple of 32: the four lanes of a block are all inside or all past it)
-      float amax = 0.f;
-      bool fine = true;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        amax = fmaxf(amax, fabsf(w[j]));
-        fine = fine && fabsf(w[j]) < INFINITY;
-      }
-      if (!fine) amax = INFINITY;
+      float amax = mx_amax8(w);
       amax = fmaxf(amax, __shfl_xor(amax, 1, 64));
       amax = fmaxf(amax, __shfl_xor(amax, 2, 64));
-      const int e = mx_exponent(amax);
       if (i < H) {
         typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        const float inv = mx_pow2(-e);
-        u32x2 q{mx_pack4(w[0] * inv, w[1] * inv, w[2] * inv, w[3] * inv),
-                mx_pack4(w[4] * inv, w[5] * inv, w[6] * inv, w[7] * inv)};
-        if (!(amax < INFINITY)) q = u32x2{0x7F7F7F7Fu, 0x7F7F7F7Fu};
-        *(u32x2*)(a.out_q + row + i) = q;
+        uint32_t q0, q1;
+        const int e = mx_pack8(w, amax, q0, q1);
+        *(u32x2*)(a.out_q + row + i) = u32x2{q0, q1};
         if ((l & 3) == 0) a.out_scale[(row + i) >> 5] = (uint8_t)(e + 127);
       }
     }

@@ -359,6 +359,30 @@ struct WgradArgs {
 };
 hipError_t launch_wgrad(const WgradArgs& a, hipStream_t s);
 
+// Expert FFN on 8-bit activations and weights (mx.h).
+struct MxFfnArgs {
+  int T, H, I, n_pub, n_priv, k;
+  const uint8_t* xq;  // [T, H] e4m3, and their scales [T, H / 32] e8m0
+  const uint8_t* xs;
+  const int32_t* offset;
+  const int32_t* row_token;
+  const void* w13_pub;
+  const void* w2_pub;
+  const void* w13_priv;
+  const void* w2_priv;
+  const float* w13s_pub;
+  const float* w2s_pub;
+  const float* w13s_priv;
+  const float* w2s_priv;
+  void* y_perm;
+  uint32_t* audit_rows;
+  uint32_t* audit_calls;
+  uint32_t* dev_status;
+  uint8_t* hq;  // workspace [T*k, I] and [T*k, I / 32]
+  uint8_t* hs;
+};
+hipError_t launch_expert_ffn_mx(const MxFfnArgs& a, hipStream_t s);
+
 struct NormArgs {
   int T, H, bf16, w_bf16;
   float eps;

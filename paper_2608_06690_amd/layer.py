@@ -245,6 +245,27 @@ class PolicyMaskedMoE:
             self.audit(T, b, audit, req_offset, stream)
         return b
 
+    def forward_mx(self, x, xq, xs, words, fp8, audit: AuditBuffers, req_offset=None, stream=None) -> LayerBuffers:
+        """The layer with 8-bit activations and weights: x [T, H] bf16 is routed, its 8-bit form
+        xq [T, H] with scales xs [T, H / 32] (pmpe_rmsnorm writes both) goes through the experts;
+        fp8 as in forward_fp8."""
+        T = x.shape[0]
+        b = self.buffers(T)
+        self.route(x, words, b, stream)
+        N.pmpe_dispatch(self.desc, T, b.topk_idx, x, b.expert_count, b.expert_offset, b.row_token, b.token_row, None,
+                        b.ws, stream)
+        d8 = N.LayerDesc(*[getattr(self.desc, f) for f, _ in N.LayerDesc._fields_])
+        d8.w_dtype = N.PMPE_FP8_E4M3
+        ws_bytes = N.pmpe_expert_ffn_mx_workspace_bytes(d8, T)
+        if b.ws.numel() < ws_bytes:
+            b.ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+        N.pmpe_expert_ffn_mx(d8, T, xq, xs, b.expert_count, b.expert_offset, b.row_token, *fp8, b.y_perm,
+                             audit.token_rows, audit.priv_calls, b.dev_status, b.ws, stream)
+        self.combine(x, b, stream)
+        if req_offset is not None:
+            self.audit(T, b, audit, req_offset, stream)
+        return b
+
     def route_record(self, T: int, b: LayerBuffers, req_offset, layer: int = 0,
                      rec: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Route records of the last forward of this T: [T, 4] int32 (pmpe_route_rec)."""
@@ -352,6 +373,78 @@ class PolicyMaskedMoE:
 
 
 _OWN_STEPS, _OWN_CALLS = _steps_of(PolicyMaskedMoE.__dict__), _calls_of(N.__dict__)
+
+
+@dataclasses.dataclass
+class BlockBuffers:
+    residual: torch.Tensor                # [T, H]: h + delta, the residual stream (the caller's h without delta)
+    norm: torch.Tensor                    # [T, H]: its norm, the layer's input
+    rstd: torch.Tensor                    # [T] fp32
+    layer: Optional[LayerBuffers] = None  # the layer's buffers of the last forward
+    norm_q: Optional[torch.Tensor] = None      # [T, H] uint8 and [T, H / 32] uint8: the norm in 8 bits
+    norm_scale: Optional[torch.Tensor] = None
+    total: Optional[torch.Tensor] = None       # the buffer of h + delta
+
+
+class NormedMoE:
+    """A policy-masked layer with the residual add and RMS norm ahead of it:
+
+        residual = h + delta;  out = layer(norm(residual))
+
+    delta is what the sublayer before added to the stream (None: nothing); the next block gets
+    (residual, out) as its (h, delta). weight [H] fp32 or bf16 is the norm's, which is frozen with
+    the public model unless a backward is given a dweight to fill."""
+
+    def __init__(self, layer: PolicyMaskedMoE, weight: torch.Tensor, eps: float = 1e-6):
+        self.layer, self.weight, self.eps = layer, weight, eps
+        self._bufs = {}
+
+    def buffers(self, T: int) -> BlockBuffers:
+        if T not in self._bufs:
+            H, dev = self.layer.desc.hidden, self.layer.device
+            act = dict(dtype=self.layer.act_dtype, device=dev)
+            norm = torch.empty(T, H, **act)
+            self._bufs[T] = BlockBuffers(norm, norm, torch.empty(T, dtype=torch.float32, device=dev))
+        return self._bufs[T]
+
+    def _norm(self, h, delta, b: BlockBuffers, stream) -> None:
+        if delta is not None and b.total is None:
+            b.total = torch.empty_like(b.norm)
+        b.residual = h if delta is None else b.total
+        N.pmpe_rmsnorm(h, delta, self.weight, self.eps, None if delta is None else b.residual, b.norm, b.norm_q,
+                       b.norm_scale, b.rstd, stream)
+
+    def forward(self, h, delta, words, audit: AuditBuffers, req_offset=None, stream=None,
+                train: bool = False) -> BlockBuffers:
+        """Returns the buffers of this T: residual, and layer.out."""
+        b = self.buffers(h.shape[0])
+        self._norm(h, delta, b, stream)
+        b.layer = self.layer.forward(b.norm, words, audit, req_offset, stream, train)
+        return b
+
+    def forward_mx(self, h, delta, words, fp8, audit: AuditBuffers, req_offset=None, stream=None) -> BlockBuffers:
+        """The block with 8-bit activations and weights (PolicyMaskedMoE.forward_mx)."""
+        T, H = h.shape
+        b = self.buffers(T)
+        if b.norm_q is None:
+            b.norm_q = torch.empty(T, H, dtype=torch.uint8, device=h.device)
+            b.norm_scale = torch.empty(T, H // 32, dtype=torch.uint8, device=h.device)
+        self._norm(h, delta, b, stream)
+        b.layer = self.layer.forward_mx(b.norm, b.norm_q, b.norm_scale, words, fp8, audit, req_offset, stream)
+        return b
+
+    def backward(self, dresidual, dout, b: BlockBuffers, dx: torch.Tensor, g: Optional[GradBuffers] = None,
+                 dweight: Optional[torch.Tensor] = None, stream=None) -> GradBuffers:
+        """Backward of the training forward that filled `b`: dout is the gradient of layer.out,
+        dresidual that of the residual (None: none). Fills dx (the gradient of h and of delta, in the
+        activation type) and, if given, dweight [H] fp32; returns the layer's gradients."""
+        g = self.layer.backward(b.norm, dout, b.layer, g, stream)
+        T, H = b.norm.shape
+        ws = None
+        if dweight is not None:
+            ws = torch.empty(N.pmpe_rmsnorm_backward_workspace_bytes(T, H), dtype=torch.uint8, device=b.norm.device)
+        N.pmpe_rmsnorm_backward(g.dx, dresidual, b.residual, self.weight, b.rstd, dx, dweight, ws, stream)
+        return g
 
 
 class PrivateAdamW:

@@ -185,3 +185,36 @@ def test_adamw_clipped():
     assert f(A, F32, None, B, C, D, 4, 0, *hp, E, None) == SHAPE
     assert f(A + 4, F32, None, B, C, D, 4, 1, *hp, E, None) == ALIGN
     assert f(None, F32, None, B, C, D, 0, 1, *hp, E, None) == 0
+
+
+def mx(d=None, T=4, xq=A, xs=B, cnt=C, off=C, rt=C, w=(A, A, A, A), s=(B, B, B, B), y=D, rows=C, ws=E, n=1 << 30):
+    if d is None:
+        d = P.make_desc(2048, 768, 128, 32, 8)
+        d.w_dtype = N.PMPE_FP8_E4M3
+    return N.lib().pmpe_expert_ffn_mx(ctypes.byref(d), T, xq, xs, cnt, off, rt, *w, *s, y, rows, None, None, ws, n, None)
+
+
+def mx_desc(**kw):
+    v = dict(hidden=2048, inter=768, n_pub=128, n_priv=32, top_k=8)
+    v.update(kw)
+    d = P.make_desc(**v)
+    d.w_dtype = N.PMPE_FP8_E4M3
+    return d
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(d=P.make_desc(2048, 768, 128, 32, 8)), DTYPE), (dict(d=mx_desc(inter=704)), SHAPE), (dict(d=mx_desc(hidden=192)), SHAPE),
+    (dict(d=mx_desc(n_shared=1, shared_inter=128)), SHAPE), (dict(d=mx_desc(top_k=33)), SHAPE), (dict(T=-1), SHAPE),
+    (dict(xq=None), NULL), (dict(xs=None), NULL), (dict(cnt=None), NULL), (dict(off=None), NULL), (dict(rt=None), NULL),
+    (dict(y=None), NULL), (dict(rows=None), NULL), (dict(w=(None, A, A, A)), NULL), (dict(s=(B, None, B, B)), NULL),
+    (dict(w=(A, A, None, A)), NULL), (dict(s=(B, B, B, None)), NULL), (dict(xq=A + 8), ALIGN), (dict(y=D + 2), ALIGN),
+    (dict(w=(A + 4, A, A, A)), ALIGN), (dict(ws=None), WORKSPACE), (dict(n=4 * 8 * 768), WORKSPACE), (dict(ws=E + 4), ALIGN),
+    (dict(T=0, xq=None), 0)])
+def test_expert_ffn_mx(kw, status):
+    assert mx(**kw) == status
+
+
+def test_expert_ffn_mx_workspace():
+    assert P.pmpe_expert_ffn_mx_workspace_bytes(mx_desc(), 4) >= 4 * 8 * 768 * 33 // 32
+    assert P.pmpe_expert_ffn_mx_workspace_bytes(mx_desc(inter=704), 4) == 0
+    assert N.lib().pmpe_expert_ffn_mx_workspace_bytes(None, 4) == 0
