@@ -248,7 +248,7 @@ pmpe_status pmpe_expert_ffn_mx(const pmpe_layer_desc* d, int32_t T, const uint8_
   if (!ws || ws_bytes < pmpe_expert_ffn_mx_workspace_bytes(d, T)) return PMPE_ERR_WORKSPACE;
   if (!aligned16(ws)) return PMPE_ERR_ALIGN;
   uint8_t* hq = (uint8_t*)ws;
-  MxFfnArgs a{T, d->hidden, d->inter, d->n_pub, d->n_priv, d->top_k, xq, xs, expert_offset, row_token,
+  MxFfnArgs a{T, d->hidden, d->inter, d->n_pub, d->n_priv, d->top_k, xq, xs, expert_count, expert_offset, row_token,
               w13_pub, w2_pub, w13_priv, w2_priv, w13s_pub, w2s_pub, w13s_priv, w2s_priv, y_perm,
               audit_token_rows, audit_priv_calls, dev_status, hq, hq + round_up((size_t)T * d->top_k * d->inter)};
   return launched(launch_expert_ffn_mx(a, (hipStream_t)stream));

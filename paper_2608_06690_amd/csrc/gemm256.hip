@@ -7,6 +7,9 @@
 //          rows to the execution audit;
 //   plain  GEMM2 without the audit, its A rows read in place or gathered by token (the
 //          backward's products with transposed weights).
+//   MX     GEMM1 and GEMM2 on 8-bit operands (mx.h): activations with block scales, weights with row
+//          scales, K steps of 128 values. Such a step has the bytes, the fragments and, on the
+//          scaled fp8 instruction, the matrix time of a bf16 step of 64, so the schedule is the same.
 //
 // Tile list: groups are the routed experts and the shared group; a tile is (group, M tile of
 // 256 rows, N tile). Every block scans the per-group tile counts on the device, so groups
@@ -44,22 +47,27 @@
 // us (1,315 with a reciprocal in place of silu's division), DeepSeek-V2-Lite-shaped 8192-token
 // layer 1,307 -> 1,240, Qwen3-30B-A3B-shaped 4096-token layer 558 -> 502.
 #include "lds_dma.h"
+#include "mx.h"
 #include "pmpe_internal.h"
 
 namespace pmpe {
 namespace {
 
-constexpr int BM = 256, BN = 256, BK = 64, THREADS = 512;
-constexpr int HALF = 128 * 128;             // bytes of a half tile (128 rows x 64 bf16)
+constexpr int BM = 256, BN = 256, THREADS = 512;
+constexpr int BKB = 128;                    // bytes of an operand row per K step (64 bf16, 128 fp8)
+constexpr int HALF = 128 * BKB;             // bytes of a half tile (128 rows)
 constexpr int STEP = 4 * HALF;              // one step's slots: A0 A1 B0 B1
 constexpr int MAXG = 2 * PMPE_MAX_POOL + 1;  // routed experts + the shared group
-constexpr int LIST = 256;                   // tiles of a block whose description is kept in LDS
+constexpr int LIST = 256;                   // tiles of a block whose description is kept in LDS (MX: half)
 constexpr int NRT = 4;                      // row_token slices in flight (see issue_rt)
 
 template <int N>
 constexpr std::integral_constant<int, N> ic{};
 
-enum { G1 = 0, G1_SAVE = 1, G2 = 2, PLAIN = 3, GATHER = 4 };
+enum { G1 = 0, G1_SAVE = 1, G2 = 2, PLAIN = 3, GATHER = 4, MX_UP = 5, MX_DOWN = 6 };
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x16 __attribute__((ext_vector_type(16)));
 
 struct TileInfo {
   int g;     // group: expert id, or E for the shared group
@@ -83,17 +91,22 @@ constexpr uint32_t NO_STORE = 0x7FFFFFF0u;  // past every buffer's size: the sto
 
 template <int MODE>
 __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
-  constexpr bool GATED = MODE == G1 || MODE == G1_SAVE, SAVE = MODE == G1_SAVE;
-  constexpr bool AUDIT = MODE == G2, GATHER_A = MODE == GATHER;
+  constexpr bool MX = MODE == MX_UP || MODE == MX_DOWN;
+  constexpr bool GATED = MODE == G1 || MODE == G1_SAVE || MODE == MX_UP, SAVE = MODE == G1_SAVE;
+  constexpr bool AUDIT = MODE == G2 || MODE == MX_DOWN, GATHER_A = MODE == GATHER;
+  constexpr int ESZ = MX ? 1 : 2;                // bytes of an operand element
+  constexpr int NLIST = MX ? LIST / 2 : LIST;
   constexpr int NCOLS = GATED ? BN / 2 : BN;  // output columns per tile
   // Stores a wave issues for a tile with both A halves, by the phase of the last step that
   // they follow the copies of (S2..S4) and after that step (S5); for a tile without A1: S2, S5.
-  constexpr int SQ = GATED ? (SAVE ? 5 : 1) : 1;  // per 16-row block and output half
+  constexpr int SQ = GATED ? (SAVE ? 5 : MX ? 2 : 1) : 1;  // per 16-row block and output half
   constexpr int S2 = GATED ? 0 : 4, S3 = GATED ? 2 * SQ : 4, S4 = GATED ? 2 * SQ : 4, S5 = 4 * SQ;
   constexpr int SALL = S2 + S3 + S4 + S5;
   __shared__ __attribute__((aligned(16))) unsigned char smem[2 * STEP];
   __shared__ __attribute__((aligned(16))) int s_rt[NRT][BM];
-  __shared__ __attribute__((aligned(16))) int4 s_list[LIST];
+  __shared__ __attribute__((aligned(16))) int4 s_list[NLIST];
+  __shared__ uint32_t s_sc[MX ? 3 * BM * 4 : 1];  // [buffer][row][step]: the four block scales of a row's step
+  __shared__ __attribute__((aligned(16))) float s_ws[MX ? NRT : 1][MX ? BN : 4];  // weight row scales of a tile
   __shared__ int s_cum[MAXG + 1];
   __shared__ int s_cnt[MAXG];
   __shared__ int s_off[MAXG];
@@ -177,10 +190,10 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     const int n = rem / mc, m = ch * c + (rem - n * mc);
     return make_int4(g | (min(BM, cnt - m * BM) << 16), m * BM, n * NCOLS, s_off[g] + m * BM);
   };
-  for (int i = tid; i < min(ntl, LIST); i += THREADS) s_list[i] = find_tile(i);
+  for (int i = tid; i < min(ntl, NLIST); i += THREADS) s_list[i] = find_tile(i);
   __syncthreads();
   auto tile_of = [&](int i) {
-    const int4 v = (i < LIST) ? s_list[i] : find_tile(i);
+    const int4 v = (i < NLIST) ? s_list[i] : find_tile(i);
     const int gr = __builtin_amdgcn_readfirstlane(v.x);
     return TileInfo{gr & 0xFFFF, __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z), gr >> 16,
                     __builtin_amdgcn_readfirstlane(v.w)};
@@ -192,6 +205,7 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
   };
   const uint32_t lds0 = lds_addr(smem);
   const uint32_t rt0 = lds_addr(&s_rt[0][0]);
+  const uint32_t sc0 = lds_addr(s_sc), ws0 = lds_addr(&s_ws[0][0]);
   // Copy row_token[base .. base + 256) of tile t into s_rt[slot] (wave 0; clamped reads). A
   // tile's slice is copied one tile before the producer reaches it. The producer is two
   // steps ahead of the consumer, whose tile's slice the audit still reads: with one step per
@@ -205,6 +219,21 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
         dma4(a.row_token + idx, rt0 + (slot * BM + j * 64) * 4);
       }
     }
+    if constexpr (MX) {
+      // and the scales of the tile's weight rows (wave 1), by the same rules
+      const bool priv = t.g >= a.n_pub && a.w13_priv && a.w2_priv;
+      const int g = priv ? t.g - a.n_pub : (t.g < a.n_pub ? t.g : 0);
+      const float* ws = (GATED ? (priv ? a.w13_scale_priv : a.w13_scale_pub) : (priv ? a.w2_scale_priv : a.w2_scale_pub)) +
+                        (size_t)g * (GATED ? 2 * a.I : H);
+      if (wave == 1) {
+#pragma unroll
+        for (int j = 0; j < BN / 64; ++j) {
+          const int c = t.n0 + (j & 1) * 64 + lane;
+          const int row = GATED ? (j >> 1) * a.I + min(c, a.I - 1) : min(c + (j >> 1) * 128, H - 1);
+          dma4(ws + row, ws0 + (slot * BN + j * 64) * 4);
+        }
+      }
+    }
   };
 
   // Producer: source offsets (bytes) of this lane's copies for the tile whose steps are being
@@ -215,7 +244,11 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
   const uint32_t cchunk = (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
   // weight row held by LDS row r of a half: within 32 rows, row 16 nb + j holds 8 (j / 4) + 4 nb + j % 4
   auto bperm = [](int r) { return (r & ~31) + 8 * ((r >> 2) & 3) + 4 * ((r >> 4) & 1) + (r & 3); };
-  uint32_t offA[4], offB[4];  // [half * 2 + copy]
+  // [half * 2 + copy]; MX weights: copy 1 lies 16 rows after copy 0 and half 1 the same distance from
+  // half 0 in every lane, so one offset does (the others cost registers that the scales need)
+  uint32_t offA[4], offB[MX ? 1 : 4];
+  uint32_t stepB = 0, halfB = 0;
+  uint32_t offS[2];           // MX: scales of row wave * 16 + lane / 4 of a half
   const unsigned char* baseA = nullptr;
   const unsigned char* baseB = nullptr;
   int p_full = 0;  // the producer's tile has more than 128 rows
@@ -228,10 +261,10 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     if (shared) {
       w = (const unsigned char*)(GATED ? a.w13_sh : a.w2_sh);
     } else if (!priv) {
-      w = (const unsigned char*)(GATED ? a.w13_pub : a.w2_pub) + (size_t)t.g * (GATED ? 2 : 1) * I * H * 2;
+      w = (const unsigned char*)(GATED ? a.w13_pub : a.w2_pub) + (size_t)t.g * (GATED ? 2 : 1) * I * H * ESZ;
     } else {
       w = (const unsigned char*)(GATED ? a.w13_priv : a.w2_priv);
-      if (w) w += (size_t)(t.g - a.n_pub) * (GATED ? 2 : 1) * I * H * 2;
+      if (w) w += (size_t)(t.g - a.n_pub) * (GATED ? 2 : 1) * I * H * ESZ;
     }
     // private rows without private weights: the copies read public rows, nothing is computed
     if (w == nullptr || (priv && (a.w13_priv == nullptr || a.w2_priv == nullptr)))
@@ -248,31 +281,60 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
       const int rr = min(r, t.rows - 1);  // rows past the valid count reload a valid row
       uint32_t row = (uint32_t)(t.base + rr);
       if (GATED ? (!shared && !a.x_perm) : GATHER_A) row = (uint32_t)s_rt[slot][rr];
-      offA[i] = row * (uint32_t)(K * 2) + cchunk;
+      offA[i] = row * (uint32_t)(K * ESZ) + cchunk;
       const int c = bperm(crow + (i & 1) * 8);
       int wrow;
       if (GATED)
         wrow = (i >> 1) * I + min(t.n0 + c, I - 1);
       else
         wrow = min(t.n0 + (i >> 1) * 128 + c, H - 1);
-      offB[i] = (uint32_t)wrow * (uint32_t)(K * 2) + cchunk;
+      if (!MX || i == 0) offB[MX ? 0 : i] = (uint32_t)wrow * (uint32_t)(K * ESZ) + cchunk;
     }
-    return K / BK;
+    if constexpr (MX) {
+      // (I and H are multiples of 128: a half is inside the width, or past it as a whole and then
+      // copies half 0 again)
+      stepB = 16 * (uint32_t)K;
+      halfB = GATED ? (uint32_t)I * (uint32_t)K : t.n0 + 128 < H ? 128 * (uint32_t)K : 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int rr = min(h * 128 + wave * 16 + (lane >> 2), t.rows - 1);
+        const uint32_t row = GATED ? (uint32_t)s_rt[slot][rr] : (uint32_t)(t.base + rr);
+        offS[h] = row * (uint32_t)(K / 32);
+      }
+    }
+    return K * ESZ / BKB;
   };
   // Copies of half h of A or B of the producer's current step (pk) into buffer `buf`.
   int pi = 0, pk = 0, pnk = 0;
   auto copyA1 = [&](auto h, auto i, uint32_t buf) {
     const uint32_t dst = lds0 + buf + h.value * HALF + wave * 2048;
-    dma16s<i.value * 1024, false>(offA[h.value * 2 + i.value], baseA + pk * (BK * 2), dst);
+    dma16s<i.value * 1024, false>(offA[h.value * 2 + i.value], baseA + pk * BKB, dst);
   };
   auto copyB1 = [&](auto h, auto i, uint32_t buf) {
     const uint32_t dst = lds0 + buf + (2 + h.value) * HALF + wave * 2048;
-    dma16s<i.value * 1024, false>(offB[h.value * 2 + i.value], baseB + pk * (BK * 2), dst);
+    if constexpr (MX)
+      dma16s<i.value * 1024, false>(offB[0], baseB + pk * BKB + (i.value ? stepB : 0) + (h.value ? halfB : 0), dst);
+    else
+      dma16s<i.value * 1024, false>(offB[h.value * 2 + i.value], baseB + pk * BKB, dst);
   };
   auto copyA = [&](auto h, uint32_t buf) { copyA1(h, ic<0>, buf); copyA1(h, ic<1>, buf); };
   auto copyB = [&](auto h, uint32_t buf) { copyB1(h, ic<0>, buf); copyB1(h, ic<1>, buf); };
   constexpr std::integral_constant<int, 0> h0{};
   constexpr std::integral_constant<int, 1> h1{};
+  // MX: the block scales of a tile's rows come four steps at a time (lane l: row l / 4 of the wave's 16,
+  // step l % 4), one request per row and four steps: a step's four bytes of every row, a request each,
+  // made half as many requests again as the operands (16384-token layer of the same shape: steps took
+  // 1.4 times as long). They are issued ahead of the first of those steps. A quad has one step at
+  // least and the producer is two steps ahead: three buffers.
+  int pq = 0;
+  auto copy_scales = [&]() {
+    const uint8_t* sc = GATED ? a.x_scale : a.h_scale;
+    const uint32_t o = 4 * (uint32_t)min(pk + (lane & 3), pnk - 1);
+    const uint32_t dst = sc0 + pq * (BM * 16) + wave * 256;
+    dma4s(offS[0] + o, sc, dst);
+    dma4s(offS[1] + o, sc, dst + 128 * 16);
+    pq = pq == 2 ? 0 : pq + 1;
+  };
   // Move to the next step to issue; its kind: 0 none left, 1 without A1, 2 with A1.
   auto next_step = [&]() {
     if (pi >= ntl) return 0;
@@ -283,6 +345,8 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
       pnk = setup(tile_of(pi), pi % NRT);
       if (pi + 1 < ntl) issue_rt(tile_of(pi + 1), (pi + 1) % NRT);
     }
+    if constexpr (MX)
+      if ((pk & 3) == 0) copy_scales();
     return 1 + p_full;
   };
   // prologue: gather indices of tiles 0 and 1, then steps 0 and 1
@@ -320,23 +384,31 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
   // Fragment addresses: row (lane & 15) of a 16-row block, K chunk 4 sub + lane / 16.
   const uint32_t lane_off = (uint32_t)((lane & 15) * 128 + (((lane >> 4) ^ (lane & 7)) << 4));
   uint32_t cbuf = 0;  // the consumer's buffer (0 or STEP)
-  bf16x8 fa[4][2], fb0[2][2], fb1[2][2];
+  // A fragment holds two 16-byte halves: the bf16 sub-steps of 32, or the MX halves of its lane
+  using Frag = std::conditional_t<MX, i32x8, bf16x16>;
+  Frag fa[4], fb0[2], fb1[2];
+  auto frag = [&](uint32_t p0, uint32_t p1) {
+    const u32x4 lo = *(const u32x4*)(smem + p0), hi = *(const u32x4*)(smem + p1);
+    return __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  const uint32_t lane_sc = (uint32_t)((lane & 15) * 16 + (lane >> 4));
+  uint32_t csc = 0, cq = 0;  // the consumer's step within s_sc, and its buffer
+  int sa[4];  // MX: block scales of the A fragments (lane: row lane % 16, values 32 (lane / 16) .. + 31)
   // Wave wm's 16-row blocks of an A half are blocks 2 mb + wm, so a partly filled half loads
   // both row groups alike.
   auto readA = [&](auto h) {
     const uint32_t p0 = lane_off + cbuf + wm * 2048, p1 = p0 ^ 64;
 #pragma unroll
     for (int mb = 0; mb < 4; ++mb) {
-      fa[mb][0] = as_bf16x8(*(const u32x4*)(smem + p0 + h.value * HALF + mb * 4096));
-      fa[mb][1] = as_bf16x8(*(const u32x4*)(smem + p1 + h.value * HALF + mb * 4096));
+      fa[mb] = frag(p0 + h.value * HALF + mb * 4096, p1 + h.value * HALF + mb * 4096);
+      if constexpr (MX) sa[mb] = ((const uint8_t*)s_sc)[lane_sc + csc + h.value * 2048 + (2 * mb + wm) * 256];
     }
   };
-  auto readB = [&](auto h, bf16x8 (&fb)[2][2]) {
+  auto readB = [&](auto h, Frag (&fb)[2]) {
     const uint32_t p0 = lane_off + cbuf + wn * 4096, p1 = p0 ^ 64;
 #pragma unroll
     for (int nb = 0; nb < 2; ++nb) {
-      fb[nb][0] = as_bf16x8(*(const u32x4*)(smem + p0 + (2 + h.value) * HALF + nb * 2048));
-      fb[nb][1] = as_bf16x8(*(const u32x4*)(smem + p1 + (2 + h.value) * HALF + nb * 2048));
+      fb[nb] = frag(p0 + (2 + h.value) * HALF + nb * 2048, p1 + (2 + h.value) * HALF + nb * 2048);
     }
   };
   // Output stores share the counter of the copies. They follow the copies of the last step of
@@ -387,40 +459,64 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     barrier_raw();
     __builtin_amdgcn_sched_barrier(0);
   };
+  // bf16: sub-step `sub` of a fragment; MX: the whole of it (K values 16 (lane / 16) .. + 15 and 64 + the
+  // same) with its block scales
+  auto mfma = [&](auto sub, const Frag& b, int mb, f32x4 c) {
+    if constexpr (MX) {
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, fa[mb], c, 0, 0, 0, 0x7F7F7F7F, 0, sa[mb]);
+    } else {
+      constexpr int o = 8 * decltype(sub)::value;
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          __builtin_shufflevector(b, b, o, o + 1, o + 2, o + 3, o + 4, o + 5, o + 6, o + 7),
+          __builtin_shufflevector(fa[mb], fa[mb], o, o + 1, o + 2, o + 3, o + 4, o + 5, o + 6, o + 7), c, 0, 0, 0);
+    }
+  };
   // the first MB row blocks of a quadrant
-  auto mul = [&](auto blocks, f32x4 (&acc)[4][2], const bf16x8 (&fb)[2][2]) {
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub)
+  constexpr int SUBS = MX ? 1 : 2;
+  // MX: the products of a phase stay in it (without this the compiler moves them past the branches
+  // of later copies, which keeps the fragments of two phases alive and spills accumulators)
+  auto pin = [&](auto blocks, f32x4 (&acc)[4][2]) {
+    if constexpr (MX) {
 #pragma unroll
       for (int mb = 0; mb < decltype(blocks)::value; ++mb)
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-          acc[mb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[nb][sub], fa[mb][sub], acc[mb][nb], 0, 0, 0);
+        for (int nb = 0; nb < 2; ++nb) asm volatile("" : "+v"(acc[mb][nb]));
+    }
+  };
+  auto mul = [&](auto blocks, f32x4 (&acc)[4][2], const Frag (&fb)[2]) {
+    Unroll<0, SUBS>::run([&](auto sub) {
+#pragma unroll
+      for (int mb = 0; mb < decltype(blocks)::value; ++mb)
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) acc[mb][nb] = mfma(sub, fb[nb], mb, acc[mb][nb]);
+    });
+    pin(blocks, acc);
   };
   // the same with copies issued between the MFMAs
-  auto mulc_mb = [&](auto blocks, f32x4 (&acc)[4][2], const bf16x8 (&fb)[2][2], auto&& copy) {
+  auto mulc_mb = [&](auto blocks, f32x4 (&acc)[4][2], const Frag (&fb)[2], auto&& copy) {
     constexpr int MB = decltype(blocks)::value;
-#pragma unroll
-    for (int sub = 0; sub < 2; ++sub) {
+    // the row blocks after which the two copies go (bf16: in the first and in the second sub-step)
+    constexpr int C0 = MX ? (MB - 1) / 4 : (MB - 1) / 2, C1 = MX ? (MB - 1) * 3 / 4 : (MB - 1) / 2;
+    Unroll<0, SUBS>::run([&](auto sub) {
 #pragma unroll
       for (int mb = 0; mb < MB; ++mb) {
 #pragma unroll
-        for (int nb = 0; nb < 2; ++nb)
-          acc[mb][nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[nb][sub], fa[mb][sub], acc[mb][nb], 0, 0, 0);
-        if (sub == 0 && mb == (MB - 1) / 2) {
+        for (int nb = 0; nb < 2; ++nb) acc[mb][nb] = mfma(sub, fb[nb], mb, acc[mb][nb]);
+        if (sub.value == 0 && mb == C0) {
           __builtin_amdgcn_sched_barrier(0);
           copy(ic<0>);
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (sub == 1 && mb == (MB - 1) / 2) {
+        if (sub.value == SUBS - 1 && mb == C1) {
           __builtin_amdgcn_sched_barrier(0);
           copy(ic<1>);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-    }
+    });
+    pin(blocks, acc);
   };
-  auto mulc = [&](f32x4 (&acc)[4][2], const bf16x8 (&fb)[2][2], auto&& copy) { mulc_mb(ic<4>, acc, fb, copy); };
+  auto mulc = [&](f32x4 (&acc)[4][2], const Frag (&fb)[2], auto&& copy) { mulc_mb(ic<4>, acc, fb, copy); };
   auto end_step = [&]() {
     cbuf ^= STEP;
     kind1 = kind2;
@@ -429,7 +525,7 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
 
   // K loop and output of one tile; halves: A halves with valid rows (0: nothing is computed);
   // blocks: row blocks per wave of the last of them that may hold valid rows.
-  auto tile_body = [&](auto halves, auto blocks, const TileInfo& ct, int cnk, void* out, int ld, int width) {
+  auto tile_body = [&](auto halves, auto blocks, const TileInfo& ct, int slot, int cnk, void* out, int ld, int width) {
     constexpr int AH = decltype(halves)::value, BLOCKS = decltype(blocks)::value;
     f32x4 acc[AH > 0 ? AH : 1][2][4][2];  // [A half][B half][row block][column block]
 #pragma unroll
@@ -447,7 +543,49 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     // reading half of a later phase, while the other row group multiplies; storing the whole
     // tile after its last step instead held both row groups up in turn.
     const bool save = SAVE && ct.g < E;
+    // MX: the same lanes and columns, times the weight rows' scales; h leaves as bytes and one scale per
+    // 32 columns, which the lanes l, l + 16, l + 32 and l + 48 hold (two lane exchanges)
+    auto store_mx = [&](auto ih, auto jh, auto mb0, auto mb1) {
+      constexpr int i = decltype(ih)::value, j = decltype(jh)::value;
+      int ln = lane, row0 = ct.base;
+      asm volatile("" : "+v"(ln));
+      asm volatile("" : "+s"(row0));
+      const int cc = wn * 32 + (ln >> 4) * 8, c = ct.n0 + j * 128 + cc;
+      const float* ws = s_ws[slot] + j * 128 + cc;
+#pragma unroll
+      for (int mb = decltype(mb0)::value; mb < decltype(mb1)::value; ++mb) {
+        const int r = i * 128 + (2 * mb + wm) * 16 + (ln & 15);
+        const f32x4 v0 = acc[i][j][mb][0] * *(const f32x4*)ws, v1 = acc[i][j][mb][1] * *(const f32x4*)(ws + 4);
+        if constexpr (GATED) {
+          const f32x4 u0 = acc[i][1][mb][0] * *(const f32x4*)(ws + 128), u1 = acc[i][1][mb][1] * *(const f32x4*)(ws + 132);
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = mx_silu(v0[e]) * u0[e];
+            v[4 + e] = mx_silu(v1[e]) * u1[e];
+          }
+          // the block's largest magnitude: the lanes l, l ^ 16, l ^ 32 and l ^ 48 hold its 32 columns
+          const float amax = mx_max_rows(mx_amax8(v));
+          typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+          uint32_t q0, q1;
+          const int e = mx_pack8(v, amax, q0, q1);
+          const __amdgpu_buffer_rsrc_t ro = buffer((const uint8_t*)out + (size_t)row0 * ld, (uint32_t)(ct.rows * ld));
+          const __amdgpu_buffer_rsrc_t rs = buffer(a.h_scale + (size_t)row0 * (ld / 32), (uint32_t)(ct.rows * (ld / 32)));
+          __builtin_amdgcn_raw_buffer_store_b64(u32x2{q0, q1}, ro, c < width ? (uint32_t)(r * ld + c) : NO_STORE, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b8((uint8_t)(e + 127), rs,
+                                               c < width && ln < 16 ? (uint32_t)(r * (ld / 32) + (c >> 5)) : NO_STORE, 0, 0);
+        } else {
+          const __amdgpu_buffer_rsrc_t ro = buffer((const uint16_t*)out + (size_t)row0 * ld, (uint32_t)(ct.rows * ld * 2));
+          const u32x4 o{cvt_pk_bf16(v0[0], v0[1]), cvt_pk_bf16(v0[2], v0[3]), cvt_pk_bf16(v1[0], v1[1]), cvt_pk_bf16(v1[2], v1[3])};
+          __builtin_amdgcn_raw_buffer_store_b128(o, ro, c < width ? (uint32_t)((r * ld + c) * 2) : NO_STORE, 0, 0);
+        }
+      }
+    };
     auto store = [&](auto ih, auto jh, auto mb0, auto mb1) {
+      if constexpr (MX) {
+        store_mx(ih, jh, mb0, mb1);
+        return;
+      }
       constexpr int i = decltype(ih)::value, j = decltype(jh)::value;
       // opaque copies, so that the addresses are formed here and not kept in registers
       // through the K loop
@@ -488,6 +626,7 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     };
     for (int kc = 0; kc < cnk; ++kc) {
       const bool last = kc == cnk - 1;
+      if constexpr (MX) csc = cq * (BM * 16) + (kc & 3) * 4;
       if constexpr (AH == 2) {
         readA(h0);
         readB(h0, fb0);
@@ -582,6 +721,8 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
           if (last) store(h0, ic<GATED ? 0 : 1>, ic<0>, ic<4>);
       }
       end_step();
+      if constexpr (MX)
+        if ((kc & 3) == 3 || last) cq = cq == 2 ? 0 : cq + 1;
     }
     fst = AH;
     // (a shared tile of the saving variant stores no projections: no allowance)
@@ -594,22 +735,23 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     const bool c_shared = ct.g >= E;
     const bool c_priv = !c_shared && ct.g >= a.n_pub;
     const int cI = c_shared ? a.Is : a.I;
-    const int cnk = (GATED ? H : cI) / BK;
+    const int cnk = (GATED ? H : cI) * ESZ / BKB;
+    const int slot = ci % NRT;
     const bool c_valid = !(c_priv && (a.w13_priv == nullptr || a.w2_priv == nullptr));
     const int width = GATED ? cI : H;
     void* out = GATED ? (c_shared ? a.h_sh : a.h) : (c_shared ? a.y_shared : a.y_perm);
     if (!c_valid)
-      tile_body(ic<0>, ic<0>, ct, cnk, out, width, width);
+      tile_body(ic<0>, ic<0>, ct, slot, cnk, out, width, width);
     else if (ct.rows <= 64)
-      tile_body(ic<1>, ic<2>, ct, cnk, out, width, width);
+      tile_body(ic<1>, ic<2>, ct, slot, cnk, out, width, width);
     else if (ct.rows <= 128)
-      tile_body(ic<1>, ic<4>, ct, cnk, out, width, width);
+      tile_body(ic<1>, ic<4>, ct, slot, cnk, out, width, width);
     else if (ct.rows <= 160)
-      tile_body(ic<2>, ic<1>, ct, cnk, out, width, width);
+      tile_body(ic<2>, ic<1>, ct, slot, cnk, out, width, width);
     else if (ct.rows <= 192)
-      tile_body(ic<2>, ic<2>, ct, cnk, out, width, width);
+      tile_body(ic<2>, ic<2>, ct, slot, cnk, out, width, width);
     else
-      tile_body(ic<2>, ic<4>, ct, cnk, out, width, width);
+      tile_body(ic<2>, ic<4>, ct, slot, cnk, out, width, width);
     if (!c_valid && !GATED) {
       // private rows without private weights: not executed, not audited, y zeroed
       if (tid == 0 && a.dev_status) atomicOr(a.dev_status, PMPE_DEV_PRIV_WEIGHTS_MISSING);
@@ -641,7 +783,7 @@ template <int MODE>
 hipError_t launch(const FfnArgs& a, hipStream_t s) {
   // Persistent grid: one block per CU (a multiple of the 8 XCDs), never more than the tiles
   // there can be.
-  constexpr bool GATED = MODE == G1 || MODE == G1_SAVE;
+  constexpr bool GATED = MODE == G1 || MODE == G1_SAVE || MODE == MX_UP;
   constexpr int NCOLS = GATED ? BN / 2 : BN;
   const int E = a.n_pub + a.n_priv;
   const int64_t w = GATED ? a.I : a.H;
@@ -664,6 +806,11 @@ hipError_t launch_gemm256_up(const FfnArgs& a, hipStream_t s) {
 hipError_t launch_gemm256_down(const FfnArgs& a, hipStream_t s) { return launch<G2>(a, s); }
 hipError_t launch_gemm256_plain(const FfnArgs& a, hipStream_t s) {
   return a.gather_a ? launch<GATHER>(a, s) : launch<PLAIN>(a, s);
+}
+
+hipError_t launch_gemm256_mx(const FfnArgs& a, hipStream_t s) {
+  const hipError_t e = launch<MX_UP>(a, s);
+  return e != hipSuccess ? e : launch<MX_DOWN>(a, s);
 }
 
 }  // namespace pmpe

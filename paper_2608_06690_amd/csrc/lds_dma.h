@@ -66,6 +66,18 @@ __device__ __forceinline__ void dma4(const void* src, uint32_t lds_base_) {
       : "memory", "m0");
 }
 
+// The same addressed like dma16s: wave-uniform base plus a 32-bit byte offset per lane.
+__device__ __forceinline__ void dma4s(uint32_t byte_off, const void* base_, uint32_t lds_base_) {
+  const void* base = uniform_ptr(base_);
+  const uint32_t lds_base = __builtin_amdgcn_readfirstlane(lds_base_);
+  asm volatile(
+      "s_mov_b32 m0, %2\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dword %0, %1 offset:0" ::"v"(byte_off),
+      "s"(base), "s"(lds_base)
+      : "memory", "m0");
+}
+
 // f(integral_constant<I>), ..., f(integral_constant<N-1>): copies whose LDS offset is an
 // immediate (IMM of dma16s) are issued from a compile-time index.
 template <int I, int N>

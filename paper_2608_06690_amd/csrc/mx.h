@@ -23,17 +23,33 @@ __device__ __forceinline__ uint32_t mx_pack4(float a, float b, float c, float d)
   return (uint32_t)v;
 }
 
-// Largest magnitude of 8 values of a block; +inf if one is not finite.
+// Largest magnitude of 8 values of a block; not below inf if one is not finite (the order of the bit
+// patterns is that of the magnitudes, with inf and then NaN above them).
 __device__ __forceinline__ float mx_amax8(const float (&v)[8]) {
-  float m = 0.f;
-  bool fine = true;
+  uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    m = fmaxf(m, fabsf(v[i]));
-    fine = fine && fabsf(v[i]) < INFINITY;
-  }
-  return fine ? m : INFINITY;
+  for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+  return __uint_as_float(m);
 }
+// The largest of such values over lanes l, l ^ a and l ^ b (that of all four, a and b applied in turn).
+template <int A, int B>
+__device__ __forceinline__ float mx_max_lanes(float amax) {
+  uint32_t m = __float_as_uint(amax);
+  m = max(m, (uint32_t)__shfl_xor((int)m, A, 64));
+  m = max(m, (uint32_t)__shfl_xor((int)m, B, 64));
+  return __uint_as_float(m);
+}
+// Of lanes l, l ^ 16, l ^ 32 and l ^ 48 (rows of 16 lanes swapped in the vector unit).
+__device__ __forceinline__ float mx_max_rows(float amax) {
+  uint32_t m = __float_as_uint(amax);
+  auto s = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+  m = max(s[0], s[1]);
+  s = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  return __uint_as_float(max(s[0], s[1]));
+}
+// silu for a result that is rounded to e4m3 next: the hardware reciprocal (1 ulp) in place of the division
+// that the bf16 paths correct to the last bit.
+__device__ __forceinline__ float mx_silu(float g) { return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)); }
 // The block's 8 values as bytes, with amax of the whole block of 32; returns the scale's exponent.
 // A block with a value that is not finite holds NaN only.
 __device__ __forceinline__ int mx_pack8(const float (&v)[8], float amax, uint32_t& q0, uint32_t& q1) {

@@ -280,17 +280,13 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
         if constexpr (GATED) {
           const f32x4 t0 = *(const f32x4*)(ws + BN / 2 + c), t1 = *(const f32x4*)(ws + BN / 2 + c + 4);
           const f32x4 u0 = acc[mb][NB / 2 + 2 * p] * t0, u1 = acc[mb][NB / 2 + 2 * p + 1] * t1;
-          const float g[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
           float h[8];
-          silu_n<8>(g, h);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            h[e] *= u0[e];
-            h[4 + e] *= u1[e];
+            h[e] = mx_silu(v0[e]) * u0[e];
+            h[4 + e] = mx_silu(v1[e]) * u1[e];
           }
-          float amax = mx_amax8(h);
-          amax = fmaxf(amax, __shfl_xor(amax, 16, 64));
-          amax = fmaxf(amax, __shfl_xor(amax, 32, 64));
+          const float amax = mx_max_rows(mx_amax8(h));
           if (r < ct.rows && col < width) {
             typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
             uint32_t q0, q1;
@@ -365,6 +361,16 @@ hipError_t launch_expert_ffn_mx(const MxFfnArgs& a, hipStream_t s) {
   if (rows < 48) {
     e = launch<MxSmall, true>(a, s);
     return e != hipSuccess ? e : launch<MxSmall, false>(a, s);
+  }
+  if (a.H >= 256 && a.I >= 256) {
+    FfnArgs f{};
+    f.T = a.T; f.H = a.H; f.I = a.I; f.n_pub = a.n_pub; f.n_priv = a.n_priv; f.k = a.k;
+    f.x = a.xq; f.x_scale = a.xs; f.count = a.count; f.offset = a.offset; f.row_token = a.row_token;
+    f.w13_pub = a.w13_pub; f.w2_pub = a.w2_pub; f.w13_priv = a.w13_priv; f.w2_priv = a.w2_priv;
+    f.w13_scale_pub = a.w13s_pub; f.w2_scale_pub = a.w2s_pub; f.w13_scale_priv = a.w13s_priv; f.w2_scale_priv = a.w2s_priv;
+    f.y_perm = a.y_perm; f.audit_rows = a.audit_rows; f.audit_calls = a.audit_calls; f.dev_status = a.dev_status;
+    f.h = a.hq; f.h_scale = a.hs;
+    return launch_gemm256_mx(f, s);
   }
   e = launch<MxMid, true>(a, s);
   return e != hipSuccess ? e : launch<MxMid, false>(a, s);

@@ -133,9 +133,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_kernel(NormArgs
     for (int j = 0; j < 8; ++j) w[j] *= r[v][j] * rstd;
     if (a.out) store8<BF16>((char*)a.out + row * el, i, H, w);
     if (a.out_q) {  // (H is a multiple of 32: the four lanes of a block are all inside or all past it)
-      float amax = mx_amax8(w);
-      amax = fmaxf(amax, __shfl_xor(amax, 1, 64));
-      amax = fmaxf(amax, __shfl_xor(amax, 2, 64));
+      const float amax = mx_max_lanes<1, 2>(mx_amax8(w));
       if (i < H) {
         typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
         uint32_t q0, q1;

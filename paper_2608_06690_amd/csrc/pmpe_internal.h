@@ -194,6 +194,9 @@ struct FfnArgs {
   const float* w2_scale_pub = nullptr;
   const float* w13_scale_priv = nullptr;
   const float* w2_scale_priv = nullptr;
+  // 8-bit activations (launch_gemm256_mx): block scales of x [T, H / 32] and h [T*k, I / 32]
+  const uint8_t* x_scale = nullptr;
+  uint8_t* h_scale = nullptr;
   int gather_a = 0;  // plain grouped product (launch_grouped_nt_gemm): A row r is x[row_token[r]]
 };
 hipError_t launch_expert_ffn(const FfnArgs& a, hipStream_t s);
@@ -204,6 +207,7 @@ hipError_t launch_expert_ffn_fp8(const FfnArgs& a, hipStream_t s);
 hipError_t launch_gemm256_up(const FfnArgs& a, hipStream_t s);
 hipError_t launch_gemm256_down(const FfnArgs& a, hipStream_t s);
 hipError_t launch_gemm256_plain(const FfnArgs& a, hipStream_t s);
+hipError_t launch_gemm256_mx(const FfnArgs& a, hipStream_t s);  // both products on 8-bit operands, H >= 256
 
 struct LoraArgs {
   int T, H, I, k, n_pub, n_priv, rank, gate;
@@ -364,6 +368,7 @@ struct MxFfnArgs {
   int T, H, I, n_pub, n_priv, k;
   const uint8_t* xq;  // [T, H] e4m3, and their scales [T, H / 32] e8m0
   const uint8_t* xs;
+  const int32_t* count;
   const int32_t* offset;
   const int32_t* row_token;
   const void* w13_pub;
