@@ -34,20 +34,26 @@ namespace {
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 constexpr int MAXE = 2 * PMPE_MAX_POOL;
 
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_, bool NT_>
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_, bool NT_, int SPC_>
 struct MxCfg {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
   static constexpr bool NT = NT_;  // weights are read once: keep them from evicting the activations
+  // Steps whose scale bytes one copy brings: 64 / SPC rows of a wave. A row's are neighbours in memory, so
+  // four steps cost a request per row where four copies cost four.
+  static constexpr int SPC = SPC_;
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
-  static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, SC_BYTES = BM * 4;
-  static constexpr int STAGE = A_BYTES + B_BYTES + SC_BYTES;
-  static constexpr int A_DMA = BM / 8 / WAVES, B_DMA = BN / 8 / WAVES, NDMA = A_DMA + B_DMA + 1;
+  static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, SC_BYTES = BM * 4 * SPC;
+  static constexpr int STAGE = A_BYTES + B_BYTES;
+  static constexpr int A_DMA = BM / 8 / WAVES, B_DMA = BN / 8 / WAVES, NDMA = A_DMA + B_DMA;
+  static constexpr int SC_WAVES = BM * SPC / 64;  // waves that copy scales
   static constexpr int MB = BM / WM / 16;  // 16-row blocks of a wave: blocks j * WM + wm
   // gather slices: a tile's is copied two tiles before its first step is issued (a tile may have one
   // step), and the audit reads it when the tile ends; scale slices: one tile before their use
   static constexpr int NRT = STAGES + 2, NWS = STAGES;
-  static constexpr int LDS = STAGES * STAGE + 256 + NRT * BM * 4 + NWS * BN * 4 + (MAXE + 1) * 8;
+  // a copy's steps are one at least and the producer is STAGES - 1 steps ahead: STAGES buffers
+  static constexpr int LDS = STAGES * (STAGE + SC_BYTES) + NRT * BM * 4 + NWS * BN * 4 + (MAXE + 1) * 8;
   static_assert(A_DMA * 8 * WAVES == BM && B_DMA * 8 * WAVES == BN, "copy split");
+  static_assert(SC_WAVES <= WAVES && SC_WAVES * 64 == BM * SPC, "scale copies");
   static_assert(BM <= 64 * WAVES && BN <= 64 * WAVES, "one slice copy per wave");
 };
 
@@ -63,7 +69,8 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
   constexpr int NQ = WC / 32;                 // its 32-column groups
   constexpr int NB = (GATED ? 2 : 1) * WC / 16;
   static_assert(WC % 32 == 0, "a wave holds whole 32-column groups");
-  __shared__ __attribute__((aligned(16))) unsigned char smem[S * C::STAGE + 256];
+  __shared__ __attribute__((aligned(16))) unsigned char smem[S * C::STAGE];
+  __shared__ __attribute__((aligned(16))) uint8_t s_sc[S][C::SC_BYTES];  // [buffer][row][step]: four bytes
   __shared__ __attribute__((aligned(16))) int s_rt[NRT][BM];
   __shared__ __attribute__((aligned(16))) float s_ws[NWS][BN];
   __shared__ int s_cum[MAXE + 1];
@@ -122,7 +129,7 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
   auto is_private = [&](const MxTile& t) { return t.g >= a.n_pub; };
   auto has_weights = [&](const MxTile& t) { return !(is_private(t) && (a.w13_priv == nullptr || a.w2_priv == nullptr)); };
 
-  const uint32_t lds0 = lds_addr(smem), dummy = lds0 + S * C::STAGE;
+  const uint32_t lds0 = lds_addr(smem), sc0 = lds_addr(&s_sc[0][0]);
   const uint32_t rt0 = lds_addr(&s_rt[0][0]), ws0 = lds_addr(&s_ws[0][0]);
   // row_token of tile i's rows (GEMM1 gathers by it, GEMM2's audit reads it), clamped into the array
   auto issue_rt = [&](int i) {
@@ -152,7 +159,7 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
   auto bperm = [](int r) { return (r & ~31) + 8 * ((r >> 2) & 3) + 4 * ((r >> 4) & 1) + (r & 3); };
   uint32_t offA[C::A_DMA], offB[C::B_DMA];
   const unsigned char* baseB = nullptr;
-  const unsigned char* srcS = nullptr;  // this lane's scale bytes
+  uint32_t offS = 0;  // this lane's scales: row wave * 64 / SPC + lane / SPC
   auto setup = [&](const MxTile& t, int i) {
     const size_t per = (size_t)(GATED ? 2 : 1) * I * H;
     const unsigned char* w = (const unsigned char*)(GATED ? a.w13_pub : a.w2_pub);
@@ -171,7 +178,7 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
 #pragma unroll
     for (int j = 0; j < C::B_DMA; ++j)
       offB[j] = (uint32_t)weight_row(t, bperm((wave * C::B_DMA + j) * 8 + crow)) * (uint32_t)K + cchunk;
-    srcS = (GATED ? a.xs : a.hs) + (size_t)row_of(min(wave * 64 + lane, BM - 1)) * (K / 32);
+    offS = row_of(min((wave * 64 + lane) / C::SPC, BM - 1)) * (uint32_t)(K / 32);
     return K / 128;
   };
   const unsigned char* baseA = (const unsigned char*)(GATED ? a.xq : a.hq);
@@ -181,12 +188,16 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
     const unsigned char *ba = baseA + step * 128, *bb = baseB + step * 128;
     Unroll<0, C::A_DMA>::run([&](auto j) { dma16s<j.value * 1024, false>(offA[j.value], ba, wa); });
     Unroll<0, C::B_DMA>::run([&](auto j) { dma16s<j.value * 1024, C::NT>(offB[j.value], bb, wb); });
-    // every wave issues one copy of scales, so that the waits count alike (waves past the rows
-    // copy into an unused place)
-    dma4(srcS + step * 4, wave < BM / 64 ? st + C::A_BYTES + C::B_BYTES + wave * 256 : dummy);
   };
 
-  int pi = 0, pk = 0, pnk = 0, issued = 0;
+  int pi = 0, pk = 0, pnk = 0, issued = 0, pq = 0;
+  // The next SPC steps' scales, ahead of the first of them (the waits count the operands' copies only:
+  // one more in flight makes them wait for one more).
+  auto issue_scales = [&]() {
+    if (wave < C::SC_WAVES)
+      dma4s(offS + 4 * (uint32_t)min(pk + lane % C::SPC, pnk - 1), GATED ? a.xs : a.hs, sc0 + pq * C::SC_BYTES + wave * 256);
+    pq = pq == S - 1 ? 0 : pq + 1;
+  };
   issue_rt(0);
   issue_rt(1);
   wait_vmcnt<0>();
@@ -208,6 +219,7 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
       issue_ws(t, pi);
       pnk = setup(t, pi);
     }
+    if (pk % C::SPC == 0) issue_scales();
     issue(slot, pk);
     ++pk;
     ++issued;
@@ -221,7 +233,7 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
     const u32x4 lo = *(const u32x4*)(smem + p), hi = *(const u32x4*)(smem + (p ^ 64));
     return i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
   };
-  int gs = 0;
+  int gs = 0, cq = 0;
   auto tile_body = [&](auto mbl, const MxTile& ct, int ci, int live) {
     constexpr int MBL = decltype(mbl)::value;
     f32x4 acc[MBL][NB];
@@ -247,7 +259,7 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
         for (int mb = 0; mb < MBL; ++mb) {
           const uint32_t row0 = (uint32_t)(mb * C::WM + wm) * 16;
           fa[mb] = frag(st + row0 * 128 + lane_off);
-          sc[mb] = (int)(*(const uint32_t*)(smem + st + C::A_BYTES + C::B_BYTES + (row0 + r16) * 4) >> (8 * g4));
+          sc[mb] = s_sc[cq][(row0 + r16) * 4 * C::SPC + kc % C::SPC * 4 + g4];
         }
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
@@ -262,6 +274,7 @@ __global__ __launch_bounds__(C::THREADS) void mx_gemm_kernel(MxFfnArgs a) {
                                                                            0, sc[mb]);
         __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's reads of the slot are done
       }
+      if (kc % C::SPC == C::SPC - 1 || kc == nk - 1) cq = cq == S - 1 ? 0 : cq + 1;
     }
     if (!has_weights(ct)) return;
     // Output: lane l holds columns 8 (l / 16) .. + 7 of each 32-column group, row l % 16 of a block.
@@ -337,8 +350,8 @@ int cu_count() {
   return 256;
 }
 
-using MxSmall = MxCfg<64, 128, 2, 2, 3, true>;
-using MxMid = MxCfg<128, 256, 2, 4, 3, false>;
+using MxSmall = MxCfg<64, 128, 2, 2, 3, true, 1>;  // two blocks per CU
+using MxMid = MxCfg<128, 256, 2, 4, 3, false, 4>;
 
 template <class C, bool GATED>
 hipError_t launch(const MxFfnArgs& a, hipStream_t s) {
@@ -356,13 +369,21 @@ hipError_t launch(const MxFfnArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_expert_ffn_mx(const MxFfnArgs& a, hipStream_t s) {
-  const int64_t rows = (int64_t)a.T * a.k / (a.n_pub + a.n_priv);  // per expert, on average
+  // Rows per expert, on average, choose the tile; us of both products (160 experts of 2048 x 768 / 52 of
+  // 1664 x 640 / 80 of 2048 x 1408), all experts alike:
+  //   rows                 32            48            56            64            96            128           192           384
+  //   64 x 128     149  51 130   163  53 148   186  55 161   237  67 206   315  81 281   356  90 315   510 120 452   870 188 740
+  //   128 x 256    165  61 151   173  63 157   177  65 160   180  66 162   195  73 176   248  81 217   299  93 248   496 133 407
+  //   256 x 256    193  80 180   199  80 184   203  82 186   205  84 188   217  87 197   228  95 209   263 111 247   474 154 397
+  // The large kernel needs a few tiles per CU (the 52 experts give it one or two), and two K steps.
+  const int64_t E = a.n_pub + a.n_priv, rows = (int64_t)a.T * a.k / E;
   hipError_t e;
-  if (rows < 48) {
+  if (rows < 52) {
     e = launch<MxSmall, true>(a, s);
     return e != hipSuccess ? e : launch<MxSmall, false>(a, s);
   }
-  if (a.H >= 256 && a.I >= 256) {
+  const int64_t large_tiles = E * ((rows + 255) / 256) * (a.I / 128);
+  if (rows >= 120 && large_tiles >= 3 * cu_count() && a.H >= 256 && a.I >= 256) {
     FfnArgs f{};
     f.T = a.T; f.H = a.H; f.I = a.I; f.n_pub = a.n_pub; f.n_priv = a.n_priv; f.k = a.k;
     f.x = a.xq; f.x_scale = a.xs; f.count = a.count; f.offset = a.offset; f.row_token = a.row_token;

@@ -213,14 +213,25 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rmsnorm_bwd_kernel(Norm
   for (int v = 0; v < V; ++v) store8<false>(part, (v * W * 64 + l) * 8, H, dw[v]);
 }
 
-// dw[h] = sum over the parts, in order within each of the block's 16 slices, then the slices in order.
-__global__ __launch_bounds__(256) void rmsnorm_dw_kernel(const float* part, int parts, int H, float* dw) {
-  __shared__ float s[16][17];
-  const int c = threadIdx.x & 15, q = threadIdx.x >> 4, h = blockIdx.x * 16 + c;
+// dw[h] = sum over the parts: 16 slices of them, eight loads in flight each, in order; then the slices in
+// order. A block takes 64 columns (whole 256-byte lines of a part).
+__global__ __launch_bounds__(1024) void rmsnorm_dw_kernel(const float* part, int parts, int H, float* dw) {
+  __shared__ float s[16][64];
+  const int c = threadIdx.x & 63, q = threadIdx.x >> 6, h = blockIdx.x * 64 + c;
   const int per = (parts + 15) / 16, p0 = min(parts, q * per), p1 = min(parts, p0 + per);
   float v = 0.f;
-  if (h < H)
-    for (int p = p0; p < p1; ++p) v += part[(size_t)p * H + h];
+  if (h < H) {
+    const float* src = part + h;
+    int p = p0;
+    for (; p + 8 <= p1; p += 8) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = src[(size_t)(p + i) * H];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v += x[i];
+    }
+    for (; p < p1; ++p) v += src[(size_t)p * H];
+  }
   s[q][c] = v;
   __syncthreads();
   if (q == 0 && h < H) {
@@ -229,20 +240,16 @@ __global__ __launch_bounds__(256) void rmsnorm_dw_kernel(const float* part, int 
   }
 }
 
-// f.operator()<W, V>() for the smallest shape that holds a row of H values: one wave up to 2048 values
-// (or four, for batches whose waves would not fill the chip), four up to 8192, sixteen up to 16384.
+// f(W, V) for the smallest shape that holds a row of H values: W waves of V vectors of 8 per lane.
 template <class F>
-hipError_t by_row(int H, bool few, F&& f) {
+hipError_t by_row(int H, F&& f) {
   using std::integral_constant;
 #define PMPE_ROW(w, v) return f(integral_constant<int, w>{}, integral_constant<int, v>{})
-  if (!few) {
-    if (H <= 512) PMPE_ROW(1, 1);
-    if (H <= 1024) PMPE_ROW(1, 2);
-    if (H <= 2048) PMPE_ROW(1, 4);
-  }
+  if (H <= 512) PMPE_ROW(1, 1);
+  if (H <= 1024) PMPE_ROW(2, 1);
   if (H <= 2048) PMPE_ROW(4, 1);
-  if (H <= 4096) PMPE_ROW(4, 2);
-  if (H <= 8192) PMPE_ROW(4, 4);
+  if (H <= 4096) PMPE_ROW(8, 1);
+  if (H <= 8192) PMPE_ROW(16, 1);
   PMPE_ROW(16, 2);
 #undef PMPE_ROW
 }
@@ -250,7 +257,7 @@ hipError_t by_row(int H, bool few, F&& f) {
 }  // namespace
 
 hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s) {
-  return by_row(a.H, a.T < 2048, [&](auto w, auto v) {
+  return by_row(a.H, [&](auto w, auto v) {
     constexpr int W = decltype(w)::value, V = decltype(v)::value, RPB = W == 1 ? 4 : 1;
     const dim3 grid((a.T + RPB - 1) / RPB), block(W == 1 ? 256 : 64 * W);
     if (a.bf16)
@@ -262,13 +269,14 @@ hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s) {
 }
 
 int rmsnorm_bwd_parts(int T, int H) {
-  const int rows = H <= 2048 ? 4 : 1;  // rows of a block at a time
-  return std::min((T + rows - 1) / rows, H <= 8192 ? 512 : 256);
+  const int waves = (H + 511) / 512;  // of a row, up to a power of two
+  const int blocks = waves <= 1 ? 512 : waves <= 2 ? 1024 : waves <= 4 ? 1024 : waves <= 8 ? 512 : 256;
+  return std::min((T + (waves <= 1 ? 3 : 0)) / (waves <= 1 ? 4 : 1), blocks);
 }
 
 hipError_t launch_rmsnorm_bwd(const NormBwdArgs& a, hipStream_t s) {
   const int parts = rmsnorm_bwd_parts(a.T, a.H);
-  const hipError_t e = a.T == 0 ? hipSuccess : by_row(a.H, false, [&](auto w, auto v) {
+  const hipError_t e = a.T == 0 ? hipSuccess : by_row(a.H, [&](auto w, auto v) {
     constexpr int W = decltype(w)::value, V = decltype(v)::value;
     const dim3 grid(parts), block(W == 1 ? 256 : 64 * W);
     if (a.bf16 && a.dy32)
@@ -280,7 +288,7 @@ hipError_t launch_rmsnorm_bwd(const NormBwdArgs& a, hipStream_t s) {
     return hipGetLastError();
   });
   if (e != hipSuccess || !a.dw) return e;
-  rmsnorm_dw_kernel<<<(a.H + 15) / 16, 256, 0, s>>>(a.dw_part, parts, a.H, a.dw);
+  rmsnorm_dw_kernel<<<(a.H + 63) / 64, 1024, 0, s>>>(a.dw_part, parts, a.H, a.dw);
   return hipGetLastError();
 }
 
