@@ -680,8 +680,9 @@ pmpe_status pmpe_rmsnorm_backward(int32_t T, int32_t H, int32_t dtype, const voi
  *   gate_e = scale softmax over the selected z                   RENORM_TOPK, softmax
  *   gate_e = scale s_e                                           POOL_SOFTMAX: scores as they are
  *
- * s, u and the ranks are 64-bit: the selection is that of 64-bit arithmetic on the fp32 logits. A
- * logit of -inf (or NaN) masks its expert: score and gate 0, no part in a group's rank, selected
+ * s, u and the ranks are 64-bit: the selection is that of 64-bit arithmetic on the fp32 logits. (A
+ * rank that is a sum of two is rounded to 45 bits, so that sums which differ only by their terms'
+ * rounding are equal: the sigmoids of z and -z add up to 1 for every z.) A logit of -inf (or NaN) masks its expert: score and gate 0, no part in a group's rank, selected
  * only when nothing else is left. +inf counts as the largest finite value. A bias of -inf (or NaN)
  * ranks an expert with the masked ones, its score staying. With route_mode SOFT (the control arm)
  * the pool is the concatenated one and neither pool may have groups.

@@ -466,51 +466,58 @@ def _dtype(t: torch.Tensor, name: str) -> int:
     return _DTYPES[t.dtype]
 
 
-def _here(t: torch.Tensor, name: str) -> torch.device:
-    """The device of `t`, which has to be the current one: the call's stream is one of its streams."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+def _here(t: torch.Tensor, name: str) -> int:
+    """The device index of `t`, which has to be the current HIP device: the call's stream is one of its streams."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError(f"{name} is on {t.device}, not on the current HIP device")
-    return t.device
+    return dev
 
 
-def _need(t: Optional[torch.Tensor], name: str, shape, dtype, dev: torch.device) -> None:
-    """`t` is None or a tensor of this shape, one of these types and this device."""
-    if t is not None and (t.shape != shape or t.dtype not in dtype or t.device != dev):
-        raise ValueError(f"{name} must be {list(shape)} of {' or '.join(map(str, dtype))} on {dev}, "
-                         f"not {list(t.shape)} of {t.dtype} on {t.device}")
+def _arg(t: Optional[torch.Tensor], name: str, shape, dtype, dev: int) -> Optional[int]:
+    """Pointer of `t`, which is None or a contiguous tensor of this shape, one of these types and this device."""
+    if t is None:
+        return None
+    if t.dtype in dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be a contiguous {list(shape)} of {' or '.join(map(str, dtype))} on device {dev}, "
+                     f"not {list(t.shape)} of {t.dtype} on {t.device} with strides {t.stride()}")
 
 
-def _need_len(t: Optional[torch.Tensor], name: str, n: int, dtype, dev: torch.device) -> None:
-    """`t` is None or a tensor of n elements (of any shape), one of these types and this device."""
-    if t is not None and (t.numel() != n or t.dtype not in dtype or t.device != dev):
-        raise ValueError(f"{name} must have {n} elements of {' or '.join(map(str, dtype))} on {dev}, "
-                         f"not {list(t.shape)} of {t.dtype} on {t.device}")
+def _arg_n(t: Optional[torch.Tensor], name: str, n: int, dtype, dev: int) -> Optional[int]:
+    """The same for a tensor of n elements, of any shape."""
+    if t is None:
+        return None
+    if t.dtype in dtype and t.get_device() == dev and t.numel() == n and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous, {n} elements of {' or '.join(map(str, dtype))} on device {dev}, "
+                     f"not {list(t.shape)} of {t.dtype} on {t.device} with strides {t.stride()}")
 
 
-def _need_bytes(ws: Optional[torch.Tensor], dev: torch.device) -> int:
-    """Bytes of a workspace on this device (0 for None)."""
+def _work(ws: Optional[torch.Tensor], dev: int):
+    """Pointer and bytes of a workspace on this device (None and 0 for None)."""
     if ws is None:
-        return 0
-    if ws.device != dev:
-        raise ValueError(f"the workspace is on {ws.device}, not on {dev}")
-    return ws.numel() * ws.element_size()
+        return None, 0
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"the workspace must be contiguous on device {dev}, not on {ws.device}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+_F32, _BF16, _U8, _I32T = (torch.float32,), (torch.bfloat16,), (torch.uint8,), (torch.int32,)
+_WORDS, _FLOATS = (torch.int32, torch.uint32), tuple(_DTYPES)
 
 
 def pmpe_rmsnorm(x, residual, weight, eps: float, sum_out, out, out_q, out_scale, rstd, stream=None) -> None:
     """Residual add and RMS norm of x [T, H] (bf16 or fp32): r = x + residual into sum_out,
     the norm of r into out and, in 8 bits, into out_q [T, H] with out_scale [T, H / 32]
     (uint8); each output may be None."""
-    T, H = x.shape
-    dev = _here(x, "x")
-    for t, name in ((residual, "residual"), (sum_out, "sum_out"), (out, "out")):
-        _need(t, name, (T, H), (x.dtype,), dev)
-    _need(weight, "weight", (H,), tuple(_DTYPES), dev)
-    _need(out_q, "out_q", (T, H), (torch.uint8,), dev)
-    _need(out_scale, "out_scale", (T, H // 32), (torch.uint8,), dev)
-    _need(rstd, "rstd", (T,), (torch.float32,), dev)
-    _check(_lib.pmpe_rmsnorm(T, H, _dtype(x, "x"), _ptr(x), _ptr(residual), _ptr(weight), _dtype(weight, "weight"), eps,
-                             _ptr(sum_out), _ptr(out), _ptr(out_q), _ptr(out_scale), _ptr(rstd), _stream(stream)),
-           "pmpe_rmsnorm")
+    dev, shape, act = _here(x, "x"), x.shape, (x.dtype,)
+    T, H = shape
+    _check(_lib.pmpe_rmsnorm(
+        T, H, _dtype(x, "x"), _ptr(x), _arg(residual, "residual", shape, act, dev), _arg(weight, "weight", (H,), _FLOATS, dev),
+        _DTYPES[weight.dtype], eps, _arg(sum_out, "sum_out", shape, act, dev), _arg(out, "out", shape, act, dev),
+        _arg(out_q, "out_q", shape, _U8, dev), _arg(out_scale, "out_scale", (T, H // 32), _U8, dev),
+        _arg(rstd, "rstd", (T,), _F32, dev), _stream(stream)), "pmpe_rmsnorm")
 
 
 def pmpe_rmsnorm_backward_workspace_bytes(T: int, H: int) -> int:
@@ -519,46 +526,34 @@ def pmpe_rmsnorm_backward_workspace_bytes(T: int, H: int) -> int:
 
 def pmpe_rmsnorm_backward(dy, dres, r, weight, rstd, dx, dweight, ws, stream=None) -> None:
     """Gradients of pmpe_rmsnorm: dx [T, H] (of r's type) and dweight [H] fp32 or None."""
-    T, H = r.shape
-    dev = _here(r, "r")
-    _need(dy, "dy", (T, H), (torch.float32, r.dtype), dev)
-    _need(dres, "dres", (T, H), (r.dtype,), dev)
-    _need(dx, "dx", (T, H), (r.dtype,), dev)
-    _need(weight, "weight", (H,), tuple(_DTYPES), dev)
-    _need(rstd, "rstd", (T,), (torch.float32,), dev)
-    _need(dweight, "dweight", (H,), (torch.float32,), dev)
-    _check(_lib.pmpe_rmsnorm_backward(T, H, _dtype(r, "r"), _ptr(dy), _dtype(dy, "dy"), _ptr(dres), _ptr(r), _ptr(weight),
-                                      _dtype(weight, "weight"), _ptr(rstd), _ptr(dx), _ptr(dweight), _ptr(ws),
-                                      _need_bytes(ws, dev), _stream(stream)),
-           "pmpe_rmsnorm_backward")
+    dev, shape, act = _here(r, "r"), r.shape, (r.dtype,)
+    T, H = shape
+    _check(_lib.pmpe_rmsnorm_backward(
+        T, H, _dtype(r, "r"), _arg(dy, "dy", shape, (torch.float32, r.dtype), dev), _dtype(dy, "dy"),
+        _arg(dres, "dres", shape, act, dev), _ptr(r), _arg(weight, "weight", (H,), _FLOATS, dev), _DTYPES[weight.dtype],
+        _arg(rstd, "rstd", (T,), _F32, dev), _arg(dx, "dx", shape, act, dev), _arg(dweight, "dweight", (H,), _F32, dev),
+        *_work(ws, dev), _stream(stream)), "pmpe_rmsnorm_backward")
 
 
 def pmpe_select(desc, rule, T, logits, select_bias, policy_word, topk_idx, topk_gate, topk_logit, allow, margin,
                 stream=None) -> None:
     """Selection and gates by `rule` from router logits [T, n_pub + n_priv] (fp32 or bf16)."""
-    dev, E, k = _here(logits, "logits"), desc.n_pub + desc.n_priv, desc.top_k
-    _need(logits, "logits", (T, E), tuple(_DTYPES), dev)
-    _need(select_bias, "select_bias", (E,), (torch.float32,), dev)
-    for t, name, n, dt in ((policy_word, "policy_word", T, (torch.int32, torch.uint32)), (topk_idx, "topk_idx", T * k, (torch.int32,)),
-                           (topk_gate, "topk_gate", T * k, (torch.float32,)),
-                           (topk_logit, "topk_logit", T * k, (torch.float32,)), (allow, "allow", T, (torch.uint8,)),
-                           (margin, "margin", T, (torch.float32,))):
-        _need_len(t, name, n, dt, dev)
-    _check(_lib.pmpe_select(ctypes.byref(desc), ctypes.byref(rule), T, _ptr(logits), _dtype(logits, "logits"),
-                            _ptr(select_bias), _ptr(policy_word), _ptr(topk_idx), _ptr(topk_gate), _ptr(topk_logit),
-                            _ptr(allow), _ptr(margin), _stream(stream)), "pmpe_select")
+    dev, E, n = _here(logits, "logits"), desc.n_pub + desc.n_priv, T * desc.top_k
+    _check(_lib.pmpe_select(
+        ctypes.byref(desc), ctypes.byref(rule), T, _arg(logits, "logits", (T, E), _FLOATS, dev), _DTYPES[logits.dtype],
+        _arg(select_bias, "select_bias", (E,), _F32, dev), _arg_n(policy_word, "policy_word", T, _WORDS, dev),
+        _arg_n(topk_idx, "topk_idx", n, _I32T, dev), _arg_n(topk_gate, "topk_gate", n, _F32, dev),
+        _arg_n(topk_logit, "topk_logit", n, _F32, dev), _arg_n(allow, "allow", T, _U8, dev),
+        _arg_n(margin, "margin", T, _F32, dev), _stream(stream)), "pmpe_select")
 
 
 def pmpe_select_backward(desc, rule, T, logits, topk_idx, dgate, dlogits, stream=None) -> None:
     """Gradient dlogits [T, n_pub + n_priv] fp32 of pmpe_select's gates for their gradient dgate."""
-    dev, E, k = _here(logits, "logits"), desc.n_pub + desc.n_priv, desc.top_k
-    _need(logits, "logits", (T, E), tuple(_DTYPES), dev)
-    _need(dlogits, "dlogits", (T, E), (torch.float32,), dev)
-    _need_len(topk_idx, "topk_idx", T * k, (torch.int32,), dev)
-    _need_len(dgate, "dgate", T * k, (torch.float32,), dev)
-    _check(_lib.pmpe_select_backward(ctypes.byref(desc), ctypes.byref(rule), T, _ptr(logits), _dtype(logits, "logits"),
-                                     _ptr(topk_idx), _ptr(dgate), _ptr(dlogits), _stream(stream)),
-           "pmpe_select_backward")
+    dev, E, n = _here(logits, "logits"), desc.n_pub + desc.n_priv, T * desc.top_k
+    _check(_lib.pmpe_select_backward(
+        ctypes.byref(desc), ctypes.byref(rule), T, _arg(logits, "logits", (T, E), _FLOATS, dev), _DTYPES[logits.dtype],
+        _arg_n(topk_idx, "topk_idx", n, _I32T, dev), _arg_n(dgate, "dgate", n, _F32, dev),
+        _arg(dlogits, "dlogits", (T, E), _F32, dev), _stream(stream)), "pmpe_select_backward")
 
 
 def pmpe_route_scored(desc, rule, T, x, wr_pub, wr_priv, logit_bias, select_bias, policy_word, topk_idx, topk_gate,
@@ -583,9 +578,11 @@ class GradList:
             _dtype(t, f"gradient {i}")
             if t.device != self.tensors[0].device:
                 raise ValueError("the gradients of a list are on one device")
+        self.device = self.tensors[0].get_device() if n else -1
         self.ptrs = (ctypes.c_void_p * n)(*[_ptr(t) for t in self.tensors])
         self.sizes = (ctypes.c_uint64 * n)(*[t.numel() for t in self.tensors])
         self.dtypes = (_I32 * n)(*[_DTYPES[t.dtype] for t in self.tensors])
+        self.key = (bytes(self.sizes), bytes(self.dtypes))
 
     def __len__(self) -> int:
         return len(self.tensors)
@@ -600,48 +597,43 @@ def pmpe_grad_norm_workspace_bytes(grads) -> int:
     return int(_lib.pmpe_grad_norm_workspace_bytes(g.sizes, len(g)))
 
 
-def _norm_of(norm: torch.Tensor) -> torch.device:
-    dev = _here(norm, "norm")
-    _need_len(norm, "norm", 2, (torch.float32,), dev)
-    return dev
+def _grad_args(grads, norm: torch.Tensor):
+    """The list of gradients, the norm's pointer and their device."""
+    g, dev = GradList.of(grads), _here(norm, "norm")
+    if len(g) and g.device != dev:
+        raise ValueError(f"the gradients are on {g.tensors[0].device}, not on device {dev}")
+    return g, _arg(norm, "norm", (2,), _F32, dev), dev
 
 
 def pmpe_grad_norm(grads, max_norm: float, norm: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
     """Global norm of the gradients (a GradList or tensors) and the factor that clips them to
     max_norm, into norm [2] fp32."""
-    g, dev = GradList.of(grads), _norm_of(norm)
-    if len(g) and g.tensors[0].device != dev:
-        raise ValueError(f"the gradients are on {g.tensors[0].device}, not on {dev}")
-    _check(_lib.pmpe_grad_norm(g.ptrs, g.sizes, g.dtypes, len(g), max_norm, _ptr(norm), _ptr(ws), _need_bytes(ws, dev),
-                               _stream(stream)), "pmpe_grad_norm")
+    g, np, dev = _grad_args(grads, norm)
+    _check(_lib.pmpe_grad_norm(g.ptrs, g.sizes, g.dtypes, len(g), max_norm, np, *_work(ws, dev), _stream(stream)),
+           "pmpe_grad_norm")
 
 
 def pmpe_clip_grads(grads, outs, norm: torch.Tensor, stream=None) -> None:
     """The gradients times the factor of pmpe_grad_norm, into `outs` (None: in place)."""
-    g, dev = GradList.of(grads), _norm_of(norm)
-    if len(g) and g.tensors[0].device != dev:
-        raise ValueError(f"the gradients are on {g.tensors[0].device}, not on {dev}")
+    g, np, dev = _grad_args(grads, norm)
     o = None
     if outs is not None:
         o = GradList.of(outs)
-        if len(o) != len(g) or bytes(o.sizes) != bytes(g.sizes) or bytes(o.dtypes) != bytes(g.dtypes) \
-                or (len(o) and o.tensors[0].device != dev):
+        if o.key != g.key or (len(o) and o.device != dev):
             raise ValueError("outs must be tensors of the gradients' sizes and types on their device")
-    _check(_lib.pmpe_clip_grads(g.ptrs, None if o is None else o.ptrs, g.sizes, g.dtypes, len(g), _ptr(norm),
-                                _stream(stream)), "pmpe_clip_grads")
+    _check(_lib.pmpe_clip_grads(g.ptrs, None if o is None else o.ptrs, g.sizes, g.dtypes, len(g), np, _stream(stream)),
+           "pmpe_clip_grads")
 
 
 def pmpe_adamw_clipped(param: torch.Tensor, master: Optional[torch.Tensor], grad: torch.Tensor,
                        m: torch.Tensor, v: torch.Tensor, step: int, lr: float, beta1: float, beta2: float,
                        eps: float, weight_decay: float, norm: torch.Tensor, stream=None) -> None:
     """pmpe_adamw on the gradient times the factor that pmpe_grad_norm wrote to `norm`."""
-    dev = _norm_of(norm)
-    for t, name in ((master, "master"), (grad, "grad"), (m, "m"), (v, "v")):
-        _need_len(t, name, param.numel(), (torch.float32,), dev)
-    _need_len(param, "param", param.numel(), tuple(_DTYPES), dev)
-    _check(_lib.pmpe_adamw_clipped(_ptr(param), _DTYPES[param.dtype], _ptr(master), _ptr(grad), _ptr(m), _ptr(v),
-                                   param.numel(), step, lr, beta1, beta2, eps, weight_decay, _ptr(norm), _stream(stream)),
-           "pmpe_adamw_clipped")
+    dev, n = _here(norm, "norm"), param.numel()
+    _check(_lib.pmpe_adamw_clipped(
+        _arg_n(param, "param", n, _FLOATS, dev), _DTYPES[param.dtype], _arg_n(master, "master", n, _F32, dev),
+        _arg_n(grad, "grad", n, _F32, dev), _arg_n(m, "m", n, _F32, dev), _arg_n(v, "v", n, _F32, dev), n, step, lr, beta1,
+        beta2, eps, weight_decay, _arg(norm, "norm", (2,), _F32, dev), _stream(stream)), "pmpe_adamw_clipped")
 
 
 def pmpe_expert_ffn_mx_workspace_bytes(desc: LayerDesc, T: int) -> int:
@@ -653,12 +645,17 @@ def pmpe_expert_ffn_mx(desc, T, xq, xs, expert_count, expert_offset, row_token, 
                        dev_status, ws, stream=None) -> None:
     """Expert FFN on 8-bit activations xq [T, H] with block scales xs [T, H / 32] (both uint8,
     as pmpe_rmsnorm writes them) and 8-bit weights with row scales."""
-    dev, H = _here(xq, "xq"), desc.hidden
-    _need(xq, "xq", (T, H), (torch.uint8,), dev)
-    _need(xs, "xs", (T, H // 32), (torch.uint8,), dev)
-    _need_len(y_perm, "y_perm", T * desc.top_k * H, (torch.bfloat16,), dev)
+    dev, H, n = _here(xq, "xq"), desc.hidden, T * desc.top_k
+    P, E = desc.n_priv, desc.n_pub + desc.n_priv
+    wt = [_arg_n(t, name, cnt * rows * cols, _U8, dev) for t, name, cnt, rows, cols in (
+        (w13_pub, "w13_pub", desc.n_pub, 2 * desc.inter, H), (w2_pub, "w2_pub", desc.n_pub, H, desc.inter),
+        (w13_priv, "w13_priv", P, 2 * desc.inter, H), (w2_priv, "w2_priv", P, H, desc.inter))]
+    ws_ = [_arg_n(t, name, cnt * rows, _F32, dev) for t, name, cnt, rows in (
+        (w13s_pub, "w13s_pub", desc.n_pub, 2 * desc.inter), (w2s_pub, "w2s_pub", desc.n_pub, H),
+        (w13s_priv, "w13s_priv", P, 2 * desc.inter), (w2s_priv, "w2s_priv", P, H))]
     _check(_lib.pmpe_expert_ffn_mx(
-        ctypes.byref(desc), T, _ptr(xq), _ptr(xs), _ptr(expert_count), _ptr(expert_offset), _ptr(row_token),
-        _ptr(w13_pub), _ptr(w2_pub), _ptr(w13_priv), _ptr(w2_priv), _ptr(w13s_pub), _ptr(w2s_pub), _ptr(w13s_priv),
-        _ptr(w2s_priv), _ptr(y_perm), _ptr(audit_token_rows), _ptr(audit_priv_calls), _ptr(dev_status), _ptr(ws),
-        _need_bytes(ws, dev), _stream(stream)), "pmpe_expert_ffn_mx")
+        ctypes.byref(desc), T, _arg(xq, "xq", (T, H), _U8, dev), _arg(xs, "xs", (T, H // 32), _U8, dev),
+        _arg_n(expert_count, "expert_count", E, _I32T, dev), _arg_n(expert_offset, "expert_offset", E + 1, _I32T, dev),
+        _arg_n(row_token, "row_token", n, _I32T, dev), *wt, *ws_, _arg_n(y_perm, "y_perm", n * H, _BF16, dev),
+        _arg_n(audit_token_rows, "audit_token_rows", T, _WORDS, dev), _arg_n(audit_priv_calls, "audit_priv_calls", P, _WORDS, dev),
+        _arg_n(dev_status, "dev_status", 1, _WORDS, dev), *_work(ws, dev), _stream(stream)), "pmpe_expert_ffn_mx")

@@ -107,6 +107,20 @@ __device__ __forceinline__ uint64_t shfl_u64(uint64_t v, int src) {
   return ((uint64_t)hi << 32) | lo;
 }
 
+// The value of lane (lane ^ stride) for the strides of a wave bitonic network, without the
+// LDS crossbar where a lane-permuting move does it: DPP quad permutations for strides 1 and 2,
+// a rotation by 8 within each row of 16 lanes for stride 8 (a rotation by 8 of 16 lanes is
+// the xor), ds_swizzle (xor mask within 32 lanes) for 4 and 16, a full shuffle for 32.
+__device__ __forceinline__ uint32_t xor_lanes(uint32_t x, int stride) {
+  const int v = (int)x;
+  if (stride == 1) return (uint32_t)__builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, false);  // [1,0,3,2]
+  if (stride == 2) return (uint32_t)__builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, false);  // [2,3,0,1]
+  if (stride == 8) return (uint32_t)__builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, false);  // row_ror:8
+  if (stride == 4) return (uint32_t)__builtin_amdgcn_ds_swizzle(v, (4 << 10) | 0x1F);
+  if (stride == 16) return (uint32_t)__builtin_amdgcn_ds_swizzle(v, (16 << 10) | 0x1F);
+  return (uint32_t)__shfl_xor(v, stride, 64);
+}
+
 // Position of expert e in the order of the grouped GEMMs on 256-row tiles: the public and the private
 // experts interleaved in proportion to the pool sizes (public j before private p iff
 // (2j+1) n_priv <= (2p+1) n_pub).

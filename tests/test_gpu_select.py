@@ -52,7 +52,10 @@ def choose(z, bias, k, rule, groups, keep, renorm):
 
         def rank(g):
             best = sorted((v for v in u[g * gs:(g + 1) * gs] if v > -math.inf), reverse=True)[:rule.group_top]
-            return sum(best) if best else -math.inf
+            if len(best) < 2 or math.isinf(sum(best)):
+                return sum(best) if best else -math.inf
+            m, e = math.frexp(sum(best))
+            return math.ldexp(round(math.ldexp(m, 45)), e - 45)  # a sum of two ranks by 45 bits
         kept = sorted(sorted(range(groups), key=lambda g: (-rank(g), g))[:keep])
         cand = [i for g in kept for i in range(g * gs, (g + 1) * gs)]
     order = sorted(cand, key=lambda i: (-u[i], i))
@@ -178,6 +181,18 @@ def test_ties_masks_and_values_that_are_not_finite(score, groups, renorm):
     bias[6] = float("nan")
     bias[70] = 1e30
     check(d, rule, z, bias.cuda(), words)
+
+
+def test_groups_whose_sums_agree_but_for_rounding_tie():
+    """s(z) + s(-z) is 1 for every z, up to the rounding of the two: the lower group stays."""
+    d = P.make_desc(128, 64, 64, 16, 2)
+    rule = P.make_score_rule(P.PMPE_SCORE_SIGMOID, (32, 1), (8, 1), 2)
+    half = rand((500, 40), 11, 2.0)
+    z = torch.stack([half, -half], dim=2).reshape(500, 80).contiguous()
+    words = torch.zeros(500, dtype=torch.int32)
+    words[250:] = ALLOW
+    got = check(d, rule, z, None, words.cuda())
+    assert (got["idx"][:250].cpu() == torch.tensor([0, 1])).all() and (got["idx"][250:].cpu() == torch.tensor([64, 65])).all()
 
 
 def test_near_ties_are_those_of_64_bits():
