@@ -177,14 +177,12 @@ pmpe_status pmpe_select_backward(const pmpe_layer_desc* d, const pmpe_score_rule
 
 size_t pmpe_grad_norm_workspace_bytes(const uint64_t* n, int32_t count) {
   if (count < 0 || count > PMPE_MAX_GRADS || (count > 0 && !n)) return 0;
-  // launches of GRAD_LIST tensors, and one more wherever the chunks of a launch would pass 2^31
-  uint64_t elements = 0;
+  uint64_t pieces = 0;
   for (int32_t i = 0; i < count; ++i) {
     if (n[i] >= ((uint64_t)1 << 43)) return 0;
-    elements += n[i];
+    pieces += (n[i] + GRAD_PIECE - 1) / GRAD_PIECE;
   }
-  const uint64_t launches = (uint64_t)count / GRAD_LIST + 1 + 2 * (elements >> 43);
-  return (size_t)launches * GRAD_BLOCKS * sizeof(double);
+  return (size_t)(pieces / GRAD_LIST + 1) * GRAD_BLOCKS * sizeof(double);
 }
 
 pmpe_status pmpe_grad_norm(const void* const* grads, const uint64_t* n, const int32_t* dtype,

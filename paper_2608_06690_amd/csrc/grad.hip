@@ -6,7 +6,13 @@
 // values are exact in fp64 and summed there (no overflow or cancellation below 1e150 terms of any
 // fp32 size; fp64 runs at the rate of scalar fp32, far below the memory time). The tensors are cut
 // into chunks; a block adds every gridDim-th chunk and a last block the blocks' sums, all in a fixed
-// order, so equal gradients give equal bits. The list travels by value, GRAD_LIST tensors to a launch.
+// order, so equal gradients give equal bits. The list travels by value, as many pieces of at most 2^31
+// elements to a launch as the 4 KB of a kernel's arguments hold. A block finds the piece of a chunk by
+// reading all of them, one load per lane and 64 of them, and comparing: one latency, where a search of
+// the list waits for eight. The norm of 604 MB of fp32 takes 102 us (5.9 TB/s). Norm and clipping of 500
+// bf16 tensors of up to 200000 elements take 42 us, 34 of them eight launches that cannot overlap: 112 us
+// with 96 tensors to a launch and the last chunk of each tensor read element by element. Chunks of 4096
+// and 8192 elements are equal on large tensors; the smaller ones fill the card with less (42 and 44 us).
 #include <algorithm>
 
 #include "pmpe_internal.h"
@@ -18,15 +24,27 @@ typedef u32x4 u32x4_a2 __attribute__((aligned(2)));  // a gradient may start at 
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 
 constexpr int GR_THREADS = 256;
-constexpr int GR_CHUNK = 8192;  // elements: four vectors of 8 per thread
+constexpr int GR_CHUNK = 4096;  // elements: two vectors of 8 per thread
 
-struct GradTable {
-  const void* src[GRAD_LIST];
-  void* dst[GRAD_LIST];
-  uint64_t n[GRAD_LIST];
-  uint32_t first[GRAD_LIST + 1];  // first chunk of each tensor, and the number of chunks
-  uint8_t bf16[GRAD_LIST];
+// A piece of a gradient: `first` is its first chunk among those of the launch. Bit 63 of src: bf16.
+constexpr uint64_t GR_BF16 = (uint64_t)1 << 63;
+struct NormPiece {
+  uint64_t src;
+  uint32_t n, first;
 };
+struct ScalePiece {
+  uint64_t src, dst;
+  uint32_t n, first;
+};
+template <class P, int COUNT>
+struct GradTable {
+  static constexpr int SIZE = COUNT;
+  P e[COUNT];
+  uint32_t count, chunks;
+};
+// 3.6 KB each
+typedef GradTable<NormPiece, GRAD_LIST> NormTable;
+typedef GradTable<ScalePiece, 152> ScaleTable;
 
 __device__ __forceinline__ double wave_add(double v) {
 #pragma unroll
@@ -45,59 +63,95 @@ __device__ __forceinline__ double block_add(double v, double* s) {
   return v;
 }
 
-// last tensor whose first chunk is at or before c
-__device__ __forceinline__ int tensor_of(const GradTable& t, int count, uint32_t c) {
-  int lo = 0, hi = count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (t.first[mid] <= c) lo = mid; else hi = mid - 1;
+// first[]: those of the pieces lane, 64 + lane, .. (past the last one: 2^32 - 1)
+template <class T>
+__device__ __forceinline__ void read_firsts(const T& t, uint32_t (&first)[(T::SIZE + 63) / 64]) {
+#pragma unroll
+  for (int r = 0; r < (T::SIZE + 63) / 64; ++r) {
+    const uint32_t i = r * 64 + lane_id();
+    first[r] = i < t.count ? t.e[i].first : ~0u;
   }
-  return lo;
+}
+// last piece whose first chunk is at or before c
+template <int R>
+__device__ __forceinline__ int piece_of(const uint32_t (&first)[R], uint32_t c) {
+  int m = -1;
+#pragma unroll
+  for (int r = 0; r < R; ++r) m += __popcll(__ballot(first[r] <= c));
+  return m;
 }
 
-template <bool BF16>
-__device__ __forceinline__ double chunk_squares(const void* p, uint64_t e0, uint64_t n) {
-  double acc[4] = {0, 0, 0, 0};
-  if (e0 + GR_CHUNK <= n) {
-    float v[GR_CHUNK / GR_THREADS];
+// A thread's vectors of 8 elements of the chunk at e0 of a piece: first elements GR_THREADS * 8 apart. Those
+// that the piece ends in are left to one thread, element by element.
+constexpr int GR_VEC = GR_CHUNK / GR_THREADS / 8;
+__device__ __forceinline__ uint32_t vector_at(uint32_t e0, int j) { return e0 + (j * GR_THREADS + threadIdx.x) * 8; }
+
+template <bool STREAM, class V>
+__device__ __forceinline__ V load_vector(const V* p) {
+  if constexpr (STREAM)
+    return __builtin_nontemporal_load(p);
+  else
+    return *p;
+}
+template <bool BF16, bool STREAM>
+__device__ __forceinline__ void load8(const void* p, uint32_t i, float (&v)[8]) {
+  if constexpr (BF16) {
+    const u32x4 q = load_vector<STREAM>((const u32x4_a2*)((const uint16_t*)p + i));
 #pragma unroll
-    for (int j = 0; j < GR_CHUNK / GR_THREADS / 8; ++j) {
-      const uint64_t i = e0 + (uint64_t)(j * GR_THREADS + threadIdx.x) * 8;
-      if constexpr (BF16) {
-        const u32x4 q = *(const u32x4_a2*)((const uint16_t*)p + i);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          v[8 * j + 2 * h] = bf16_to_f32(q[h] & 0xFFFFu);
-          v[8 * j + 2 * h + 1] = bf16_to_f32(q[h] >> 16);
-        }
-      } else {
-        const f32x4 a = *(const f32x4_a4*)((const float*)p + i), b = *(const f32x4_a4*)((const float*)p + i + 4);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          v[8 * j + h] = a[h];
-          v[8 * j + 4 + h] = b[h];
-        }
-      }
+    for (int h = 0; h < 4; ++h) {
+      v[2 * h] = bf16_to_f32(q[h] & 0xFFFFu);
+      v[2 * h + 1] = bf16_to_f32(q[h] >> 16);
     }
-#pragma unroll
-    for (int j = 0; j < GR_CHUNK / GR_THREADS; ++j) acc[j & 3] += (double)v[j] * (double)v[j];
   } else {
-    for (uint64_t i = e0 + threadIdx.x; i < n; i += GR_THREADS) {
-      const double x = BF16 ? bf16_to_f32(((const uint16_t*)p)[i]) : ((const float*)p)[i];
-      acc[0] += x * x;
+    const f32x4_a4* q = (const f32x4_a4*)((const float*)p + i);
+    const f32x4 a = load_vector<STREAM>(q), b = load_vector<STREAM>(q + 1);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      v[h] = a[h];
+      v[4 + h] = b[h];
     }
   }
+}
+template <bool BF16>
+__device__ __forceinline__ float load1(const void* p, uint32_t i) {
+  return BF16 ? bf16_to_f32(((const uint16_t*)p)[i]) : ((const float*)p)[i];
+}
+
+template <bool BF16, bool STREAM>
+__device__ __forceinline__ double chunk_squares(const void* p, uint32_t e0, uint32_t n) {
+  float v[GR_VEC][8];
+#pragma unroll
+  for (int j = 0; j < GR_VEC; ++j) {
+    const uint32_t i = vector_at(e0, j);
+#pragma unroll
+    for (int h = 0; h < 8; ++h) v[j][h] = 0.f;
+    if (i + 8 <= n) {
+      load8<BF16, STREAM>(p, i, v[j]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 7; ++h)
+        if (i + h < n) v[j][h] = load1<BF16>(p, i + h);
+    }
+  }
+  double acc[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < GR_VEC; ++j)
+#pragma unroll
+    for (int h = 0; h < 8; ++h) acc[h & 3] += (double)v[j][h] * (double)v[j][h];
   return (acc[0] + acc[1]) + (acc[2] + acc[3]);
 }
 
-__global__ __launch_bounds__(GR_THREADS) void grad_squares_kernel(GradTable t, int count, double* part) {
+template <bool STREAM>
+__global__ __launch_bounds__(GR_THREADS) void grad_squares_kernel(NormTable t, double* part) {
   __shared__ double s[GR_THREADS / 64];
   double acc = 0.0;
-  const uint32_t chunks = t.first[count];
-  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const int i = tensor_of(t, count, c);
-    const uint64_t e0 = (uint64_t)(c - t.first[i]) * GR_CHUNK;
-    acc += t.bf16[i] ? chunk_squares<true>(t.src[i], e0, t.n[i]) : chunk_squares<false>(t.src[i], e0, t.n[i]);
+  uint32_t first[(NormTable::SIZE + 63) / 64];
+  read_firsts(t, first);
+  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const NormPiece& e = t.e[piece_of(first, c)];
+    const uint32_t e0 = (c - e.first) * GR_CHUNK;
+    const void* src = (const void*)(e.src & ~GR_BF16);
+    acc += (e.src & GR_BF16) ? chunk_squares<true, STREAM>(src, e0, e.n) : chunk_squares<false, STREAM>(src, e0, e.n);
   }
   acc = block_add<GR_THREADS>(acc, s);
   if (threadIdx.x == 0) part[blockIdx.x] = acc;
@@ -116,82 +170,111 @@ __global__ __launch_bounds__(1024) void grad_total_kernel(const double* part, in
 }
 
 template <bool BF16>
-__device__ __forceinline__ void chunk_scale(const void* p, void* o, uint64_t e0, uint64_t n, float coef) {
-  const uint64_t end = e0 + GR_CHUNK < n ? e0 + GR_CHUNK : n;
-  if (e0 + GR_CHUNK <= n) {
-    constexpr int V = GR_CHUNK / GR_THREADS / 8;
-    if constexpr (BF16) {
-      u32x4 q[V];
+__device__ __forceinline__ void store8(void* o, uint32_t i, const float (&v)[8], float coef) {
+  if constexpr (BF16) {
+    u32x4 q;
 #pragma unroll
-      for (int j = 0; j < V; ++j) q[j] = *(const u32x4_a2*)((const uint16_t*)p + e0 + (j * GR_THREADS + threadIdx.x) * 8);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-#pragma unroll
-        for (int h = 0; h < 4; ++h) q[j][h] = pack_bf16x2(bf16_to_f32(q[j][h] & 0xFFFFu) * coef, bf16_to_f32(q[j][h] >> 16) * coef);
-        *(u32x4_a2*)((uint16_t*)o + e0 + (j * GR_THREADS + threadIdx.x) * 8) = q[j];
-      }
-    } else {
-      f32x4 q[2 * V];
-#pragma unroll
-      for (int j = 0; j < 2 * V; ++j) q[j] = *(const f32x4_a4*)((const float*)p + e0 + (j * GR_THREADS + threadIdx.x) * 4);
-#pragma unroll
-      for (int j = 0; j < 2 * V; ++j) *(f32x4_a4*)((float*)o + e0 + (j * GR_THREADS + threadIdx.x) * 4) = q[j] * coef;
-    }
+    for (int h = 0; h < 4; ++h) q[h] = pack_bf16x2(v[2 * h] * coef, v[2 * h + 1] * coef);
+    *(u32x4_a2*)((uint16_t*)o + i) = q;
   } else {
-    for (uint64_t i = e0 + threadIdx.x; i < end; i += GR_THREADS) {
-      if constexpr (BF16)
-        ((uint16_t*)o)[i] = (uint16_t)f32_to_bf16_rne(bf16_to_f32(((const uint16_t*)p)[i]) * coef);
-      else
-        ((float*)o)[i] = ((const float*)p)[i] * coef;
+    const f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+    *(f32x4_a4*)((float*)o + i) = a * coef;
+    *(f32x4_a4*)((float*)o + i + 4) = b * coef;
+  }
+}
+
+template <bool BF16>
+__device__ __forceinline__ void chunk_scale(const void* p, void* o, uint32_t e0, uint32_t n, float coef) {
+  float v[GR_VEC][8];
+#pragma unroll
+  for (int j = 0; j < GR_VEC; ++j) {
+    const uint32_t i = vector_at(e0, j);
+    if (i + 8 <= n) load8<BF16, false>(p, i, v[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < GR_VEC; ++j) {
+    const uint32_t i = vector_at(e0, j);
+    if (i + 8 <= n) {
+      store8<BF16>(o, i, v[j], coef);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 7; ++h) {
+        if (i + h >= n) continue;
+        if constexpr (BF16)
+          ((uint16_t*)o)[i + h] = (uint16_t)f32_to_bf16_rne(load1<true>(p, i + h) * coef);
+        else
+          ((float*)o)[i + h] = load1<false>(p, i + h) * coef;
+      }
     }
   }
 }
 
-__global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(GradTable t, int count, const float* norm) {
+__global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(ScaleTable t, const float* norm) {
   const float coef = norm[1];
-  const uint32_t chunks = t.first[count];
-  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const int i = tensor_of(t, count, c);
-    if (coef == 1.0f && t.dst[i] == t.src[i]) continue;  // in place and inside the bound: nothing changes
-    const uint64_t e0 = (uint64_t)(c - t.first[i]) * GR_CHUNK;
-    if (t.bf16[i])
-      chunk_scale<true>(t.src[i], t.dst[i], e0, t.n[i], coef);
+  uint32_t first[(ScaleTable::SIZE + 63) / 64];
+  read_firsts(t, first);
+  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const ScalePiece& e = t.e[piece_of(first, c)];
+    const void* src = (const void*)(e.src & ~GR_BF16);
+    void* dst = (void*)e.dst;
+    if (coef == 1.0f && dst == src) continue;  // in place and inside the bound: nothing changes
+    const uint32_t e0 = (c - e.first) * GR_CHUNK;
+    if (e.src & GR_BF16)
+      chunk_scale<true>(src, dst, e0, e.n, coef);
     else
-      chunk_scale<false>(t.src[i], t.dst[i], e0, t.n[i], coef);
+      chunk_scale<false>(src, dst, e0, e.n, coef);
   }
 }
 
-// The next tensors of the list that have elements, from *at on: up to GRAD_LIST of them and 2^31 chunks.
-int fill(const GradListArgs& a, int* at, GradTable* t) {
-  int m = 0;
-  uint64_t chunks = 0;
-  for (; *at < a.count && m < GRAD_LIST; ++*at) {
-    const int i = *at;
-    if (a.n[i] == 0) continue;
-    const uint64_t c = (a.n[i] + GR_CHUNK - 1) / GR_CHUNK;
-    if (m > 0 && chunks + c > GRAD_MAX_CHUNKS) break;
-    t->src[m] = a.src[i];
-    t->dst[m] = a.dst ? a.dst[i] : const_cast<void*>(a.src[i]);
-    t->n[m] = a.n[i];
-    t->bf16[m] = a.dtype[i] == PMPE_BF16;
-    t->first[m] = (uint32_t)chunks;
-    chunks += c;
-    ++m;
+// The pieces of the list, a table at a time.
+template <class T>
+class Tables {
+ public:
+  explicit Tables(const GradListArgs& a) : a_(a) {}
+  // false: no piece is left
+  bool next(T* t) {
+    t->count = t->chunks = 0;
+    while (at_ < a_.count && t->count < (uint32_t)T::SIZE) {
+      const uint64_t n = std::min(a_.n[at_] - done_, GRAD_PIECE), el = a_.dtype[at_] == PMPE_BF16 ? 2 : 4;
+      if (n > 0) {
+        auto& e = t->e[t->count++];
+        e.src = ((uint64_t)(uintptr_t)a_.src[at_] + done_ * el) | (el == 2 ? GR_BF16 : 0);
+        if constexpr (sizeof(e) == sizeof(ScalePiece))
+          e.dst = (uint64_t)(uintptr_t)(a_.dst ? a_.dst[at_] : a_.src[at_]) + done_ * el;
+        e.n = (uint32_t)n;
+        e.first = t->chunks;
+        t->chunks += (uint32_t)((n + GR_CHUNK - 1) / GR_CHUNK);
+      }
+      done_ += n;
+      if (done_ == a_.n[at_]) {
+        ++at_;
+        done_ = 0;
+      }
+    }
+    return t->count > 0;
   }
-  t->first[m] = (uint32_t)chunks;
-  return m;
-}
+
+ private:
+  const GradListArgs& a_;
+  int at_ = 0;
+  uint64_t done_ = 0;
+};
 
 }  // namespace
 
 hipError_t launch_grad_norm(const GradListArgs& a, double max_norm, float* norm, double* part, hipStream_t s) {
-  int at = 0, parts = 0;
-  while (at < a.count) {
-    GradTable t;
-    const int m = fill(a, &at, &t);
-    if (m == 0) break;
-    const int grid = (int)std::min<uint32_t>(t.first[m], GRAD_BLOCKS);
-    grad_squares_kernel<<<grid, GR_THREADS, 0, s>>>(t, m, part + parts);
+  // Lists that the caches cannot hold until the step are read past them: what they hold (the last step's
+  // states among it) is not pushed out. Norm and step of 604 MB of fp32 gradients: 931 us -> 909, of
+  // 151 MB: 244 -> 238; of 38 MB 74 -> 76, where the step then finds less in them.
+  uint64_t bytes = 0;
+  for (int i = 0; i < a.count; ++i) bytes += a.n[i] * (a.dtype[i] == PMPE_BF16 ? 2 : 4);
+  const auto kernel = bytes >= ((uint64_t)128 << 20) ? grad_squares_kernel<true> : grad_squares_kernel<false>;
+  int parts = 0;
+  Tables<NormTable> list(a);
+  NormTable t;
+  while (list.next(&t)) {
+    const int grid = (int)std::min<uint32_t>(t.chunks, GRAD_BLOCKS);
+    kernel<<<grid, GR_THREADS, 0, s>>>(t, part + parts);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     parts += grid;
@@ -201,13 +284,10 @@ hipError_t launch_grad_norm(const GradListArgs& a, double max_norm, float* norm,
 }
 
 hipError_t launch_clip_grads(const GradListArgs& a, const float* norm, hipStream_t s) {
-  int at = 0;
-  while (at < a.count) {
-    GradTable t;
-    const int m = fill(a, &at, &t);
-    if (m == 0) break;
-    const int grid = (int)std::min<uint32_t>(t.first[m], 16384);
-    grad_scale_kernel<<<grid, GR_THREADS, 0, s>>>(t, m, norm);
+  Tables<ScaleTable> list(a);
+  ScaleTable t;
+  while (list.next(&t)) {
+    grad_scale_kernel<<<std::min<uint32_t>(t.chunks, 16384), GR_THREADS, 0, s>>>(t, norm);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -468,9 +468,9 @@ struct GradListArgs {
   const int32_t* dtype;
   int count;
 };
-constexpr int GRAD_LIST = 96;      // tensors of a launch
+constexpr int GRAD_LIST = 224;     // pieces of a launch of the norm
 constexpr int GRAD_BLOCKS = 2048;  // blocks of a launch of the norm
-constexpr uint64_t GRAD_MAX_CHUNKS = (uint64_t)1 << 31;
+constexpr uint64_t GRAD_PIECE = (uint64_t)1 << 31;  // elements of a piece at most
 // part: GRAD_BLOCKS doubles per launch
 hipError_t launch_grad_norm(const GradListArgs& a, double max_norm, float* norm, double* part, hipStream_t s);
 hipError_t launch_clip_grads(const GradListArgs& a, const float* norm, hipStream_t s);

@@ -172,7 +172,7 @@ def test_clip_grads(kw, status):
 
 def test_grad_norm_workspace():
     size = lambda *n: N.lib().pmpe_grad_norm_workspace_bytes((ctypes.c_uint64 * len(n))(*n), len(n))  # noqa: E731
-    assert size() > 0 and size(5) == size(1 << 40) and size(*[1] * 96) == 2 * size(5)
+    assert size() > 0 and size(5) == size(1 << 31) < size(1 << 42) and size(5) < size(*[1] * 500) == size(*[1, 0] * 500)
     assert size(1 << 43) == 0 and N.lib().pmpe_grad_norm_workspace_bytes(None, 1) == 0
     assert N.lib().pmpe_grad_norm_workspace_bytes(None, -1) == 0
 
