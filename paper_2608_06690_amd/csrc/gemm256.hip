@@ -102,6 +102,7 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
   constexpr int SQ = GATED ? (SAVE ? 5 : MX ? 2 : 1) : 1;  // per 16-row block and output half
   constexpr int S2 = GATED ? 0 : 4, S3 = GATED ? 2 * SQ : 4, S4 = GATED ? 2 * SQ : 4, S5 = 4 * SQ;
   constexpr int SALL = S2 + S3 + S4 + S5;
+  constexpr int AFTER2 = SALL / 2;  // MX, both A halves: the second one's, after the last step
   __shared__ __attribute__((aligned(16))) unsigned char smem[2 * STEP];
   __shared__ __attribute__((aligned(16))) int s_rt[NRT][BM];
   __shared__ __attribute__((aligned(16))) int4 s_list[NLIST];
@@ -434,6 +435,11 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     constexpr int SL = decltype(stored)::value;
     if (kind1 == 0 || kind2 == 0) {
       wait_vmcnt<0>();
+    } else if (MX && kind1 == 2) {  // (B1 as well)
+      if (last)
+        wait_vmcnt<N2 - 2 + SL>();
+      else
+        wait_copies(ic<N2 - 2>, ic<AFTER2>, ic<S5>, fresh == 2);
     } else if (kind1 == 2) {
       if (last)
         wait_vmcnt<N2 + SL>();
@@ -517,6 +523,30 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     pin(blocks, acc);
   };
   auto mulc = [&](f32x4 (&acc)[4][2], const Frag (&fb)[2], auto&& copy) { mulc_mb(ic<4>, acc, fb, copy); };
+  // MX: an A half with both B halves; copies 0 .. NC - 1 are spread over it, two MFMAs to a slot
+  auto mul_half = [&](auto blocks, f32x4 (&acc0)[4][2], const Frag (&f0)[2], f32x4 (&acc1)[4][2], const Frag (&f1)[2], auto nc,
+                      auto&& copy) {
+    constexpr int MB = decltype(blocks)::value, NC = decltype(nc)::value;
+    Unroll<0, 2 * MB>::run([&](auto slot) {
+      constexpr int mb = decltype(slot)::value / 2;
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) {
+        if constexpr (decltype(slot)::value % 2 == 0)
+          acc0[mb][nb] = mfma(ic<0>, f0[nb], mb, acc0[mb][nb]);
+        else
+          acc1[mb][nb] = mfma(ic<0>, f1[nb], mb, acc1[mb][nb]);
+      }
+      Unroll<0, NC>::run([&](auto c) {
+        if constexpr (decltype(c)::value * 2 * MB / NC == decltype(slot)::value) {
+          __builtin_amdgcn_sched_barrier(0);
+          copy(c);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      });
+    });
+    pin(blocks, acc0);
+    pin(blocks, acc1);
+  };
   auto end_step = [&]() {
     cbuf ^= STEP;
     kind1 = kind2;
@@ -627,7 +657,57 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     for (int kc = 0; kc < cnk; ++kc) {
       const bool last = kc == cnk - 1;
       if constexpr (MX) csc = cq * (BM * 16) + (kc & 3) * 4;
-      if constexpr (AH == 2) {
+      if constexpr (AH == 2 && MX) {
+        // Two phases, an A half each. A0, B0 and B1 of this step landed in the last one.
+        readA(h0);
+        readB(h0, fb0);
+        readB(h1, fb1);
+        // A1 of this step landed; younger: the next step's other half tiles
+        if (kind1)
+          wait_copies(ic<6>, ic<SALL>, ic<S2 + S5>, fresh == 2);
+        else
+          wait_vmcnt<0>();
+        phase_mid();
+        mul_half(ic<4>, acc[0][0], fb0, acc[0][1], fb1, ic<2>, [&](auto c) { if (late) copyA1(h1, c, cbuf ^ STEP); });
+        if (kind1) ++pk;
+        phase_end();
+
+        readA(h1);
+        if (last) {
+          store(h0, h0, ic<0>, ic<4>);
+          if constexpr (!GATED) store(h0, h1, ic<0>, ic<4>);
+        }
+        // the next step's A0, B0 and B1 landed; younger: its A1
+        if (kind1 == 2) {
+          if (last)
+            wait_vmcnt<2 + SALL - AFTER2>();
+          else
+            wait_copies(ic<2>, ic<AFTER2>, ic<S5>, fresh == 2);
+        } else if (kind1 == 1) {
+          if (last)
+            wait_vmcnt<SALL - AFTER2>();
+          else
+            wait_copies(ic<0>, ic<AFTER2>, ic<S5>, fresh == 2);
+        }
+        kind2 = next_step();
+        phase_mid();
+        mul_half(blocks, acc[1][1], fb1, acc[1][0], fb0, ic<6>, [&](auto c) {
+          constexpr int C = decltype(c)::value;
+          if (!kind2) return;
+          if constexpr (C < 2)
+            copyA1(h0, ic<C>, cbuf);
+          else if constexpr (C < 4)
+            copyB1(h0, ic<C - 2>, cbuf);
+          else
+            copyB1(h1, ic<C - 4>, cbuf);
+        });
+        phase_end();
+        late = kind2 == 2;
+        if (last) {
+          store(h1, h0, ic<0>, ic<4>);
+          if constexpr (!GATED) store(h1, h1, ic<0>, ic<4>);
+        }
+      } else if constexpr (AH == 2) {
         readA(h0);
         readB(h0, fb0);
         // B1 of this step landed; younger: its A1 and the next step
