@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from typing import Optional
 
 import torch
@@ -574,14 +575,17 @@ class GradList:
     def __init__(self, tensors) -> None:
         self.tensors = list(tensors)
         n = len(self.tensors)
-        for i, t in enumerate(self.tensors):
-            _dtype(t, f"gradient {i}")
-            if t.device != self.tensors[0].device:
-                raise ValueError("the gradients of a list are on one device")
-        self.device = self.tensors[0].get_device() if n else -1
-        self.ptrs = (ctypes.c_void_p * n)(*[_ptr(t) for t in self.tensors])
-        self.sizes = (ctypes.c_uint64 * n)(*[t.numel() for t in self.tensors])
-        self.dtypes = (_I32 * n)(*[_DTYPES[t.dtype] for t in self.tensors])
+        types, devices = [t.dtype for t in self.tensors], {t.get_device() for t in self.tensors}
+        if not set(types) <= set(_FLOATS):
+            raise ValueError("gradients must be float32 or bfloat16")
+        if len(devices) > 1:
+            raise ValueError("the gradients of a list are on one device")
+        if not all([t.is_contiguous() for t in self.tensors]):
+            raise ValueError("tensors passed to libpmpe must be contiguous")
+        self.device = devices.pop() if n else -1
+        self.ptrs = (ctypes.c_uint64 * n).from_buffer(array("Q", [t.data_ptr() for t in self.tensors]))
+        self.sizes = (ctypes.c_uint64 * n).from_buffer(array("Q", [t.numel() for t in self.tensors]))
+        self.dtypes = (_I32 * n).from_buffer(array("i", [_DTYPES[d] for d in types]))
         self.key = (bytes(self.sizes), bytes(self.dtypes))
 
     def __len__(self) -> int:
