@@ -797,8 +797,9 @@ pmpe_status pmpe_grad_norm(const void* const* grads, const uint64_t* n, const in
 /*
  * pmpe_clip_grads - outs[i] = round(norm[1] * grads[i]) for every tensor of the list, with the norm
  * that pmpe_grad_norm wrote. outs: HOST array of device pointers (tensors of the gradients' sizes
- * and types), or NULL: in place. outs[i] may be grads[i] but must not overlap it otherwise; with a
- * factor of 1, tensors clipped in place are not touched.
+ * and types), or NULL: in place. outs[i] may be grads[i]; otherwise no output may overlap a tensor
+ * of the list or another output (PMPE_ERR_SHAPE). With a factor of 1, tensors clipped in place are
+ * not touched.
  */
 pmpe_status pmpe_clip_grads(const void* const* grads, void* const* outs, const uint64_t* n,
                             const int32_t* dtype, int32_t count, const float* norm,

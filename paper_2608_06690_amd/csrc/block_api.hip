@@ -1,6 +1,9 @@
 // C ABI of the operators around the layer: argument validation (host only, before any launch)
-// and dispatch to the kernel launchers. No exception crosses this boundary; nothing is allocated.
+// and dispatch to the kernel launchers. No exception crosses this boundary; no device memory is allocated.
+#include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "pmpe_internal.h"
 
@@ -44,6 +47,42 @@ pmpe_status check_grads(const void* const* grads, const uint64_t* n, const int32
     if (((uintptr_t)grads[i] & (dtype[i] == PMPE_BF16 ? 1u : 3u)) != 0) return PMPE_ERR_ALIGN;
   }
   return PMPE_OK;
+}
+
+// Whether an output shares memory with another output, or with a gradient that is not its own. (Lists
+// side by side in memory, the usual ones, are seen to be apart in one pass.)
+bool outputs_overlap(const void* const* grads, const void* const* outs, const uint64_t* n, const int32_t* dtype, int32_t count) {
+  const auto bytes = [&](int32_t i) { return n[i] * (dtype[i] == PMPE_BF16 ? 2 : 4); };
+  bool ascending = true, in_place = true;
+  uintptr_t end = 0, o0 = UINTPTR_MAX, g0 = UINTPTR_MAX, g1 = 0, o1 = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (n[i] == 0) continue;
+    const uintptr_t o = (uintptr_t)outs[i], g = (uintptr_t)grads[i];
+    ascending = ascending && o >= end;
+    in_place = in_place && o == g;
+    end = o + bytes(i);
+    o0 = std::min(o0, o);
+    o1 = std::max(o1, end);
+    g0 = std::min(g0, g);
+    g1 = std::max(g1, g + bytes(i));
+  }
+  if (ascending && (in_place || o1 <= g0 || g1 <= o0)) return false;
+  std::unique_ptr<int32_t[]> at(new (std::nothrow) int32_t[(size_t)count]);
+  if (!at) return true;
+  int32_t m = 0;
+  for (int32_t i = 0; i < count; ++i)
+    if (n[i] > 0) at[m++] = i;
+  std::sort(at.get(), at.get() + m, [&](int32_t a, int32_t b) { return (uintptr_t)outs[a] < (uintptr_t)outs[b]; });
+  for (int32_t j = 1; j < m; ++j)
+    if ((uintptr_t)outs[at[j - 1]] + bytes(at[j - 1]) > (uintptr_t)outs[at[j]]) return true;
+  for (int32_t i = 0; i < count; ++i) {  // the outputs lie apart: those around gradient i
+    if (n[i] == 0) continue;
+    const uintptr_t g = (uintptr_t)grads[i], e = g + bytes(i);
+    int32_t j = (int32_t)(std::upper_bound(at.get(), at.get() + m, g, [&](uintptr_t v, int32_t a) { return v < (uintptr_t)outs[a]; }) - at.get());
+    for (j = j > 0 ? j - 1 : 0; j < m && (uintptr_t)outs[at[j]] < e; ++j)
+      if ((uintptr_t)outs[at[j]] + bytes(at[j]) > g && !(at[j] == i && (uintptr_t)outs[i] == g)) return true;
+  }
+  return false;
 }
 
 }  // namespace
@@ -209,11 +248,9 @@ pmpe_status pmpe_clip_grads(const void* const* grads, void* const* outs, const u
   for (int32_t i = 0; outs && i < count; ++i) {
     if (n[i] == 0) continue;
     if (!outs[i]) return PMPE_ERR_NULL;
-    const uint64_t el = dtype[i] == PMPE_BF16 ? 2 : 4;
-    if (((uintptr_t)outs[i] & (el - 1)) != 0) return PMPE_ERR_ALIGN;
-    const uintptr_t g = (uintptr_t)grads[i], o = (uintptr_t)outs[i];
-    if (g != o && g < o + n[i] * el && o < g + n[i] * el) return PMPE_ERR_SHAPE;  // overlapping
+    if (((uintptr_t)outs[i] & (dtype[i] == PMPE_BF16 ? 1u : 3u)) != 0) return PMPE_ERR_ALIGN;
   }
+  if (outputs_overlap(grads, outs ? outs : grads, n, dtype, count)) return PMPE_ERR_SHAPE;
   return launched(launch_clip_grads(GradListArgs{grads, outs, n, dtype, count}, norm, (hipStream_t)stream));
 }
 

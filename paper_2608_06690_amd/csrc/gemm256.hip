@@ -9,7 +9,7 @@
 //          backward's products with transposed weights).
 //   MX     GEMM1 and GEMM2 on 8-bit operands (mx.h): activations with block scales, weights with row
 //          scales, K steps of 128 values. Such a step has the bytes, the fragments and, on the
-//          scaled fp8 instruction, the matrix time of a bf16 step of 64, so the schedule is the same.
+//          scaled fp8 instruction, the matrix time of a bf16 step of 64; its schedule is below.
 //
 // Tile list: groups are the routed experts and the shared group; a tile is (group, M tile of
 // 256 rows, N tile). Every block scans the per-group tile counts on the device, so groups
@@ -46,6 +46,15 @@
 // two-stage ring drained at every step (the kernel before it): 16384-token layer 1,466 -> 1,345
 // us (1,315 with a reciprocal in place of silu's division), DeepSeek-V2-Lite-shaped 8192-token
 // layer 1,307 -> 1,240, Qwen3-30B-A3B-shaped 4096-token layer 558 -> 502.
+//
+// MX: a step of a tile with two A halves has two phases, an A half against both B halves (16 matrix
+// instructions each, 32 clocks an instruction): what a phase costs beyond them, the latency of its
+// fragment reads and two barriers, then comes half as often (16384 tokens of the Qwen3-30B-A3B-shaped
+// layer, both products: 857 us with four phases, 798 with two; 4096 tokens 303 -> 293). The reading wave
+// issues the copies (of all but A1). Timing builds of that batch: without copies 524 us, without stores
+// 603, without block scales 726, with all operands in L2 713, without MFMAs 747, without fragment reads
+// 799: copies, stores and scales each hold up the lock step of the two row groups, and the matrix
+// instructions are not what bounds it. 1.24 TFLOP in 790 us.
 #include "lds_dma.h"
 #include "mx.h"
 #include "pmpe_internal.h"
@@ -527,26 +536,20 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
     pin(blocks, acc);
   };
   auto mulc = [&](f32x4 (&acc)[4][2], const Frag (&fb)[2], auto&& copy) { mulc_mb(ic<4>, acc, fb, copy); };
-  // MX: an A half with both B halves; copies 0 .. NC - 1 are spread over it, two MFMAs to a slot
-  auto mul_half = [&](auto blocks, f32x4 (&acc0)[4][2], const Frag (&f0)[2], f32x4 (&acc1)[4][2], const Frag (&f1)[2], auto nc,
+  // MX: an A half with both B halves; two copies go after its first and its third quarter
+  auto mul_half = [&](auto blocks, f32x4 (&acc0)[4][2], const Frag (&f0)[2], f32x4 (&acc1)[4][2], const Frag (&f1)[2],
                       auto&& copy) {
-    constexpr int MB = decltype(blocks)::value, NC = decltype(nc)::value;
-    Unroll<0, 2 * MB>::run([&](auto slot) {
-      constexpr int mb = decltype(slot)::value / 2;
+    constexpr int MB = decltype(blocks)::value;
+    Unroll<0, MB>::run([&](auto mb) {
 #pragma unroll
-      for (int nb = 0; nb < 2; ++nb) {
-        if constexpr (decltype(slot)::value % 2 == 0)
-          acc0[mb][nb] = mfma(ic<0>, f0[nb], mb, acc0[mb][nb]);
-        else
-          acc1[mb][nb] = mfma(ic<0>, f1[nb], mb, acc1[mb][nb]);
+      for (int nb = 0; nb < 2; ++nb) acc0[mb.value][nb] = mfma(ic<0>, f0[nb], mb.value, acc0[mb.value][nb]);
+      if constexpr (MB == 4 && mb.value % 2 == 0) {
+        __builtin_amdgcn_sched_barrier(0);
+        copy(ic<mb.value / 2>);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      Unroll<0, NC>::run([&](auto c) {
-        if constexpr (decltype(c)::value * 2 * MB / NC == decltype(slot)::value) {
-          __builtin_amdgcn_sched_barrier(0);
-          copy(c);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      });
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) acc1[mb.value][nb] = mfma(ic<0>, f1[nb], mb.value, acc1[mb.value][nb]);
     });
     pin(blocks, acc0);
     pin(blocks, acc1);
@@ -672,7 +675,7 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
         else
           wait_vmcnt<0>();
         phase_mid();
-        mul_half(ic<4>, acc[0][0], fb0, acc[0][1], fb1, ic<2>, [&](auto c) { if (late) copyA1(h1, c, cbuf ^ STEP); });
+        mul_half(ic<4>, acc[0][0], fb0, acc[0][1], fb1, [&](auto c) { if (late) copyA1(h1, c, cbuf ^ STEP); });
         if (kind1) ++pk;
         phase_end();
 
@@ -693,18 +696,16 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
           else
             wait_copies(ic<0>, ic<AFTER2>, ic<S5>, fresh == 2);
         }
+        // the copies of the step after it: by the reading wave, which waits anyway (between the 16 MFMAs
+        // they hold those up: 808 against 790 us)
         kind2 = next_step();
+        if (kind2) {
+          copyA(h0, cbuf);
+          copyB(h0, cbuf);
+          copyB(h1, cbuf);
+        }
         phase_mid();
-        mul_half(blocks, acc[1][1], fb1, acc[1][0], fb0, ic<6>, [&](auto c) {
-          constexpr int C = decltype(c)::value;
-          if (!kind2) return;
-          if constexpr (C < 2)
-            copyA1(h0, ic<C>, cbuf);
-          else if constexpr (C < 4)
-            copyB1(h0, ic<C - 2>, cbuf);
-          else
-            copyB1(h1, ic<C - 4>, cbuf);
-        });
+        mul_half(blocks, acc[1][1], fb1, acc[1][0], fb0, [](auto) {});
         phase_end();
         late = kind2 == 2;
         if (last) {

@@ -30,6 +30,7 @@ class LayerBuffers:
     dev_status: torch.Tensor
     ab: Optional[torch.Tensor] = None   # [T*k, 2I] fp32, filled by a training forward
     topk_logit: Optional[torch.Tensor] = None  # [T*k] fp32, filled by routing with a score rule
+    ws_mx: Optional[torch.Tensor] = None       # workspace of the 8-bit experts
 
 
 @dataclasses.dataclass
@@ -257,10 +258,10 @@ class PolicyMaskedMoE:
         d8 = N.LayerDesc(*[getattr(self.desc, f) for f, _ in N.LayerDesc._fields_])
         d8.w_dtype = N.PMPE_FP8_E4M3
         ws_bytes = N.pmpe_expert_ffn_mx_workspace_bytes(d8, T)
-        if b.ws.numel() < ws_bytes:
-            b.ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+        if b.ws_mx is None:  # (a buffer of its own: b.ws may be in a captured pass)
+            b.ws_mx = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
         N.pmpe_expert_ffn_mx(d8, T, xq, xs, b.expert_count, b.expert_offset, b.row_token, *fp8, b.y_perm,
-                             audit.token_rows, audit.priv_calls, b.dev_status, b.ws, stream)
+                             audit.token_rows, audit.priv_calls, b.dev_status, b.ws_mx, stream)
         self.combine(x, b, stream)
         if req_offset is not None:
             self.audit(T, b, audit, req_offset, stream)
@@ -453,8 +454,8 @@ class PrivateAdamW:
     handed to the optimizer (they are not arguments of any call here).
 
     With max_norm the gradients of a step are clipped to that global norm; `norm` [2] then
-    holds the norm and the factor of the last step, and a step whose norm is not finite changes
-    nothing. Several layers are clipped together by step_clipped: their norm is taken over all
+    holds the norm and the factor of the last step, and a step whose norm is not finite leaves
+    parameters and states as they are (it counts in t). Several layers are clipped together by step_clipped: their norm is taken over all
     their gradients."""
 
     def __init__(self, layer: PolicyMaskedMoE, lr: float = 1e-4, betas=(0.9, 0.999),
@@ -468,7 +469,7 @@ class PrivateAdamW:
         self.m = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in self.params]
         self.v = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in self.params]
         self.t = 0
-        self.max_norm, self.norm, self._ws = max_norm, None, None
+        self.max_norm, self.norm, self._ws = max_norm, None, {}
 
     @staticmethod
     def _grads(g: GradBuffers):
@@ -498,14 +499,16 @@ def step_clipped(steps, max_norm: float, stream=None) -> torch.Tensor:
     and the factor they were multiplied with (kept by the first optimizer, overwritten by its
     next step)."""
     steps = list(steps)
+    if not steps or len({id(opt) for opt, _ in steps}) < len(steps):
+        raise ValueError("a step needs optimizers, each of them once")
     grads = N.GradList([t for opt, g in steps for t in opt._grads(g)])
     first = steps[0][0]
     need = N.pmpe_grad_norm_workspace_bytes(grads)
-    if first._ws is None or first._ws.numel() < need:
-        first._ws = torch.empty(need, dtype=torch.uint8, device=first.m[0].device)
+    if need not in first._ws:  # one per size, kept: a captured step may hold it
+        first._ws[need] = torch.empty(need, dtype=torch.uint8, device=first.m[0].device)
     if first.norm is None:
         first.norm = torch.empty(2, dtype=torch.float32, device=first.m[0].device)
-    N.pmpe_grad_norm(grads, max_norm, first.norm, first._ws, stream)
+    N.pmpe_grad_norm(grads, max_norm, first.norm, first._ws[need], stream)
     for opt, g in steps:
         opt.t += 1
         for p, mp, gr, m, v in zip(opt.params, opt.master, opt._grads(g), opt.m, opt.v):

@@ -177,6 +177,22 @@ def test_grad_norm_workspace():
     assert N.lib().pmpe_grad_norm_workspace_bytes(None, -1) == 0
 
 
+@pytest.mark.parametrize("ptrs,sizes,outs", [
+    ((A, A), (10, 5), None), ((A + 16, A), (10, 5), None), ((A, A + 36), (10, 5), None),   # a tensor twice; one inside the other
+    ((B, A, B + 4), (4, 4, 1), None), ((A, B), (10, 5), (D, D)), ((A, B), (10, 5), (D, D + 36)),
+    ((A, B), (10, 5), (E, E - 16)), ((A, B), (10, 5), (B, D)), ((A, B), (10, 5), (B + 16, D)),  # an output on another gradient
+    ((A, B), (10, 5), (D, A + 36)), ((B, A), (5, 10), (B, A + 4)), ((A, B, C), (9, 0, 9), (B, None, C - 4))])
+def test_clip_grads_refuses_outputs_that_overlap(ptrs, sizes, outs):
+    assert clip_grads(arrays(ptrs, sizes, (F32,) * len(ptrs)), outs) == SHAPE
+
+
+def test_a_clipped_step_takes_each_optimizer_once():
+    opt = object()
+    for steps in ([], [(opt, None), (opt, None)]):
+        with pytest.raises(ValueError):
+            P.step_clipped(steps, 1.0)
+
+
 def test_adamw_clipped():
     f = N.lib().pmpe_adamw_clipped
     hp = (1e-3, 0.9, 0.99, 1e-8, 0.0)

@@ -133,6 +133,19 @@ def test_refusals_of_the_binding():
         P.pmpe_grad_norm(g, 0.0, norm, torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
 
 
+def test_outputs_in_any_order_and_partly_in_place():
+    g = grads_of([1000, 0, 70, 9000, 5], torch.float32, 8)
+    g = [g[3], g[1], g[0], g[4], g[2]]
+    norm = norm_of(g, 0.1)
+    want = [t.double() * float(norm[1]) for t in g]
+    to = torch.full((10020,), 9.0, device="cuda")
+    outs = [to[10:9010], to[:0], g[2], to[9010:9015], to[9015:9085]]
+    P.pmpe_clip_grads(g, outs, norm)
+    for o, w in zip(outs, want):
+        assert torch.all((o.double() - w).abs() <= 2.0 ** -23 * w.abs())
+    assert torch.all(to[:10] == 9.0) and torch.all(to[9085:] == 9.0)
+
+
 HP = dict(lr=1e-2, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1)
 
 
