@@ -371,11 +371,12 @@ hipError_t launch(const MxFfnArgs& a, hipStream_t s) {
 hipError_t launch_expert_ffn_mx(const MxFfnArgs& a, hipStream_t s) {
   // Rows per expert, on average, choose the tile; us of both products (160 experts of 2048 x 768 / 52 of
   // 1664 x 640 / 80 of 2048 x 1408), all experts alike:
-  //   rows                 32            48            56            64            96            128           192           384
-  //   64 x 128     149  51 130   163  53 148   186  55 161   237  67 206   315  81 281   356  90 315   510 120 452   870 188 740
-  //   128 x 256    165  61 151   173  63 157   177  65 160   180  66 162   195  73 176   248  81 217   299  93 248   496 133 407
-  //   256 x 256    193  80 180   199  80 184   203  82 186   205  84 188   217  87 197   228  95 209   263 111 247   474 154 397
-  // The large kernel needs a few tiles per CU (the 52 experts give it one or two), and two K steps.
+  //   rows                 48            56            64            96            128           192           384
+  //   64 x 128     163  53 148   186  55 161   237  67 206   315  81 281   356  90 315   510 120 452   870 188 740
+  //   128 x 256    171  63 153   174  65 156   178  62 160   196  69 177   251  78 224   317  92 271   540 136 446
+  //   256 x 256    196  80 180   202  82 183   202  79 187   220  83 198   227  91 211   266 101 243   449 137 372
+  // (32 rows: 149, 51, 130 and 165, 61, 148 with the two smaller.) The large kernel needs a few tiles per
+  // CU (the 52 experts give it one or two), and two K steps.
   const int64_t E = a.n_pub + a.n_priv, rows = (int64_t)a.T * a.k / E;
   hipError_t e;
   if (rows < 52) {
