@@ -196,6 +196,37 @@ def test_missing_private_weights(T):
     assert torch.all(rows == 0) and torch.all(calls == 0) and status == P._native.PMPE_DEV_PRIV_WEIGHTS_MISSING
 
 
+# Batches of the 256 x 256 kernel (768 of its tiles and more, 120 rows per expert): tiles of every number of
+# rows, two K steps, a last tile of half the width, three steps, experts of many tiles
+LARGE = [(2900, 256, 256, 256, 128, 16), (2900, 384, 256, 256, 128, 16), (4800, 1280, 384, 128, 128, 16), (9000, 256, 2048, 8, 4, 4)]
+
+
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+@pytest.mark.parametrize("allow,hot", [(0.5, None), (0.05, None), (1.0, None), (0.4, 3)])
+def test_large_batches(shape, allow, hot):
+    log(f"mx {shape} allow={allow} hot={hot}")
+    c = Case(*shape, seed=5, allow=allow, hot=hot)
+    got, rows, calls, status = c.run()
+    check(c, got, *c.exact())
+    priv = torch.zeros_like(rows)
+    at = int(c.off[c.n])
+    priv.index_add_(0, c.rt[at:].long(), torch.ones_like(c.rt[at:]))
+    assert torch.equal(rows, priv) and torch.equal(calls, (c.count[c.n:] > 0).int()) and status == 0
+    for _ in range(3):
+        assert torch.equal(got, c.run()[0])
+
+
+@pytest.mark.parametrize("shape", LARGE, ids=str)
+def test_large_batches_without_private_weights(shape):
+    log(f"mx {shape} without private weights")
+    c = Case(*shape, seed=6)
+    full = c.run()[0]
+    y, rows, calls, status = c.run(private=False)
+    at = int(c.off[c.n])
+    assert torch.equal(y[:at], full[:at]) and torch.all(y[at:] == 0)
+    assert torch.all(rows == 0) and torch.all(calls == 0) and status == P._native.PMPE_DEV_PRIV_WEIGHTS_MISSING
+
+
 def test_values_that_are_not_finite():
     c = Case(600, 256, 128, 8, 4, 2, seed=4)
     want = c.run()[0]
