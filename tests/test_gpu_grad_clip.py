@@ -115,6 +115,24 @@ def test_empty_lists_and_values_that_are_not_finite():
     assert norm_of(g, 1.0).isnan().all()
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_tensors_of_more_than_2_31_elements(dt):
+    n = (1 << 31) + 8195
+    g = torch.zeros(n, dtype=dt, device="cuda")
+    at = torch.tensor([0, 4095, (1 << 31) - 1, 1 << 31, (1 << 31) + 4096, n - 1], device="cuda")
+    g[at] = torch.tensor([1.0, 2.0, 4.0, 8.0, 16.0, 32.0], dtype=dt, device="cuda")
+    g = [torch.ones(3, dtype=dt, device="cuda"), g]
+    norm = norm_of(g, 0.5)
+    total = math.sqrt(3 + 1365)
+    assert abs(float(norm[0]) - total) <= U * total
+    P.pmpe_clip_grads(g, None, norm)
+    want = torch.tensor([1.0, 2.0, 4.0, 8.0, 16.0, 32.0], device="cuda").double() * (0.5 / (total + 1e-6))
+    step = (2.0 ** -8 if dt == torch.bfloat16 else 2.0 ** -24) + U
+    assert torch.all((g[1][at].double() - want).abs() <= step * want)
+    g[1][at] = 0
+    assert not g[1].any()
+
+
 def test_refusals_of_the_binding():
     g, norm = grads_of([10, 20], torch.float32, 6), torch.ones(2, device="cuda")
     for outs in (g[:1], [g[0], g[1][:19]], [g[0], g[1].bfloat16()]):

@@ -194,6 +194,33 @@ def test_backward_against_differences():
     assert abs(got - float((dw.double() * e.double()).sum())) <= size * 2.0 ** -18 / h  # linear in w
 
 
+def test_rows_beyond_2_31_elements():
+    """The last rows of a batch whose offsets pass 32 bits: the bits that the rows alone give."""
+    T, H, n = 131080, 16384, 3
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.empty(T, H, dtype=torch.bfloat16, device="cuda").normal_(0.0, 1.0, generator=g)
+    w = torch.empty(H, device="cuda").normal_(1.0, 0.1, generator=g)
+
+    def forward(x, out):
+        q = torch.zeros(x.shape, dtype=torch.uint8, device="cuda")
+        s = torch.zeros(x.shape[0], H // 32, dtype=torch.uint8, device="cuda")
+        rstd = torch.zeros(x.shape[0], device="cuda")
+        P.pmpe_rmsnorm(x, None, w, 1e-6, None, out, q, s, rstd)
+        return q, s, rstd
+
+    last = x[-n:].clone()
+    y = torch.empty_like(last)
+    q, s, rstd = forward(last, y)
+    dx = torch.empty_like(last)
+    P.pmpe_rmsnorm_backward(y, None, last, w, rstd, dx, None, None)
+    out = torch.empty_like(x)
+    all_q, all_s, all_rstd = forward(x, out)
+    assert torch.equal(out[-n:], y) and torch.equal(all_q[-n:], q) and torch.equal(all_s[-n:], s)
+    assert torch.equal(all_rstd[-n:], rstd)
+    P.pmpe_rmsnorm_backward(out, None, x, w, all_rstd, out, None, None)
+    assert torch.equal(out[-n:], dx)
+
+
 def test_empty_batch_and_graph():
     w, dw = torch.ones(64, device="cuda"), torch.full((64,), 3.0, device="cuda")
     e = torch.empty(0, 64, device="cuda")
