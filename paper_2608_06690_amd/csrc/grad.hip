@@ -7,12 +7,13 @@
 // fp32 size; fp64 runs at the rate of scalar fp32, far below the memory time). The tensors are cut
 // into chunks; a block adds every gridDim-th chunk and a last block the blocks' sums, all in a fixed
 // order, so equal gradients give equal bits. The list travels by value, as many pieces of at most 2^31
-// elements to a launch as the 4 KB of a kernel's arguments hold. A block finds the piece of a chunk by
-// reading all of them, one load per lane and 64 of them, and comparing: one latency, where a search of
-// the list waits for eight. The norm of 604 MB of fp32 takes 102 us (5.9 TB/s). Norm and clipping of 500
-// bf16 tensors of up to 200000 elements take 42 us, 34 of them eight launches that cannot overlap: 112 us
-// with 96 tensors to a launch and the last chunk of each tensor read element by element. Chunks of 4096
-// and 8192 elements are equal on large tensors; the smaller ones fill the card with less (42 and 44 us).
+// elements to a launch as the 4 KB of a kernel's arguments hold: 256, or 160 where gradients and outputs
+// lie apart in different orders. A block finds the piece of a chunk by reading all of them, one load per
+// lane and 64 of them, and comparing: one latency, where a search of the list waits for eight. The norm of
+// 604 MB of fp32 takes 102 us (5.9 TB/s). Norm and clipping of 500 bf16 tensors of up to 200000 elements
+// take 28 us in five launches that cannot overlap (35 when a call took 2.5 us more of host time); 112 with 96
+// tensors to a launch and the last chunk of each tensor read element by element. Chunks of 4096 and 8192 elements are equal on large tensors; the
+// smaller ones fill the card with less.
 #include <algorithm>
 
 #include "pmpe_internal.h"
@@ -26,25 +27,23 @@ typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 constexpr int GR_THREADS = 256;
 constexpr int GR_CHUNK = 4096;  // elements: two vectors of 8 per thread
 
-// A piece of a gradient: `first` is its first chunk among those of the launch. Bit 63 of src: bf16.
+// Pieces of gradients. Bit 63 of src: bf16. Piece i has the launch's chunks first[i] .. first[i + 1] - 1, and
+// tail[i] elements in the last of them. DST: its output is at dst[i]; without, all of them lie at the distance
+// dst[0] of their gradients (0: in place), and more pieces fit.
 constexpr uint64_t GR_BF16 = (uint64_t)1 << 63;
-struct NormPiece {
-  uint64_t src;
-  uint32_t n, first;
-};
-struct ScalePiece {
-  uint64_t src, dst;
-  uint32_t n, first;
-};
-template <class P, int COUNT>
+template <int COUNT, bool DST_>
 struct GradTable {
   static constexpr int SIZE = COUNT;
-  P e[COUNT];
-  uint32_t count, chunks;
+  static constexpr bool DST = DST_;
+  uint64_t src[COUNT];
+  uint64_t dst[DST ? COUNT : 1];
+  uint32_t first[COUNT + 1];
+  uint16_t tail[COUNT];
+  uint32_t count;
 };
 // 3.6 KB each
-typedef GradTable<NormPiece, GRAD_LIST> NormTable;
-typedef GradTable<ScalePiece, 152> ScaleTable;
+typedef GradTable<GRAD_LIST, false> NearTable;
+typedef GradTable<160, true> FarTable;
 
 __device__ __forceinline__ double wave_add(double v) {
 #pragma unroll
@@ -69,8 +68,13 @@ __device__ __forceinline__ void read_firsts(const T& t, uint32_t (&first)[(T::SI
 #pragma unroll
   for (int r = 0; r < (T::SIZE + 63) / 64; ++r) {
     const uint32_t i = r * 64 + lane_id();
-    first[r] = i < t.count ? t.e[i].first : ~0u;
+    first[r] = i < t.count ? t.first[i] : ~0u;
   }
+}
+// elements of piece i
+template <class T>
+__device__ __forceinline__ uint32_t elements_of(const T& t, int i) {
+  return (t.first[i + 1] - t.first[i] - 1) * GR_CHUNK + t.tail[i];
 }
 // last piece whose first chunk is at or before c
 template <int R>
@@ -142,16 +146,18 @@ __device__ __forceinline__ double chunk_squares(const void* p, uint32_t e0, uint
 }
 
 template <bool STREAM>
-__global__ __launch_bounds__(GR_THREADS) void grad_squares_kernel(NormTable t, double* part) {
+__global__ __launch_bounds__(GR_THREADS) void grad_squares_kernel(NearTable t, double* part) {
   __shared__ double s[GR_THREADS / 64];
   double acc = 0.0;
-  uint32_t first[(NormTable::SIZE + 63) / 64];
+  uint32_t first[(NearTable::SIZE + 63) / 64];
   read_firsts(t, first);
-  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    const NormPiece& e = t.e[piece_of(first, c)];
-    const uint32_t e0 = (c - e.first) * GR_CHUNK;
-    const void* src = (const void*)(e.src & ~GR_BF16);
-    acc += (e.src & GR_BF16) ? chunk_squares<true, STREAM>(src, e0, e.n) : chunk_squares<false, STREAM>(src, e0, e.n);
+  const uint32_t chunks = t.first[t.count];
+  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    const int i = piece_of(first, c);
+    const uint64_t p = t.src[i];
+    const uint32_t e0 = (c - t.first[i]) * GR_CHUNK, n = elements_of(t, i);
+    const void* src = (const void*)(p & ~GR_BF16);
+    acc += (p & GR_BF16) ? chunk_squares<true, STREAM>(src, e0, n) : chunk_squares<false, STREAM>(src, e0, n);
   }
   acc = block_add<GR_THREADS>(acc, s);
   if (threadIdx.x == 0) part[blockIdx.x] = acc;
@@ -209,20 +215,21 @@ __device__ __forceinline__ void chunk_scale(const void* p, void* o, uint32_t e0,
   }
 }
 
-__global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(ScaleTable t, const float* norm) {
+template <class T>
+__global__ __launch_bounds__(GR_THREADS) void grad_scale_kernel(T t, const float* norm) {
   const float coef = norm[1];
-  uint32_t first[(ScaleTable::SIZE + 63) / 64];
+  uint32_t first[(T::SIZE + 63) / 64];
   read_firsts(t, first);
-  for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    const ScalePiece& e = t.e[piece_of(first, c)];
-    const void* src = (const void*)(e.src & ~GR_BF16);
-    void* dst = (void*)e.dst;
-    if (coef == 1.0f && dst == src) continue;  // in place and inside the bound: nothing changes
-    const uint32_t e0 = (c - e.first) * GR_CHUNK;
-    if (e.src & GR_BF16)
-      chunk_scale<true>(src, dst, e0, e.n, coef);
+  const uint32_t chunks = t.first[t.count];
+  for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+    const int i = piece_of(first, c);
+    const uint64_t p = t.src[i], q = p & ~GR_BF16, o = T::DST ? t.dst[T::DST ? i : 0] : q + t.dst[0];
+    if (coef == 1.0f && o == q) continue;  // in place and inside the bound: nothing changes
+    const uint32_t e0 = (c - t.first[i]) * GR_CHUNK, n = elements_of(t, i);
+    if (p & GR_BF16)
+      chunk_scale<true>((const void*)q, (void*)o, e0, n, coef);
     else
-      chunk_scale<false>(src, dst, e0, e.n, coef);
+      chunk_scale<false>((const void*)q, (void*)o, e0, n, coef);
   }
 }
 
@@ -233,17 +240,16 @@ class Tables {
   explicit Tables(const GradListArgs& a) : a_(a) {}
   // false: no piece is left
   bool next(T* t) {
-    t->count = t->chunks = 0;
+    t->count = 0;
+    t->first[0] = 0;
     while (at_ < a_.count && t->count < (uint32_t)T::SIZE) {
       const uint64_t n = std::min(a_.n[at_] - done_, GRAD_PIECE), el = a_.dtype[at_] == PMPE_BF16 ? 2 : 4;
       if (n > 0) {
-        auto& e = t->e[t->count++];
-        e.src = ((uint64_t)(uintptr_t)a_.src[at_] + done_ * el) | (el == 2 ? GR_BF16 : 0);
-        if constexpr (sizeof(e) == sizeof(ScalePiece))
-          e.dst = (uint64_t)(uintptr_t)(a_.dst ? a_.dst[at_] : a_.src[at_]) + done_ * el;
-        e.n = (uint32_t)n;
-        e.first = t->chunks;
-        t->chunks += (uint32_t)((n + GR_CHUNK - 1) / GR_CHUNK);
+        const uint32_t i = t->count++;
+        t->src[i] = ((uint64_t)(uintptr_t)a_.src[at_] + done_ * el) | (el == 2 ? GR_BF16 : 0);
+        if constexpr (T::DST) t->dst[i] = (uint64_t)(uintptr_t)a_.dst[at_] + done_ * el;
+        t->first[i + 1] = t->first[i] + (uint32_t)((n + GR_CHUNK - 1) / GR_CHUNK);
+        t->tail[i] = (uint16_t)((n - 1) % GR_CHUNK + 1);
       }
       done_ += n;
       if (done_ == a_.n[at_]) {
@@ -270,10 +276,11 @@ hipError_t launch_grad_norm(const GradListArgs& a, double max_norm, float* norm,
   for (int i = 0; i < a.count; ++i) bytes += a.n[i] * (a.dtype[i] == PMPE_BF16 ? 2 : 4);
   const auto kernel = bytes >= ((uint64_t)128 << 20) ? grad_squares_kernel<true> : grad_squares_kernel<false>;
   int parts = 0;
-  Tables<NormTable> list(a);
-  NormTable t;
+  Tables<NearTable> list(a);
+  NearTable t;
+  t.dst[0] = 0;
   while (list.next(&t)) {
-    const int grid = (int)std::min<uint32_t>(t.chunks, GRAD_BLOCKS);
+    const int grid = (int)std::min<uint32_t>(t.first[t.count], GRAD_BLOCKS);
     kernel<<<grid, GR_THREADS, 0, s>>>(t, part + parts);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -283,15 +290,39 @@ hipError_t launch_grad_norm(const GradListArgs& a, double max_norm, float* norm,
   return hipGetLastError();
 }
 
-hipError_t launch_clip_grads(const GradListArgs& a, const float* norm, hipStream_t s) {
-  Tables<ScaleTable> list(a);
-  ScaleTable t;
+namespace {
+
+template <class T>
+hipError_t scale_all(const GradListArgs& a, T& t, const float* norm, hipStream_t s) {
+  Tables<T> list(a);
   while (list.next(&t)) {
-    grad_scale_kernel<<<std::min<uint32_t>(t.chunks, 16384), GR_THREADS, 0, s>>>(t, norm);
+    grad_scale_kernel<T><<<std::min<uint32_t>(t.first[t.count], 16384), GR_THREADS, 0, s>>>(t, norm);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_clip_grads(const GradListArgs& a, const float* norm, hipStream_t s) {
+  // one distance from every gradient to its output (in place, or both lists laid out alike)?
+  bool any = false, near = true;
+  uint64_t dist = 0;
+  for (int i = 0; a.dst && near && i < a.count; ++i) {
+    if (a.n[i] == 0) continue;
+    const uint64_t d = (uint64_t)(uintptr_t)a.dst[i] - (uint64_t)(uintptr_t)a.src[i];
+    near = !any || d == dist;
+    dist = d;
+    any = true;
+  }
+  if (near) {
+    NearTable t;
+    t.dst[0] = dist;
+    return scale_all(a, t, norm, s);
+  }
+  FarTable t;
+  return scale_all(a, t, norm, s);
 }
 
 }  // namespace pmpe

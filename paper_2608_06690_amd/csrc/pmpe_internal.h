@@ -468,7 +468,7 @@ struct GradListArgs {
   const int32_t* dtype;
   int count;
 };
-constexpr int GRAD_LIST = 224;     // pieces of a launch of the norm
+constexpr int GRAD_LIST = 256;     // pieces of a launch of the norm
 constexpr int GRAD_BLOCKS = 2048;  // blocks of a launch of the norm
 constexpr uint64_t GRAD_PIECE = (uint64_t)1 << 31;  // elements of a piece at most
 // part: GRAD_BLOCKS doubles per launch
