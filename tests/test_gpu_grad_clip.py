@@ -115,6 +115,20 @@ def test_empty_lists_and_values_that_are_not_finite():
     assert norm_of(g, 1.0).isnan().all()
 
 
+@pytest.mark.parametrize("count", [160, 161, 700])
+def test_many_outputs_in_another_order(count):
+    grads = grads_of([1 + (37 * i) % 9001 for i in range(count)], torch.bfloat16, 10)
+    back = torch.empty(sum(t.numel() for t in grads), dtype=torch.bfloat16, device="cuda")
+    outs = list(back.split([t.numel() for t in grads[::-1]]))[::-1]
+    norm = norm_of(grads, 0.1)
+    n, coef = exact(grads, 0.1)
+    assert abs(float(norm[0]) - n) <= U * n
+    P.pmpe_clip_grads(grads, outs, norm)
+    for o, t in zip(outs, grads):
+        w = t.double() * coef
+        assert torch.all((o.double() - w).abs() <= (2.0 ** -8 + U) * w.abs())
+
+
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 def test_tensors_of_more_than_2_31_elements(dt):
     n = (1 << 31) + 8195
