@@ -385,6 +385,7 @@ class BlockBuffers:
     norm_q: Optional[torch.Tensor] = None      # [T, H] uint8 and [T, H / 32] uint8: the norm in 8 bits
     norm_scale: Optional[torch.Tensor] = None
     total: Optional[torch.Tensor] = None       # the buffer of h + delta
+    ws: Optional[torch.Tensor] = None          # workspace of a backward with a dweight
 
 
 class NormedMoE:
@@ -441,10 +442,10 @@ class NormedMoE:
         activation type) and, if given, dweight [H] fp32; returns the layer's gradients."""
         g = self.layer.backward(b.norm, dout, b.layer, g, stream)
         T, H = b.norm.shape
-        ws = None
-        if dweight is not None:
-            ws = torch.empty(N.pmpe_rmsnorm_backward_workspace_bytes(T, H), dtype=torch.uint8, device=b.norm.device)
-        N.pmpe_rmsnorm_backward(g.dx, dresidual, b.residual, self.weight, b.rstd, dx, dweight, ws, stream)
+        if dweight is not None and b.ws is None:  # (kept: kernels on `stream` use it when this call has returned)
+            b.ws = torch.empty(N.pmpe_rmsnorm_backward_workspace_bytes(T, H), dtype=torch.uint8, device=b.norm.device)
+        N.pmpe_rmsnorm_backward(g.dx, dresidual, b.residual, self.weight, b.rstd, dx, dweight,
+                                None if dweight is None else b.ws, stream)
         return g
 
 
