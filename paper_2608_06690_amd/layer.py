@@ -456,8 +456,9 @@ class PrivateAdamW:
 
     With max_norm the gradients of a step are clipped to that global norm; `norm` [2] then
     holds the norm and the factor of the last step, and a step whose norm is not finite leaves
-    parameters and states as they are (it counts in t). Several layers are clipped together by step_clipped: their norm is taken over all
-    their gradients."""
+    parameters and states as they are (it counts in t). Several layers are clipped together by
+    step_clipped: their norm is taken over all their gradients, and `norm` of each is that one
+    until its next step."""
 
     def __init__(self, layer: PolicyMaskedMoE, lr: float = 1e-4, betas=(0.9, 0.999),
                  eps: float = 1e-8, weight_decay: float = 0.0, max_norm: Optional[float] = None):
@@ -470,7 +471,7 @@ class PrivateAdamW:
         self.m = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in self.params]
         self.v = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in self.params]
         self.t = 0
-        self.max_norm, self.norm, self._ws = max_norm, None, {}
+        self.max_norm, self.norm, self._ws, self._norms = max_norm, None, {}, {}
 
     @staticmethod
     def _grads(g: GradBuffers):
@@ -497,8 +498,8 @@ class PrivateAdamW:
 def step_clipped(steps, max_norm: float, stream=None) -> torch.Tensor:
     """One optimizer step of several layers whose gradients are clipped together: steps are pairs
     (PrivateAdamW, GradBuffers). Returns norm [2]: the global norm of all their private gradients
-    and the factor they were multiplied with (kept by the first optimizer, overwritten by its
-    next step)."""
+    and the factor they were multiplied with (kept by the first optimizer, overwritten by the next step
+    of these optimizers in this order)."""
     steps = list(steps)
     if not steps or len({id(opt) for opt, _ in steps}) < len(steps):
         raise ValueError("a step needs optimizers, each of them once")
@@ -507,14 +508,18 @@ def step_clipped(steps, max_norm: float, stream=None) -> torch.Tensor:
     need = N.pmpe_grad_norm_workspace_bytes(grads)
     if need not in first._ws:  # one per size, kept: a captured step may hold it
         first._ws[need] = torch.empty(need, dtype=torch.uint8, device=first.m[0].device)
-    if first.norm is None:
-        first.norm = torch.empty(2, dtype=torch.float32, device=first.m[0].device)
-    N.pmpe_grad_norm(grads, max_norm, first.norm, first._ws[need], stream)
+    # one norm per company of optimizers: a step of some of them, or with others, leaves it to those whose last
+    # step it was
+    who = tuple(id(opt) for opt, _ in steps)
+    if who not in first._norms:
+        first._norms[who] = torch.empty(2, dtype=torch.float32, device=first.m[0].device)
+    norm = first._norms[who]
+    N.pmpe_grad_norm(grads, max_norm, norm, first._ws[need], stream)
     for opt, g in steps:
         opt.t += 1
         for p, mp, gr, m, v in zip(opt.params, opt.master, opt._grads(g), opt.m, opt.v):
             N.pmpe_adamw_clipped(p, mp, gr, m, v, opt.t, opt.lr, opt.betas[0], opt.betas[1], opt.eps, opt.wd,
-                                 first.norm, stream)
-        opt.norm = first.norm
+                                 norm, stream)
+        opt.norm = norm
         opt._follow(stream)
-    return first.norm
+    return norm

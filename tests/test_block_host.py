@@ -40,3 +40,56 @@ def test_the_workspace_of_a_backward_outlives_it(monkeypatch):
     assert none is None and no_dw is None  # a frozen norm needs none
     assert first() is not None and again() is first() and at2 == at
     assert first().numel() >= P.pmpe_rmsnorm_backward_workspace_bytes(8, H)
+
+
+def grads_of(lay, value):
+    like = lambda p: torch.full(p.shape, value, dtype=torch.float32)  # noqa: E731
+    return Lmod.GradBuffers(None, like(lay.w13_priv), like(lay.w2_priv), like(lay.wr_priv), None, None)
+
+
+def total_of(*grads):
+    return sum(float(t.double().square().sum()) for g in grads for t in (g.dwr_priv, g.dw13_priv, g.dw2_priv)) ** 0.5
+
+
+def test_every_optimizer_shows_the_norm_of_its_own_last_step(monkeypatch):
+    """Joint steps of several optimizers, in changing company, and single ones: `norm` is that of the
+    optimizer's last step, and the factor that a step reads is written by that step only."""
+    used = []
+
+    def grad_norm(grads, max_norm, norm, ws, stream):
+        n = sum(float(t.double().square().sum()) for t in grads.tensors) ** 0.5
+        norm.copy_(torch.tensor([n, min(1.0, max_norm / (n + 1e-6))]))
+
+    monkeypatch.setattr(N, "pmpe_grad_norm", grad_norm)
+    monkeypatch.setattr(N, "pmpe_adamw_clipped", lambda *a: used.append(a[-2]))
+    lays = [make_layer() for _ in range(3)]
+    a, b, c = [P.PrivateAdamW(lay, max_norm=0.5) for lay in lays]
+    ga, gb, gc_ = [grads_of(lay, v) for lay, v in zip(lays, (1.0, 2.0, 4.0))]
+    expected = {}
+
+    def check():
+        for opt, n in expected.items():
+            assert abs(float(opt.norm[0]) - n) <= 2.0 ** -22 * n
+
+    def joint(*pairs):
+        norm = P.step_clipped(pairs, 0.5)
+        n = total_of(*[g for _, g in pairs])
+        assert abs(float(norm[0]) - n) <= 2.0 ** -22 * n and all(u is norm for u in used[-3 * len(pairs):])
+        expected.update({opt: n for opt, _ in pairs})
+        check()
+        return norm
+
+    def single(opt, g):
+        opt.step(g)
+        assert all(u is opt.norm for u in used[-3:])
+        expected[opt] = total_of(g)
+        check()
+
+    first = joint((a, ga), (b, gb))
+    single(b, gb)   # leaves the joint step's norm to a
+    single(a, ga)
+    assert joint((a, ga), (b, gb)) is first  # the same tensors each time: a captured step may hold them
+    joint((a, ga), (c, gc_))                 # a steps with others: b's last step stays b's
+    joint((b, gb), (a, ga))
+    single(c, gc_)
+    single(a, ga)
