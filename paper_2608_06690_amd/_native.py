@@ -356,20 +356,6 @@ def pmpe_backward(desc, T, x, dout, topk_idx, topk_gate, expert_count, expert_of
         0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "pmpe_backward")
 
 
-def pmpe_backward_scored(desc, rule, T, topk_logit, x, dout, topk_idx, topk_gate, expert_count, expert_offset,
-                         row_token, token_row, y_perm, wr_pub, wr_priv, w13_pub, w2_pub, w13_priv, w2_priv,
-                         logit_bias, w13_sh, w2_sh, w2t_pub, w13t_pub, w2t_priv, w13t_priv, ab, dx, dw13_priv,
-                         dw2_priv, dwr_priv, grad_rows, ws, stream=None) -> None:
-    """pmpe_backward of a layer that routed by `rule` (pmpe_route_scored)."""
-    _check(_lib.pmpe_backward_scored(
-                ctypes.byref(desc), ctypes.byref(rule), T, _ptr(topk_logit), _ptr(x), _ptr(dout), _ptr(topk_idx),
-        _ptr(topk_gate), _ptr(expert_count), _ptr(expert_offset), _ptr(row_token), _ptr(token_row), _ptr(y_perm),
-        _ptr(wr_pub), _ptr(wr_priv), _ptr(w13_pub), _ptr(w2_pub), _ptr(w13_priv), _ptr(w2_priv), _ptr(logit_bias),
-        _ptr(w13_sh), _ptr(w2_sh), _ptr(w2t_pub), _ptr(w13t_pub), _ptr(w2t_priv), _ptr(w13t_priv), _ptr(ab),
-        _ptr(dx), _ptr(dw13_priv), _ptr(dw2_priv), _ptr(dwr_priv), _ptr(grad_rows), _ptr(ws),
-        0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "pmpe_backward_scored")
-
-
 def pmpe_fingerprint_workspace_bytes(nbytes: int) -> int:
     return int(_lib.pmpe_fingerprint_workspace_bytes(nbytes))
 
@@ -566,11 +552,41 @@ def pmpe_select_backward(desc, rule, T, logits, topk_idx, dgate, dlogits, stream
 def pmpe_route_scored(desc, rule, T, x, wr_pub, wr_priv, logit_bias, select_bias, policy_word, topk_idx, topk_gate,
                       topk_logit, allow, margin, dev_status, ws, stream=None) -> None:
     """pmpe_route with the selection and gates of a score rule."""
-    _check(_lib.pmpe_route_scored(ctypes.byref(desc), ctypes.byref(rule), T, _ptr(x), _ptr(wr_pub), _ptr(wr_priv),
-                                  _ptr(logit_bias), _ptr(select_bias), _ptr(policy_word), _ptr(topk_idx),
-                                  _ptr(topk_gate), _ptr(topk_logit), _ptr(allow), _ptr(margin), _ptr(dev_status), _ptr(ws),
-                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
-           "pmpe_route_scored")
+    dev, H, P, n = _here(x, "x"), desc.hidden, desc.n_priv, T * desc.top_k
+    E = desc.n_pub + P
+    _check(_lib.pmpe_route_scored(
+        ctypes.byref(desc), ctypes.byref(rule), T, _arg_n(x, "x", T * H, _BF16 if desc.act_dtype == PMPE_BF16 else _F32, dev),
+        _arg_n(wr_pub, "wr_pub", desc.n_pub * H, _F32, dev), _arg_n(wr_priv, "wr_priv", P * H, _F32, dev),
+        _arg_n(logit_bias, "logit_bias", E, _F32, dev), _arg_n(select_bias, "select_bias", E, _F32, dev),
+        _arg_n(policy_word, "policy_word", T, _WORDS, dev), _arg_n(topk_idx, "topk_idx", n, _I32T, dev),
+        _arg_n(topk_gate, "topk_gate", n, _F32, dev), _arg_n(topk_logit, "topk_logit", n, _F32, dev),
+        _arg_n(allow, "allow", T, _U8, dev), _arg_n(margin, "margin", T, _F32, dev),
+        _arg_n(dev_status, "dev_status", 1, _WORDS, dev), *_work(ws, dev), _stream(stream)), "pmpe_route_scored")
+
+
+def pmpe_backward_scored(desc, rule, T, topk_logit, x, dout, topk_idx, topk_gate, expert_count, expert_offset,
+                         row_token, token_row, y_perm, wr_pub, wr_priv, w13_pub, w2_pub, w13_priv, w2_priv,
+                         logit_bias, w13_sh, w2_sh, w2t_pub, w13t_pub, w2t_priv, w13t_priv, ab, dx, dw13_priv,
+                         dw2_priv, dwr_priv, grad_rows, ws, stream=None) -> None:
+    """pmpe_backward of a layer that routed by `rule` (pmpe_route_scored)."""
+    dev, H, I, N, P, n = _here(x, "x"), desc.hidden, desc.inter, desc.n_pub, desc.n_priv, T * desc.top_k
+    E, S = N + P, desc.n_shared * desc.shared_inter
+    _check(_lib.pmpe_backward_scored(
+        ctypes.byref(desc), ctypes.byref(rule), T, _arg_n(topk_logit, "topk_logit", n, _F32, dev),
+        _arg_n(x, "x", T * H, _BF16, dev), _arg_n(dout, "dout", T * H, _BF16, dev), _arg_n(topk_idx, "topk_idx", n, _I32T, dev),
+        _arg_n(topk_gate, "topk_gate", n, _F32, dev), _arg_n(expert_count, "expert_count", E, _I32T, dev),
+        _arg_n(expert_offset, "expert_offset", E + 1, _I32T, dev), _arg_n(row_token, "row_token", n, _I32T, dev),
+        _arg_n(token_row, "token_row", n, _I32T, dev), _arg_n(y_perm, "y_perm", n * H, _BF16, dev),
+        _arg_n(wr_pub, "wr_pub", N * H, _F32, dev), _arg_n(wr_priv, "wr_priv", P * H, _F32, dev),
+        _arg_n(w13_pub, "w13_pub", N * 2 * I * H, _BF16, dev), _arg_n(w2_pub, "w2_pub", N * H * I, _BF16, dev),
+        _arg_n(w13_priv, "w13_priv", P * 2 * I * H, _BF16, dev), _arg_n(w2_priv, "w2_priv", P * H * I, _BF16, dev),
+        _arg_n(logit_bias, "logit_bias", E, _F32, dev), _arg_n(w13_sh, "w13_sh", 2 * S * H, _BF16, dev),
+        _arg_n(w2_sh, "w2_sh", H * S, _BF16, dev), _arg_n(w2t_pub, "w2t_pub", N * I * H, _BF16, dev),
+        _arg_n(w13t_pub, "w13t_pub", N * H * 2 * I, _BF16, dev), _arg_n(w2t_priv, "w2t_priv", P * I * H, _BF16, dev),
+        _arg_n(w13t_priv, "w13t_priv", P * H * 2 * I, _BF16, dev), _arg_n(ab, "ab", n * 2 * I, _F32, dev),
+        _arg_n(dx, "dx", T * H, _F32, dev), _arg_n(dw13_priv, "dw13_priv", P * 2 * I * H, _F32, dev),
+        _arg_n(dw2_priv, "dw2_priv", P * H * I, _F32, dev), _arg_n(dwr_priv, "dwr_priv", P * H, _F32, dev),
+        _arg_n(grad_rows, "grad_rows", P, _WORDS, dev), *_work(ws, dev), _stream(stream)), "pmpe_backward_scored")
 
 
 class GradList:

@@ -96,6 +96,9 @@ class PolicyMaskedMoE:
         self.gather_in_dispatch = gather_in_dispatch
         if select_bias is not None and rule is None:
             raise ValueError("select_bias needs a score rule")
+        if select_bias is not None and (select_bias.dtype != torch.float32 or select_bias.device != wr_pub.device
+                                        or select_bias.shape != (desc.n_pub + desc.n_priv,) or not select_bias.is_contiguous()):
+            raise ValueError(f"select_bias must be {desc.n_pub + desc.n_priv} contiguous float32 values on {wr_pub.device}")
         self.rule, self.select_bias = rule, select_bias
         self._bufs = {}
 

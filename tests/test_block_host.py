@@ -4,6 +4,7 @@ import gc
 import types
 import weakref
 
+import pytest
 import torch
 
 import paper_2608_06690_amd as P
@@ -93,3 +94,79 @@ def test_every_optimizer_shows_the_norm_of_its_own_last_step(monkeypatch):
     joint((b, gb), (a, ga))
     single(c, gc_)
     single(a, ga)
+
+
+def scored_route_args(T=6):
+    """pmpe_route_scored's tensors by name, in order, as a layer with a score rule gives them."""
+    d = P.make_desc(H, I, PUB, PRIV, K)
+    E = PUB + PRIV
+    f = lambda *s: torch.zeros(*s)  # noqa: E731
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    return d, P.make_score_rule(), T, dict(
+        x=f(T, H).bfloat16(), wr_pub=f(PUB, H), wr_priv=f(PRIV, H), logit_bias=f(E), select_bias=f(E), policy_word=i(T),
+        topk_idx=i(T * K), topk_gate=f(T * K), topk_logit=f(T * K), allow=torch.zeros(T, dtype=torch.uint8), margin=f(T),
+        dev_status=i(1), ws=torch.zeros(P.pmpe_workspace_bytes(d, T), dtype=torch.uint8))
+
+
+def scored_backward_args(T=6):
+    d = P.make_desc(H, I, PUB, PRIV, K, 1, 128)
+    E, R = PUB + PRIV, T * K
+    f = lambda *s: torch.zeros(*s)  # noqa: E731
+    b = lambda *s: torch.zeros(*s).bfloat16()  # noqa: E731
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    return d, P.make_score_rule(), T, dict(
+        topk_logit=f(R), x=b(T, H), dout=b(T, H), topk_idx=i(R), topk_gate=f(R), expert_count=i(E), expert_offset=i(E + 1),
+        row_token=i(R), token_row=i(R), y_perm=b(R, H), wr_pub=f(PUB, H), wr_priv=f(PRIV, H), w13_pub=b(PUB, 2 * I, H),
+        w2_pub=b(PUB, H, I), w13_priv=b(PRIV, 2 * I, H), w2_priv=b(PRIV, H, I), logit_bias=f(E), w13_sh=b(2 * 128, H),
+        w2_sh=b(H, 128), w2t_pub=b(PUB, I, H), w13t_pub=b(PUB, H, 2 * I), w2t_priv=b(PRIV, I, H), w13t_priv=b(PRIV, H, 2 * I),
+        ab=f(R, 2 * I), dx=f(T, H), dw13_priv=f(PRIV, 2 * I, H), dw2_priv=f(PRIV, H, I), dwr_priv=f(PRIV, H),
+        grad_rows=i(PRIV), ws=torch.zeros(P.pmpe_backward_workspace_bytes(d, T), dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("call,make", [("pmpe_route_scored", scored_route_args), ("pmpe_backward_scored", scored_backward_args)])
+def test_calls_of_a_scored_layer_check_their_tensors(monkeypatch, call, make):
+    """Every tensor has to have its elements, type, device and order: a short one would be read or written
+    past its end."""
+    d, rule, T, good = make()
+    calls, here = [], []
+    monkeypatch.setattr(N, "_lib", types.SimpleNamespace(**{call: lambda *a: calls.append(a) or 0}))
+    monkeypatch.setattr(N, "_here", lambda t, name: here.append(name) or -1)  # the device of these tensors
+    monkeypatch.setattr(N, "_stream", lambda stream: 0)
+    f = lambda v: getattr(P, call)(d, rule, T, *v.values())  # noqa: E731
+    f(good)
+    assert len(calls) == 1 and here == ["x"]
+    for name, t in good.items():
+        if name in ("x", "ws"):  # (the library checks a workspace's size)
+            continue
+        other = torch.float64 if t.dtype != torch.float64 else torch.float32
+        longer = torch.cat([t.flatten(), t.flatten()[:1]])
+        for bad in (t.flatten()[:-1], longer, t.to(other), torch.stack([t, t], dim=-1)[..., 0]):
+            if bad.dtype == t.dtype and bad.numel() == t.numel() and bad.is_contiguous():
+                continue  # one element is contiguous at any stride
+            with pytest.raises(ValueError, match=name):
+                f({**good, name: bad})
+    for bad in (good["x"][:-1], good["x"].double(), good["x"].t().contiguous().t()):
+        with pytest.raises(ValueError, match="x must"):
+            f({**good, "x": bad})
+    with pytest.raises(ValueError, match="workspace"):
+        f({**good, "ws": torch.zeros(64, 64, dtype=torch.uint8)[:, 0]})
+    monkeypatch.setattr(N, "_here", lambda t, name: 0)  # x on a device, the others on the host
+    with pytest.raises(ValueError, match="device"):
+        f({**good, "x": types.SimpleNamespace(dtype=good["x"].dtype, get_device=lambda: 0, numel=good["x"].numel,
+                                              is_contiguous=lambda: True, data_ptr=lambda: 0)})
+    monkeypatch.setattr(N, "_here", lambda t, name: -1)
+    assert len(calls) == 1
+    # what may be absent
+    may = {"pmpe_route_scored": ("wr_priv", "logit_bias", "select_bias", "policy_word", "topk_logit", "margin", "dev_status"),
+           "pmpe_backward_scored": ("logit_bias", "w2t_pub", "w13t_pub", "w2t_priv", "w13t_priv", "ab", "grad_rows")}[call]
+    f({**good, **dict.fromkeys(may)})
+    assert len(calls) == 2
+
+
+def test_a_layer_checks_its_balance_bias():
+    rule = P.make_score_rule()
+    make_layer(rule, torch.zeros(PUB + PRIV))
+    for bad in (torch.zeros(PUB), torch.zeros(PUB + PRIV).bfloat16(), torch.zeros(2 * (PUB + PRIV))[::2],
+                torch.zeros(PUB + PRIV, device="meta")):
+        with pytest.raises(ValueError, match="select_bias"):
+            make_layer(rule, bad)
