@@ -398,7 +398,10 @@ class NormedMoE:
 
     delta is what the sublayer before added to the stream (None: nothing); the next block gets
     (residual, out) as its (h, delta). weight [H] fp32 or bf16 is the norm's, which is frozen with
-    the public model unless a backward is given a dweight to fill."""
+    the public model unless a backward is given a dweight to fill.
+
+    The buffers of a batch size hold its last forward, as the layer's do: a backward comes before the next
+    forward of as many tokens."""
 
     def __init__(self, layer: PolicyMaskedMoE, weight: torch.Tensor, eps: float = 1e-6):
         self.layer, self.weight, self.eps = layer, weight, eps
@@ -412,12 +415,12 @@ class NormedMoE:
             self._bufs[T] = BlockBuffers(norm, norm, torch.empty(T, dtype=torch.float32, device=dev))
         return self._bufs[T]
 
-    def _norm(self, h, delta, b: BlockBuffers, stream) -> None:
+    def _norm(self, h, delta, b: BlockBuffers, stream, q=None, scale=None) -> None:
         if delta is not None and b.total is None:
             b.total = torch.empty_like(b.norm)
         b.residual = h if delta is None else b.total
-        N.pmpe_rmsnorm(h, delta, self.weight, self.eps, None if delta is None else b.residual, b.norm, b.norm_q,
-                       b.norm_scale, b.rstd, stream)
+        N.pmpe_rmsnorm(h, delta, self.weight, self.eps, None if delta is None else b.residual, b.norm, q, scale, b.rstd,
+                       stream)
 
     def forward(self, h, delta, words, audit: AuditBuffers, req_offset=None, stream=None,
                 train: bool = False) -> BlockBuffers:
@@ -434,7 +437,7 @@ class NormedMoE:
         if b.norm_q is None:
             b.norm_q = torch.empty(T, H, dtype=torch.uint8, device=h.device)
             b.norm_scale = torch.empty(T, H // 32, dtype=torch.uint8, device=h.device)
-        self._norm(h, delta, b, stream)
+        self._norm(h, delta, b, stream, b.norm_q, b.norm_scale)
         b.layer = self.layer.forward_mx(b.norm, b.norm_q, b.norm_scale, words, fp8, audit, req_offset, stream)
         return b
 

@@ -170,3 +170,19 @@ def test_a_layer_checks_its_balance_bias():
                 torch.zeros(PUB + PRIV, device="meta")):
         with pytest.raises(ValueError, match="select_bias"):
             make_layer(rule, bad)
+
+
+def test_a_plain_forward_after_one_in_8_bits_writes_no_bytes(monkeypatch):
+    outs = []
+    monkeypatch.setattr(N, "pmpe_rmsnorm", lambda x, res, w, eps, total, out, q, s, rstd, stream: outs.append((q, s)))
+    blk = P.NormedMoE(make_layer(), torch.ones(H))
+    monkeypatch.setattr(blk.layer, "forward", lambda *a: None)
+    monkeypatch.setattr(blk.layer, "forward_mx", lambda *a: None)
+    h = torch.zeros(4, H).bfloat16()
+    blk.forward(h, None, None, None)
+    b = blk.forward_mx(h, None, None, None, None)
+    kept = b.norm_q, b.norm_scale
+    blk.forward(h, None, None, None)
+    blk.forward_mx(h, None, None, None, None)
+    assert outs[0] == outs[2] == (None, None)
+    assert all(t is k for i in (1, 3) for t, k in zip(outs[i], kept))
