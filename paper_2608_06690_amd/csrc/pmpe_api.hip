@@ -652,6 +652,7 @@ pmpe_status pmpe_adamw_clipped(void* param, int32_t param_dtype, float* master, 
                                float beta2, float eps, float weight_decay, const float* norm,
                                pmpe_stream_t stream) {
   if (!norm) return PMPE_ERR_NULL;
+  if (((uintptr_t)norm & 3u) != 0) return PMPE_ERR_ALIGN;
   return adamw_impl(param, param_dtype, master, grad, m, v, n, step, lr, beta1, beta2, eps, weight_decay, norm, stream);
 }
 

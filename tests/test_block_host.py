@@ -186,3 +186,11 @@ def test_a_plain_forward_after_one_in_8_bits_writes_no_bytes(monkeypatch):
     blk.forward_mx(h, None, None, None, None)
     assert outs[0] == outs[2] == (None, None)
     assert all(t is k for i in (1, 3) for t, k in zip(outs[i], kept))
+
+
+def test_the_norm_of_a_clipped_step_is_aligned():
+    f, hp = N.lib().pmpe_adamw_clipped, (1e-3, 0.9, 0.99, 1e-8, 0.0)
+    a, b, c, d, e = 0x10000, 0x20000, 0x30000, 0x40000, 0x50000
+    for norm in (e + 1, e + 2, e + 3):
+        assert f(a, N.PMPE_F32, None, b, c, d, 4, 1, *hp, norm, None) == -5  # PMPE_ERR_ALIGN
+    assert f(a, N.PMPE_F32, None, b, c, d, 0, 1, *hp, e, None) == 0
