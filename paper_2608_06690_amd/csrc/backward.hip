@@ -26,6 +26,8 @@
 // public gradient is ever formed; then per-token input-gradient and
 // per-private-expert router-gradient reductions. Every output element is summed by
 // one thread in a fixed order, so the results are bitwise reproducible.
+#include <cfloat>
+
 #include "pmpe_internal.h"
 
 namespace pmpe {
@@ -421,7 +423,8 @@ __global__ __launch_bounds__(BT) void bwd_swiglu_kernel(BwdArgs a, const float* 
 // Softmax over the whole permitted pool (POOL_SOFTMAX), one wave per token t: from its pool logits
 // z_e = x_t . W_r[e] (+ b_e) at zt, given as zsplit partial sums pstride apart that are added in
 // order, p = softmax(z) and dz_e = p_e ([e selected] dg_e - sum_sel p_i dg_i) for every pool
-// member e, written to dz_pool[t, e - first id of the pool] (zt may be that row).
+// member e, written to dz_pool[t, e - first id of the pool] (zt may be that row). A route by
+// scores masks logits (-inf or NaN: p = 0, +inf as the largest finite value), and so does this.
 // The pool of the token is the one its selection lies in (a masked route never mixes pools;
 // the soft control ranks the concatenated pool).
 struct TokenPool {
@@ -444,7 +447,7 @@ __device__ __forceinline__ void pool_dz(const BwdArgs& a, int t, const float* zt
     sel = a.topk_idx[(size_t)t * a.k + lane] - first;
     dg = a.dz_row[a.token_row[(size_t)t * a.k + lane]];
   }
-  float v[NPL], u[NPL], mx = -INFINITY;
+  float v[NPL], u[NPL], mx = a.scored ? -FLT_MAX : -INFINITY;
 #pragma unroll
   for (int r = 0; r < NPL; ++r) {
     const int i = r * 64 + lane;
@@ -453,6 +456,7 @@ __device__ __forceinline__ void pool_dz(const BwdArgs& a, int t, const float* zt
     if (i < pool) {
       v[r] = zt[i];
       for (int p = 1; p < zsplit; ++p) v[r] += zt[p * pstride + i];
+      if (a.scored) v[r] = v[r] > -INFINITY ? fminf(v[r], FLT_MAX) : -INFINITY;
     }
     mx = fmaxf(mx, v[r]);
   }
@@ -474,7 +478,7 @@ __device__ __forceinline__ void pool_dz(const BwdArgs& a, int t, const float* zt
   den = wave_sum(den);
 #pragma unroll
   for (int r = 0; r < NPL; ++r) {
-    v[r] = v[r] / den;
+    v[r] = a.scored && den == 0.f ? 0.f : v[r] / den;  // (den 0: nothing but masked logits)
     sum += v[r] * u[r];
   }
   sum = wave_sum(sum);

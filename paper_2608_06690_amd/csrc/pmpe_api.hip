@@ -253,6 +253,7 @@ pmpe_status backward_impl(const pmpe_layer_desc* d, const pmpe_score_rule* rule,
             L.P > 0 ? (uint16_t*)(w + L.tr) : nullptr, L.P, (float*)(w + L.grow)};
   if (rule) {
     a.gate_scale = rule->scale;
+    a.scored = 1;
     a.sigmoid = sigmoid;
     a.renorm = d->gate_mode == PMPE_GATE_RENORM_TOPK;
     a.topk_logit = topk_logit;

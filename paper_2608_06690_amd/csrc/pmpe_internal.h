@@ -344,7 +344,7 @@ struct BwdArgs {
   float* g_row;           // [T*k]: the gate of each row (its upstream rows are g_row[r] dout[t])
   // routing by scores: the gates' scale, and with sigmoid scores the selected logits
   float gate_scale = 1.f;
-  int sigmoid = 0, renorm = 0;
+  int scored = 0, sigmoid = 0, renorm = 0;
   const float* topk_logit = nullptr;  // [T*k]
 };
 constexpr int BWD_DWR_SPLIT = 16;  // row chunks per private expert in the router-row gradient
