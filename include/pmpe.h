@@ -680,9 +680,10 @@ pmpe_status pmpe_rmsnorm_backward(int32_t T, int32_t H, int32_t dtype, const voi
  *   gate_e = scale softmax over the selected z                   RENORM_TOPK, softmax
  *   gate_e = scale s_e                                           POOL_SOFTMAX: scores as they are
  *
- * s, u and the ranks are 64-bit: the selection is that of 64-bit arithmetic on the fp32 logits. (A
- * rank that is a sum of two is rounded to 45 bits, so that sums which differ only by their terms'
- * rounding are equal: the sigmoids of z and -z add up to 1 for every z.) A logit of -inf (or NaN) masks its expert: score and gate 0, no part in a group's rank, selected
+ * s, u and the ranks are 64-bit: the selection is that of 64-bit arithmetic on the fp32 logits, with
+ * s(z) = 1 - s(-z) for the sigmoid of z >= 0 and a rank of two as (s + s) + (b + b). (Sums that are
+ * equal in the mathematics then are so in 64 bits: the sigmoids of z and -z, a bias on either of two
+ * experts.) A logit of -inf (or NaN) masks its expert: score and gate 0, no part in a group's rank, selected
  * only when nothing else is left. +inf counts as the largest finite value. A bias of -inf (or NaN)
  * ranks an expert with the masked ones, its score staying. With route_mode SOFT (the control arm)
  * the pool is the concatenated one and neither pool may have groups.
@@ -710,7 +711,8 @@ typedef struct {
  *   topk_logit   [T, k] fp32 out or NULL: the selected logits (pmpe_backward_scored reads them)
  *   allow        [T] uint8 out: the resolved policy decision
  *   margin       [T] fp32 out or NULL: u of the last selected expert minus the largest u that was
- *                left among the groups that stayed; +inf when none, or only masked ones, were left
+ *                left among the groups that stayed; 0 where they are equal, also as two masked ones;
+ *                else +inf when none, or only masked ones, were left
  * d gives the pools, top_k, gate_mode and route_mode. No workspace.
  * Errors: those of the descriptor, PMPE_ERR_SHAPE (a rule out of range), PMPE_ERR_NULL,
  * PMPE_ERR_DTYPE. Pointers need the alignment of their elements only.

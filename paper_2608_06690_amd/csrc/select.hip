@@ -2,7 +2,7 @@
 // best groups of experts, and the gradient of the gates.
 //
 //   s = sigmoid(z), or softmax(z) over the pool;  u = s + select_bias
-//   a group's rank: the sum of its best one or two u; the best `keep` groups stay
+//   a group's rank: its best u, or the sum of its best two, (s + s) + (bias + bias); the best `keep` stay
 //   the k largest u of the experts that stay win, ties to the lower id
 //   gates: scale s, or scale s / sum of the winners' s (softmax: the softmax of the winners' z)
 //
@@ -12,8 +12,8 @@
 // compares the upper word (20 bits of mantissa) by six DPP maxima; only when experts tie there
 // does it look at the lower word. The k winners are k such rounds: a sort of the pool takes more for
 // k up to 16. Bound by the vector instructions of a token (530 at 256 experts in 8 groups, k 8: half of
-// them the scores in 64 bits): 16384 such tokens take 21.5 us, of which their issue is 15; 16.8 MB of
-// logits alone would take 4. 32 us with fp64 maxima, library exponentials and winners gathered by lane
+// them the scores in 64 bits): 16384 such tokens take 22 us, of which their issue is 15; 16.8 MB of
+// logits alone would take 4. (A balance bias adds 1 us, the test for ranks that are as good as equal.) 32 us with fp64 maxima, library exponentials and winners gathered by lane
 // moves; 26 with the rows' loads behind one another.
 #include <cfloat>
 
@@ -138,9 +138,13 @@ __device__ __forceinline__ void logits(const SelectArgs& a, int t, const Pool& p
 // A masked logit (-inf) or NaN has score 0 and ranks behind every other; +inf counts as the
 // largest finite value.
 __device__ __forceinline__ bool live_logit(float z) { return z > -INFINITY; }
+// For z >= 0 the complement of that of -z: the two then add up to 1 in fp64 as well (the complement is off by
+// 2^-54 at most, the sum of the two by less than half a step from 1).
 __device__ __forceinline__ double sigmoid64(float z) {
+#pragma clang fp contract(off)
   const double e = exp64(-fabs((double)z));
-  return (z < 0.f ? e : 1.0) * rcp64(1.0 + e);
+  const double q = e * rcp64(1.0 + e);
+  return z < 0.f ? q : 1.0 - q;
 }
 
 // LDS of a wave: u of the pool for the groups' ranks, then the winners' ids and logits.
@@ -157,6 +161,44 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_s_waitcnt(0xc07f);
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+}
+
+// Ranks of the groups where two of them are as good as equal: a rank is (s + s) + (bias + bias), so that
+// equal sums have equal bits wherever the biases lie, and the u of two experts are each rounded. One lane per
+// group; u in LDS, where the experts of the groups that do not stay become -inf. Only where few values of logits and
+// biases occur (one lane walks a group: the 16384 tokens take 44 us if all of them come here).
+__device__ __forceinline__ void near_ranks(const SelectArgs& a, int t, const Pool& p, float top, double inv, SelectLds& lds) {
+#pragma clang fp contract(off)
+  const int gs = p.n / p.groups, g = lane_id();
+  double* u = lds.u + g * gs;
+  double r = -INFINITY;
+  if (g < p.groups) {
+    int i0 = 0, i1 = -1;
+    for (int i = 1; i < gs; ++i) {
+      if (u[i] > u[i0]) {
+        i1 = i0;
+        i0 = i;
+      } else if (i1 < 0 || u[i] > u[i1]) {
+        i1 = i;
+      }
+    }
+    r = u[i0];
+    if (i1 >= 0 && u[i1] > -DBL_MAX) {
+      auto score = [&](int i) {
+        const float z = logit(a, t, p, g * gs + i);
+        return a.sigmoid ? sigmoid64(z) : exp64((double)fminf(z, FLT_MAX) - (double)top) * inv;
+      };
+      const float* bias = a.select_bias + p.first + g * gs;
+      r = (score(i0) + score(i1)) + ((double)bias[i0] + (double)bias[i1]);
+    }
+  }
+  int rank = 0;
+  for (int q = 0; q < p.groups; ++q) {
+    const double v = read_lane(r, q);
+    rank += (v > r || (v == r && q < g)) ? 1 : 0;
+  }
+  if (g < p.groups && rank >= p.keep)
+    for (int i = 0; i < gs; ++i) u[i] = -INFINITY;
 }
 
 // NPL registers of experts per lane; tau and the pool are the wave's own.
@@ -233,18 +275,34 @@ __device__ void select_token(const SelectArgs& a, int t, int tau, const Pool& p,
     if (per > 16) merge(16);
     if (per > 32) merge(32);
     // masked experts add nothing; a group of masked ones only ranks behind the others
-    if (a.group_top == 2 && b1 > -DBL_MAX) {
-      // to 45 bits: sums that are equal but for their terms' rounding (s(z) + s(-z) = 1) tie
-      b0 += b1;
-      b0 = __longlong_as_double((long long)(((uint64_t)__double_as_longlong(b0) + 0x80) & ~0xFFull));
-    }
+    const bool two = a.group_top == 2 && b1 > -DBL_MAX;
+    const double room = 0x1p-48 * (fabs(b0) + (two ? fabs(b1) : 0.0) + 1.0);
+    const double u0 = b0, u1 = b1;
+    if (two) b0 += b1;
     int rank = 0;
     for (int q = 0; q < p.groups; ++q) {
       const double v = read_lane(b0, q * per);
       rank += (v > b0 || (v == b0 && q < g)) ? 1 : 0;
     }
-    // the experts of the other groups are out of the running
-    if (g < p.groups && rank >= p.keep)
+    // A sum of two u is off by less than an eighth of `room`, as is near_ranks' own: where a group that stays and the
+    // first that does not, or one that does not and the last that stays, lie nearer to one another (and are not the
+    // same two u), theirs decides.
+    bool near = false;
+    if (a.select_bias && a.group_top == 2) {
+      const bool in = g < p.groups, stays = rank < p.keep;
+      const int last = __builtin_ctzll(__ballot(in && rank == p.keep - 1)), next = __builtin_ctzll(__ballot(in && rank == p.keep));
+      const double vl = read_lane(b0, last), vn = read_lane(b0, next);
+      near = in && fmin(b0, vn) > -DBL_MAX && (stays ? b0 - vn : vl - b0) <= room;
+      if (__ballot(near) != 0) {
+        const double l0 = read_lane(u0, last), l1 = read_lane(u1, last), n0 = read_lane(u0, next), n1 = read_lane(u1, next);
+        near = __ballot(near && (u0 != (stays ? n0 : l0) || u1 != (stays ? n1 : l1))) != 0;
+      } else {
+        near = false;
+      }
+    }
+    if (near)
+      near_ranks(a, t, p, top, inv, lds);
+    else if (g < p.groups && rank >= p.keep)  // the experts of the other groups are out of the running
       for (int i = lane % per; i < gs; i += per) lds.u[g * gs + i] = -INFINITY;
     wave_lds_fence();
 #pragma unroll
