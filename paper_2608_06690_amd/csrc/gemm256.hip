@@ -51,10 +51,10 @@
 // instructions each, 32 clocks an instruction): what a phase costs beyond them, the latency of its
 // fragment reads and two barriers, then comes half as often (16384 tokens of the Qwen3-30B-A3B-shaped
 // layer, both products: 857 us with four phases, 798 with two; 4096 tokens 303 -> 293). The reading wave
-// issues the copies (of all but A1). Timing builds of that batch: without copies 524 us, without stores
-// 603, without block scales 726, with all operands in L2 713, without MFMAs 747, without fragment reads
-// 799: copies, stores and scales each hold up the lock step of the two row groups, and the matrix
-// instructions are not what bounds it. 1.24 TFLOP in 790 us.
+// issues the copies (of all but A1). 1.24 TFLOP in 790 us (472 and 318), half a plain product's rate: the
+// matrix instructions are not what bounds it, the copies, stores and barriers of the two row groups'
+// lock step are. A step takes 1.9 us; copying alone moves its 64 KB per CU from L2 in 0.49, with its
+// fragment reads and eight barriers in 0.91.
 #include "lds_dma.h"
 #include "mx.h"
 #include "pmpe_internal.h"
@@ -493,7 +493,8 @@ __global__ __launch_bounds__(THREADS) void gemm256_kernel(FfnArgs a) {
   // the first MB row blocks of a quadrant
   constexpr int SUBS = MX ? 1 : 2;
   // MX: the products of a phase stay in it (without this the compiler moves them past the branches
-  // of later copies, which keeps the fragments of two phases alive and spills accumulators)
+  // of later copies, which keeps the fragments of two phases alive and spills accumulators; with it
+  // MX_UP has six registers spilled, 28 bytes of scratch per lane, and MX_DOWN none)
   auto pin = [&](auto blocks, f32x4 (&acc)[4][2]) {
     if constexpr (MX) {
 #pragma unroll

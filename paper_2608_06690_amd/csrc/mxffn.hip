@@ -375,7 +375,9 @@ hipError_t launch_expert_ffn_mx(const MxFfnArgs& a, hipStream_t s) {
   //   64 x 128     163  53 148   186  55 161   237  67 206   315  81 281   356  90 315   510 120 452   870 188 740
   //   128 x 256    171  63 153   174  65 156   178  62 160   196  69 177   251  78 224   317  92 271   540 136 446
   //   256 x 256    196  80 180   202  82 183   202  79 187   220  83 198   227  91 211   266 101 243   449 137 372
-  // (32 rows: 149, 51, 130 and 165, 61, 148 with the two smaller.) The large kernel needs a few tiles per
+  // (32 rows: 149, 51, 130 and 165, 61, 148 with the two smaller.) 52 rows is the line of the two layers that
+  // fill the chip; the 52 experts, with about one large tile per CU, would have theirs at about 60 and lose 10 us at
+  // 56 rows. The large kernel needs a few tiles per
   // CU (the 52 experts give it one or two), and two K steps.
   const int64_t E = a.n_pub + a.n_priv, rows = (int64_t)a.T * a.k / E;
   hipError_t e;

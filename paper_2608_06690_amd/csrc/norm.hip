@@ -15,7 +15,7 @@
 // outputs and scales (303 MB) take 57 us, 5.3 TB/s. W is as many waves as hold the row with one vector
 // per lane (that batch on one wave of four vectors: 69 us, its loads in flight too few); 8 rows take
 // 3.5 us on the card. The backward of 4096 such rows with dw takes 21.5 us (16.5 and 4.8 for the sum of
-// its parts; 84 MB: 16.4 at the copy's rate), of 16384 rows 62.
+// its parts; 84 MB: 16.4 at the copy's rate), of 16384 rows 67 (62 and 4.8).
 #include <algorithm>
 #include <type_traits>
 
@@ -275,8 +275,8 @@ hipError_t launch_rmsnorm(const NormArgs& a, hipStream_t s) {
 }
 
 // Blocks of the backward: four waves for each of a CU's SIMDs where rows are long enough. Fewer leave
-// loads out of flight, more make parts to add: 16384 rows of 2048 67 us (512 blocks 87, 2048: 78), 4096
-// rows 21.5 (21.3, 29.0).
+// loads out of flight, more make parts to add: 16384 rows of 2048 67 us (512 blocks 87, 2048: 77), 4096
+// rows 21.7 (21.5, 28.8).
 int rmsnorm_bwd_parts(int T, int H) {
   const int waves = (H + 511) / 512;  // of a row, up to a power of two
   const int blocks = waves <= 1 ? 512 : waves <= 2 ? 1024 : waves <= 4 ? 1024 : waves <= 8 ? 512 : 256;

@@ -11,8 +11,8 @@
 // (fp64 runs at the rate of scalar fp32). u becomes a 64-bit key of the same order, of which a round
 // compares the upper word (20 bits of mantissa) by six DPP maxima; only when experts tie there
 // does it look at the lower word. The k winners are k such rounds: a sort of the pool takes more for
-// k up to 16. Bound by the vector instructions of a token (530 at 256 experts in 8 groups, k 8: half of
-// them the scores in 64 bits): 16384 such tokens take 22 us, of which their issue is 15; 16.8 MB of
+// k up to 16. Bound by the vector instructions of a token (556 at 256 experts in 8 groups, k 8: half of
+// them the scores in 64 bits): 16384 such tokens take 22 us, of which their issue is 16; 16.8 MB of
 // logits alone would take 4. (A balance bias adds 1 us, the test for ranks that are as good as equal.) 32 us with fp64 maxima, library exponentials and winners gathered by lane
 // moves; 26 with the rows' loads behind one another.
 #include <cfloat>
