@@ -13,8 +13,9 @@
 // does it look at the lower word. The k winners are k such rounds: a sort of the pool takes more for
 // k up to 16. Bound by the vector instructions of a token (556 at 256 experts in 8 groups, k 8: half of
 // them the scores in 64 bits): 16384 such tokens take 22 us, of which their issue is 16; 16.8 MB of
-// logits alone would take 4. (A balance bias adds 1 us, the test for ranks that are as good as equal.) 32 us with fp64 maxima, library exponentials and winners gathered by lane
-// moves; 26 with the rows' loads behind one another.
+// logits alone would take 4. (Of them the test for ranks that are as good as equal takes 1, with a balance
+// bias.) 32 us with fp64 maxima, library exponentials and winners gathered by lane moves; 26 with the rows'
+// loads behind one another.
 #include <cfloat>
 
 #include "pmpe_internal.h"

@@ -121,3 +121,49 @@ def test_biases_that_mask_or_are_huge():
         if want == [6, 0]:  # the group that stays has one live expert; the other place goes to its lowest masked one
             want = [4, 6]
         assert got["idx"][0].tolist() == want, bias
+
+
+@pytest.mark.parametrize("T", [5, 300, 2304])  # logits in partial sums, and whole
+@pytest.mark.parametrize("score", [P.PMPE_SCORE_SOFTMAX, P.PMPE_SCORE_SIGMOID])
+def test_a_layer_whose_experts_have_one_router_row(T, score):
+    """Logits that are equal, or nearly so (their sums have an order of their own in each lane of the router):
+    the selection is that of the layer's own fp32 logits, read one expert at a time through a bias that
+    nothing else reaches."""
+    pub, priv, k, H = 64, 16, 4, 256
+    d = P.make_desc(H, 128, pub, priv, k)
+    rule = P.make_score_rule(score, (8, 3), (4, 2), 2)
+    gen = torch.Generator().manual_seed(T)
+    bias = torch.randint(0, 4, (pub + priv,), generator=gen).float() * 0.3
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.empty(T, H, device="cuda").normal_(0, 1, generator=g).bfloat16()
+    row = torch.empty(1, H, device="cuda").normal_(0, 0.06, generator=g)
+    ws = torch.empty(P.pmpe_workspace_bytes(d, T), dtype=torch.uint8, device="cuda")
+    words, allow = words_of(T, 2), torch.empty(T, dtype=torch.uint8, device="cuda")
+
+    def route(d, rule, bias, words):
+        idx = torch.full((T, d.top_k), -7, dtype=torch.int32, device="cuda")
+        gate, logit = torch.empty(T, d.top_k, device="cuda"), torch.empty(T, d.top_k, device="cuda")
+        P.pmpe_route_scored(d, rule, T, x, row.repeat(pub, 1), row.repeat(priv, 1), None, bias.cuda(), words, idx, gate, logit,
+                            allow, None, None, ws)
+        torch.cuda.synchronize()
+        return idx, gate, logit
+
+    z = torch.empty(T, pub + priv)
+    one, any_rule = P.make_desc(H, 128, pub, priv, 1), P.make_score_rule(score)
+    for e in range(pub + priv):
+        b = torch.zeros(pub + priv)
+        b[e] = 100.0
+        idx, _, logit = route(one, any_rule, b, torch.full_like(words, P.PMPE_POLICY_ALLOW - (1 << 32)) if e >= pub else None)
+        assert torch.all(idx == e)
+        z[:, e] = logit.view(-1).cpu()
+    idx, gate, logit = route(d, rule, bias, words)
+    zs, b, al = z.double().tolist(), bias.double().tolist(), allow.tolist()
+    for t in range(T):
+        first, n, groups, keep = (pub, priv, 4, 2) if al[t] else (0, pub, 8, 3)
+        pool = zs[t][first:first + n]
+        want = choose(pool, b[first:first + n], k, score, groups, keep)
+        assert idx[t].tolist() == [first + i for i in want], t
+        assert logit[t].tolist() == [pool[i] for i in want]
+        s = [sigmoid(pool[i]) for i in want] if score == P.PMPE_SCORE_SIGMOID else softmax([pool[i] for i in want])
+        for got, e in zip(gate[t].tolist(), s):
+            assert abs(got - e / sum(s)) <= (2.0 ** -24 + 2.0 ** -40) * e / sum(s)
