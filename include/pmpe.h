@@ -87,6 +87,10 @@ typedef enum { PMPE_ROUTE_MASKED = 0, PMPE_ROUTE_SOFT = 1 } pmpe_route_mode;
 #define PMPE_DEV_PRIV_ROUTER_MISSING 0x1u  /* allow rows met wr_priv == NULL: routed as deny */
 #define PMPE_DEV_PRIV_WEIGHTS_MISSING 0x2u /* private rows met NULL private expert weights:
                                               those rows were NOT executed, outputs zeroed */
+#define PMPE_DEV_CACHE_REFUSED 0x4u        /* a request met a cache page of another decision: not
+                                              written, not read */
+#define PMPE_DEV_CACHE_RANGE 0x8u          /* a position outside the block table, or a page number
+                                              outside the pool: not written, not read */
 
 /* Supported ranges (checked by host validation). */
 #define PMPE_MAX_POOL 256  /* n_pub and n_priv each in [top_k, 256] */
@@ -850,6 +854,131 @@ pmpe_status pmpe_expert_ffn_mx(const pmpe_layer_desc* d, int32_t T, const uint8_
                                uint32_t* audit_token_rows, uint32_t* audit_priv_calls,
                                uint32_t* dev_status, void* ws, size_t ws_bytes,
                                pmpe_stream_t stream);
+
+/*
+ * Paged cache of keys and values: the attention state of requests whose tokens go through policy-masked
+ * layers one by one. App. B.2 tags caches with the policy decision and refuses reuse across tags:
+ * pmpe_cache_tag_check does so on the host before a model call; here every page carries the decision of
+ * the requests it was given to, and the kernels refuse the page to requests of the other decision,
+ * whatever a block table says.
+ *
+ *   k_cache, v_cache  [n_pages, n_kv_heads, page_size, head_dim] of cache_dtype
+ *   k_scale, v_scale  [n_pages, n_kv_heads, head_dim / 32, page_size] uint8 with PMPE_FP8_E4M3, NULL
+ *                     otherwise: the format of pmpe_rmsnorm's 8-bit output, e4m3(x / s) with
+ *                     s = 2^ceil(log2(amax / 448)) of 32 consecutive values of a head, stored as its
+ *                     biased exponent; a block with a value that is not finite becomes NaN
+ *   block_table       [R, max_pages] int32: position p of request r is row p % page_size of page
+ *                     block_table[r, p / page_size]. Entries past a request's length are not read
+ *   page_tag          [n_pages] uint32 or NULL (no check): PMPE_POLICY_ALLOW or PMPE_POLICY_DENY. A
+ *                     request may use a page only if its tag is the request's resolved decision; any
+ *                     other tag is refused to every request
+ *   policy_word       [R] uint32 or NULL (every request denies); read with page_tag only
+ *   dev_status        optional: PMPE_DEV_CACHE_REFUSED, PMPE_DEV_CACHE_RANGE
+ *
+ * A row that a request may not use takes no part: not written, not attended to, read back as zeros. Two
+ * requests may read one page; a page that a call writes belongs to one request of the batch.
+ */
+typedef struct {
+  int32_t n_pages;     /* pages in the pool, at least 1 */
+  int32_t page_size;   /* rows of a page, a multiple of 16, 16..1024 */
+  int32_t n_kv_heads;  /* 1..1024, with n_kv_heads * page_size * head_dim below 2^31 */
+  int32_t head_dim;    /* a multiple of 32, 32..256 */
+  int32_t max_pages;   /* columns of block_table, at least 1; max_pages * page_size below 2^30 */
+  int32_t act_dtype;   /* PMPE_BF16 or PMPE_F32: keys, values, queries and outputs */
+  int32_t cache_dtype; /* act_dtype, or PMPE_FP8_E4M3 with PMPE_BF16 */
+} pmpe_cache_desc;
+
+#define PMPE_MAX_REQUESTS (1 << 16)
+
+/*
+ * pmpe_kv_write - keys and values of a batch's tokens into their requests' pages.
+ *
+ * Request r has tokens [req_offset[r], req_offset[r + 1]) of the batch and seq_len[r] rows once they are
+ * written: its last token goes to position seq_len[r] - 1. Tokens outside every request are left out.
+ *
+ *   k, v         [T, n_kv_heads, head_dim] of act_dtype, tokens k_stride and v_stride elements apart (the
+ *                parts of one projection need no copy)
+ *   req_offset   [R + 1] int32, ascending; seq_len [R] int32
+ * Errors: PMPE_ERR_NULL, PMPE_ERR_SHAPE, PMPE_ERR_DTYPE, PMPE_ERR_ALIGN (k, v, the cache and its scales,
+ * and the strides in bytes: 16).
+ */
+pmpe_status pmpe_kv_write(const pmpe_cache_desc* c, int32_t T, int32_t R, const void* k, int64_t k_stride,
+                          const void* v, int64_t v_stride, const int32_t* req_offset,
+                          const int32_t* seq_len, const int32_t* block_table, const uint32_t* page_tag,
+                          const uint32_t* policy_word, void* k_cache, void* v_cache, uint8_t* k_scale,
+                          uint8_t* v_scale, uint32_t* dev_status, pmpe_stream_t stream);
+
+/*
+ * pmpe_kv_read - cached rows back in the activation type: row req_offset[r] + i of k and v is position
+ * first[r] + i of request r (first NULL: 0). Values are exact in bf16 (a power of two times an e4m3 value,
+ * down to bf16's subnormals). Rows of k and v outside every request are left as they were.
+ *   k, v   [T, n_kv_heads, head_dim] of act_dtype, out. Errors as pmpe_kv_write.
+ */
+pmpe_status pmpe_kv_read(const pmpe_cache_desc* c, int32_t T, int32_t R, void* k, void* v,
+                         const int32_t* req_offset, const int32_t* first, const int32_t* block_table,
+                         const uint32_t* page_tag, const uint32_t* policy_word, const void* k_cache,
+                         const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                         uint32_t* dev_status, pmpe_stream_t stream);
+
+/*
+ * pmpe_attn_decode - attention of one new token per request over its cached rows (its own among them).
+ *
+ *   s_j = scale q . k_j for positions j in [seq_first[r], seq_len[r]) whose page the request may use
+ *   out = sum_j exp(s_j - max s) v_j / sum_j exp(s_j - max s);  lse = max s + ln sum_j exp(s_j - max s)
+ *   query head i reads kv head i / (n_heads / n_kv_heads). A request without such a position has out 0
+ *   and lse -inf. Products, softmax statistics and sums are fp32, also of values cached in 8 bits.
+ *
+ *   q, out       [R, n_heads, head_dim] of act_dtype, requests of q q_stride elements apart; n_heads a
+ *                multiple of n_kv_heads, up to 1024
+ *   seq_first    [R] int32 or NULL (0): positions before it are out of the window
+ *   seq_len      [R] int32: rows of the request, the new token's among them (0 or less: none)
+ *   lse          [R, n_heads] fp32 out or NULL
+ *   ws           pmpe_attn_decode_workspace_bytes(c, R, n_heads) bytes, 16-byte aligned; the size does not
+ *                depend on lengths. Two calls equal in all inputs have equal bits
+ * Errors: as pmpe_kv_write, and PMPE_ERR_WORKSPACE.
+ */
+size_t pmpe_attn_decode_workspace_bytes(const pmpe_cache_desc* c, int32_t R, int32_t n_heads);
+
+pmpe_status pmpe_attn_decode(const pmpe_cache_desc* c, int32_t R, int32_t n_heads, const void* q,
+                             int64_t q_stride, const int32_t* seq_first, const int32_t* seq_len,
+                             const int32_t* block_table, const uint32_t* page_tag,
+                             const uint32_t* policy_word, const void* k_cache, const void* v_cache,
+                             const uint8_t* k_scale, const uint8_t* v_scale, float scale, void* out,
+                             float* lse, uint32_t* dev_status, void* ws, size_t ws_bytes,
+                             pmpe_stream_t stream);
+
+/*
+ * pmpe_sample - one token per row of logits, from given uniform numbers.
+ *
+ * The tokens of a row in descending order of their logits (equal logits: the lower id first), with masses
+ * m = exp((z - max z) / temperature), are cut to a leading part and drawn from it:
+ *   top_k        the first top_k (0 or less: no cut)
+ *   top_p        of these the fewest whose masses reach top_p times the sum of all of them, at least one
+ *                (1 or more, or NaN: no cut)
+ *   min_p        of these the ones with m >= min_p, at least one (0 or less, or NaN: no cut)
+ *   token        the first whose cumulated mass exceeds u times the sum of those left
+ * A temperature of 0 (or less, or NaN) takes the first token of the order. Masses and their sums are 64-bit,
+ * a mass resolved to 2^-44 of its neighbourhood's: the choice is that of 64-bit arithmetic but where a sum
+ * comes as near to its threshold as that. A logit of -inf (or NaN) masks its token; +inf counts as the largest
+ * finite value. A row without any token left has token -1, prob 0 and kept 0.
+ *
+ *   logits       [B, V] of logits_dtype (PMPE_F32 or PMPE_BF16), rows `stride` elements apart; V 1..PMPE_MAX_VOCAB
+ *   temperature, top_p, min_p [B] fp32 or NULL (1, 1 and 0); top_k [B] int32 or NULL (0)
+ *   u            [B] fp32 in [0, 1) (below 0 or NaN counts as 0, 1 or more as the last token's)
+ *   token        [B] int32 out
+ *   prob         [B] fp32 out or NULL: the token's mass over the sum of those left
+ *   kept         [B] int32 out or NULL: tokens left
+ *   ws           pmpe_sample_workspace_bytes(B, V) bytes, 16-byte aligned
+ * Errors: PMPE_ERR_NULL, PMPE_ERR_SHAPE (B above PMPE_MAX_REQUESTS, stride below V), PMPE_ERR_DTYPE,
+ * PMPE_ERR_ALIGN (elements; 16 bytes for ws), PMPE_ERR_WORKSPACE. B = 0 is valid.
+ */
+#define PMPE_MAX_VOCAB (1 << 19)
+size_t pmpe_sample_workspace_bytes(int32_t B, int32_t V);
+
+pmpe_status pmpe_sample(int32_t B, int32_t V, const void* logits, int32_t logits_dtype, int64_t stride,
+                        const float* temperature, const int32_t* top_k, const float* top_p,
+                        const float* min_p, const float* u, int32_t* token, float* prob, int32_t* kept,
+                        void* ws, size_t ws_bytes, pmpe_stream_t stream);
 
 #ifdef __cplusplus
 }

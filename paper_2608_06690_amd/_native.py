@@ -38,6 +38,8 @@ PMPE_POLICY_ALLOW = 0xA11C0DE5
 PMPE_POLICY_DENY = 0x00000000
 PMPE_DEV_PRIV_ROUTER_MISSING = 0x1
 PMPE_DEV_PRIV_WEIGHTS_MISSING = 0x2
+PMPE_DEV_CACHE_REFUSED = 0x4
+PMPE_DEV_CACHE_RANGE = 0x8
 
 STATUS_NAMES = {
     0: "PMPE_OK", -1: "PMPE_ERR_NULL", -2: "PMPE_ERR_SHAPE", -3: "PMPE_ERR_K_EXCEEDS_POOL",
@@ -110,6 +112,19 @@ def make_score_rule(score: int = 1, groups=(1, 1), groups_priv=(1, 1), group_top
                     scale: float = 1.0) -> ScoreRule:
     """A score rule; groups and groups_priv are (groups, groups that stay) of the two pools."""
     return ScoreRule(score, group_top, groups[0], groups[1], groups_priv[0], groups_priv[1], scale)
+
+
+class CacheDesc(ctypes.Structure):
+    """pmpe_cache_desc: sizes and types of a paged cache."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "max_pages", "act_dtype",
+                                              "cache_dtype")]
+
+
+def make_cache_desc(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, max_pages: int, bf16: bool = True,
+                    fp8: bool = False) -> CacheDesc:
+    """A paged cache of n_pages pages, of which a request has max_pages at most; fp8: values in 8 bits."""
+    act = PMPE_BF16 if bf16 else PMPE_F32
+    return CacheDesc(n_pages, page_size, n_kv_heads, head_dim, max_pages, act, PMPE_FP8_E4M3 if fp8 else act)
 
 
 _P = ctypes.c_void_p
@@ -194,6 +209,20 @@ _lib.pmpe_expert_ffn_mx_workspace_bytes.restype = _SZ
 _lib.pmpe_expert_ffn_mx_workspace_bytes.argtypes = [_DESC, _I32]
 _lib.pmpe_expert_ffn_mx.restype = _I32
 _lib.pmpe_expert_ffn_mx.argtypes = [_DESC, _I32] + [_P] * 17 + [_P, _SZ, _P]
+_CACHE = ctypes.POINTER(CacheDesc)
+_I64 = ctypes.c_int64
+_lib.pmpe_kv_write.restype = _I32
+_lib.pmpe_kv_write.argtypes = [_CACHE, _I32, _I32, _P, _I64, _P, _I64] + [_P] * 11
+_lib.pmpe_kv_read.restype = _I32
+_lib.pmpe_kv_read.argtypes = [_CACHE, _I32, _I32] + [_P] * 13
+_lib.pmpe_attn_decode_workspace_bytes.restype = _SZ
+_lib.pmpe_attn_decode_workspace_bytes.argtypes = [_CACHE, _I32, _I32]
+_lib.pmpe_attn_decode.restype = _I32
+_lib.pmpe_attn_decode.argtypes = [_CACHE, _I32, _I32, _P, _I64] + [_P] * 9 + [ctypes.c_float] + [_P] * 4 + [_SZ, _P]
+_lib.pmpe_sample_workspace_bytes.restype = _SZ
+_lib.pmpe_sample_workspace_bytes.argtypes = [_I32, _I32]
+_lib.pmpe_sample.restype = _I32
+_lib.pmpe_sample.argtypes = [_I32, _I32, _P, _I32, _I64] + [_P] * 9 + [_SZ, _P]
 
 EXPORTED = ["pmpe_version", "pmpe_status_string", "pmpe_workspace_bytes", "pmpe_check_desc",
             "pmpe_route", "pmpe_dispatch", "pmpe_expert_ffn", "pmpe_combine", "pmpe_audit",
@@ -204,7 +233,8 @@ EXPORTED = ["pmpe_version", "pmpe_status_string", "pmpe_workspace_bytes", "pmpe_
             "pmpe_rmsnorm", "pmpe_rmsnorm_backward_workspace_bytes", "pmpe_rmsnorm_backward",
             "pmpe_select", "pmpe_select_backward", "pmpe_route_scored", "pmpe_backward_scored",
             "pmpe_grad_norm_workspace_bytes", "pmpe_grad_norm", "pmpe_clip_grads", "pmpe_adamw_clipped",
-            "pmpe_expert_ffn_mx_workspace_bytes", "pmpe_expert_ffn_mx"]
+            "pmpe_expert_ffn_mx_workspace_bytes", "pmpe_expert_ffn_mx", "pmpe_kv_write", "pmpe_kv_read",
+            "pmpe_attn_decode_workspace_bytes", "pmpe_attn_decode", "pmpe_sample_workspace_bytes", "pmpe_sample"]
 
 PMPE_FP_LEAF_BYTES = 1024
 PMPE_FP_FANOUT = 16
@@ -685,3 +715,102 @@ def pmpe_expert_ffn_mx(desc, T, xq, xs, expert_count, expert_offset, row_token, 
         _arg_n(row_token, "row_token", n, _I32T, dev), *wt, *ws_, _arg_n(y_perm, "y_perm", n * H, _BF16, dev),
         _arg_n(audit_token_rows, "audit_token_rows", T, _WORDS, dev), _arg_n(audit_priv_calls, "audit_priv_calls", P, _WORDS, dev),
         _arg_n(dev_status, "dev_status", 1, _WORDS, dev), *_work(ws, dev), _stream(stream)), "pmpe_expert_ffn_mx")
+
+
+def _rows(t: torch.Tensor, name: str, shape, dtype, dev: int):
+    """Pointer of a tensor of this shape, type and device whose first dimension may have any stride of at least a
+    row, and that stride."""
+    if t.shape == shape and t.dtype == dtype and t.get_device() == dev:
+        n, row = len(shape), 1
+        for d in range(n - 1, 0, -1):
+            if shape[d] != 1 and t.stride(d) != row:
+                break
+            row *= shape[d]
+        else:
+            stride = t.stride(0) if shape[0] > 1 else row
+            if stride >= row:
+                return t.data_ptr(), stride
+    raise ValueError(f"{name} must be {list(shape)} of {dtype} on device {dev} with contiguous rows, not {list(t.shape)} "
+                     f"of {t.dtype} on {t.device} with strides {t.stride()}")
+
+
+_CACHE_T = {PMPE_F32: _F32, PMPE_BF16: _BF16, PMPE_FP8_E4M3: _U8}
+_ACT_T = {PMPE_F32: torch.float32, PMPE_BF16: torch.bfloat16}
+
+
+def _cache_args(c: CacheDesc, R: int, block_table, page_tag, policy_word, k_cache, v_cache, k_scale, v_scale, dev: int):
+    """The pointers of a paged cache, in two parts: its table, tags and words; its values and scales."""
+    shape = (c.n_pages, c.n_kv_heads, c.page_size, c.head_dim)
+    sshape = (c.n_pages, c.n_kv_heads, c.head_dim // 32, c.page_size)
+    dt = _CACHE_T.get(c.cache_dtype, ())
+    return ((_arg(block_table, "block_table", (R, c.max_pages), _I32T, dev), _arg_n(page_tag, "page_tag", c.n_pages, _WORDS, dev),
+             _arg_n(policy_word, "policy_word", R, _WORDS, dev)),
+            (_arg(k_cache, "k_cache", shape, dt, dev), _arg(v_cache, "v_cache", shape, dt, dev),
+             _arg(k_scale, "k_scale", sshape, _U8, dev), _arg(v_scale, "v_scale", sshape, _U8, dev)))
+
+
+def _act_of(c: CacheDesc) -> torch.dtype:
+    if c.act_dtype not in _ACT_T:
+        raise ValueError("the cache's act_dtype must be PMPE_F32 or PMPE_BF16")
+    return _ACT_T[c.act_dtype]
+
+
+def pmpe_kv_write(cache: CacheDesc, k, v, req_offset, seq_len, block_table, page_tag, policy_word, k_cache, v_cache,
+                  k_scale, v_scale, dev_status, stream=None) -> None:
+    """Keys and values [T, n_kv_heads, head_dim] of a batch's tokens into their requests' pages; seq_len [R] counts
+    the new rows already. k and v may be slices of one projection (any stride of tokens)."""
+    dev, R = _here(k, "k"), seq_len.numel()
+    shape, act = (k.shape[0], cache.n_kv_heads, cache.head_dim), _act_of(cache)
+    table, values = _cache_args(cache, R, block_table, page_tag, policy_word, k_cache, v_cache, k_scale, v_scale, dev)
+    _check(_lib.pmpe_kv_write(
+        ctypes.byref(cache), shape[0], R, *_rows(k, "k", shape, act, dev), *_rows(v, "v", shape, act, dev),
+        _arg(req_offset, "req_offset", (R + 1,), _I32T, dev), _arg(seq_len, "seq_len", (R,), _I32T, dev), *table, *values,
+        _arg_n(dev_status, "dev_status", 1, _WORDS, dev), _stream(stream)), "pmpe_kv_write")
+
+
+def pmpe_kv_read(cache: CacheDesc, k, v, req_offset, first, block_table, page_tag, policy_word, k_cache, v_cache,
+                 k_scale, v_scale, dev_status, stream=None) -> None:
+    """Cached rows from position first [R] on (None: 0) into k and v [T, n_kv_heads, head_dim]."""
+    dev, R = _here(k, "k"), req_offset.numel() - 1
+    shape, act = (k.shape[0], cache.n_kv_heads, cache.head_dim), (_act_of(cache),)
+    table, values = _cache_args(cache, R, block_table, page_tag, policy_word, k_cache, v_cache, k_scale, v_scale, dev)
+    _check(_lib.pmpe_kv_read(
+        ctypes.byref(cache), shape[0], R, _arg(k, "k", shape, act, dev), _arg(v, "v", shape, act, dev),
+        _arg(req_offset, "req_offset", (R + 1,), _I32T, dev), _arg(first, "first", (R,), _I32T, dev), *table, *values,
+        _arg_n(dev_status, "dev_status", 1, _WORDS, dev), _stream(stream)), "pmpe_kv_read")
+
+
+def pmpe_attn_decode_workspace_bytes(cache: CacheDesc, R: int, n_heads: int) -> int:
+    return int(_lib.pmpe_attn_decode_workspace_bytes(ctypes.byref(cache), R, n_heads))
+
+
+def pmpe_attn_decode(cache: CacheDesc, q, seq_first, seq_len, block_table, page_tag, policy_word, k_cache, v_cache, k_scale,
+                     v_scale, scale: float, out, lse, dev_status, ws, stream=None) -> None:
+    """Attention of one new token per request, q and out [R, n_heads, head_dim], over its cached rows
+    [seq_first, seq_len); lse [R, n_heads] fp32 or None."""
+    dev, (R, heads) = _here(q, "q"), q.shape[:2]
+    shape, act = (R, heads, cache.head_dim), _act_of(cache)
+    table, values = _cache_args(cache, R, block_table, page_tag, policy_word, k_cache, v_cache, k_scale, v_scale, dev)
+    _check(_lib.pmpe_attn_decode(
+        ctypes.byref(cache), R, heads, *_rows(q, "q", shape, act, dev), _arg(seq_first, "seq_first", (R,), _I32T, dev),
+        _arg(seq_len, "seq_len", (R,), _I32T, dev), *table, *values, scale, _arg(out, "out", shape, (act,), dev),
+        _arg(lse, "lse", (R, heads), _F32, dev), _arg_n(dev_status, "dev_status", 1, _WORDS, dev), *_work(ws, dev),
+        _stream(stream)), "pmpe_attn_decode")
+
+
+def pmpe_sample_workspace_bytes(B: int, V: int) -> int:
+    return int(_lib.pmpe_sample_workspace_bytes(B, V))
+
+
+def pmpe_sample(logits, temperature, top_k, top_p, min_p, u, token, prob, kept, ws, stream=None) -> None:
+    """One token per row of logits [B, V] (fp32 or bf16, rows of any stride) with the row's temperature, top_k, top_p
+    and min_p ([B] each, or None) and uniform number u [B]; prob and kept [B] may be None."""
+    dev, (B, V) = _here(logits, "logits"), logits.shape
+    dt = _dtype(logits, "logits")
+    at, stride = _rows(logits, "logits", (B, V), logits.dtype, dev)
+    _check(_lib.pmpe_sample(
+        B, V, at, dt, stride,
+        _arg(temperature, "temperature", (B,), _F32, dev), _arg(top_k, "top_k", (B,), _I32T, dev),
+        _arg(top_p, "top_p", (B,), _F32, dev), _arg(min_p, "min_p", (B,), _F32, dev), _arg(u, "u", (B,), _F32, dev),
+        _arg(token, "token", (B,), _I32T, dev), _arg(prob, "prob", (B,), _F32, dev), _arg(kept, "kept", (B,), _I32T, dev),
+        *_work(ws, dev), _stream(stream)), "pmpe_sample")

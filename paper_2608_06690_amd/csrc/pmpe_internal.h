@@ -475,6 +475,62 @@ constexpr uint64_t GRAD_PIECE = (uint64_t)1 << 31;  // elements of a piece at mo
 hipError_t launch_grad_norm(const GradListArgs& a, double max_norm, float* norm, double* part, hipStream_t s);
 hipError_t launch_clip_grads(const GradListArgs& a, const float* norm, hipStream_t s);
 
+// The paged cache of a call (pmpe_cache_desc, its tags and the requests' words).
+struct CacheArgs {
+  int R, n_pages, page_size, kv, dim, max_pages, act_bf16, fp8;
+  const int32_t* table;
+  const uint32_t* tag;    // or NULL: no check
+  const uint32_t* words;  // or NULL: every request denies
+  void* k;
+  void* v;
+  uint8_t* ks;            // with fp8
+  uint8_t* vs;
+  uint32_t* dev_status;
+};
+struct KvRowsArgs {
+  CacheArgs c;
+  int T;
+  void* k;  // rows: read by the write, written by the read
+  void* v;
+  int64_t k_stride, v_stride;  // elements
+  const int32_t* offset;
+  const int32_t* at;  // the write's seq_len, the read's first positions (or NULL)
+};
+hipError_t launch_kv_write(const KvRowsArgs& a, hipStream_t s);
+hipError_t launch_kv_read(const KvRowsArgs& a, hipStream_t s);
+
+struct AttnArgs {
+  CacheArgs c;
+  int heads;
+  const void* q;
+  int64_t q_stride;
+  const int32_t* first;  // or NULL
+  const int32_t* len;
+  float scale;
+  void* out;
+  float* lse;            // or NULL
+  float* ws;
+};
+size_t attn_decode_workspace(int R, int heads, const pmpe_cache_desc* c);
+hipError_t launch_attn_decode(const AttnArgs& a, hipStream_t s);
+
+struct SampleArgs {
+  int B, V, bf16;
+  const void* z;
+  int64_t stride;
+  const float* temperature;  // these four or NULL
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+  int32_t* token;
+  float* prob;               // or NULL
+  int32_t* kept;             // or NULL
+  void* ws;
+};
+size_t sample_workspace(int B, int V);
+hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
+
 // Fingerprint tree: 1 KiB leaves, 16 digests per inner node.
 constexpr uint32_t kFpLeafBytes = 1024;
 constexpr uint32_t kFpFanout = 16;
