@@ -2,86 +2,659 @@
 //
 //   s_j = scale q . k_j, out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m), lse = m + ln sum_j exp(s_j - m)
 //
-// A block has one query head of one request; each of its waves goes over every fourth row with a running
-// maximum and sum, lane l holding values l, 64 + l, .. of the head; the waves' parts are joined in LDS.
+// The query heads that share a kv head are the columns of 16 x 16 matrix products: a wave takes a tile of 32 rows of
+// the cache, S^T = K Q^T (rows x heads), then O^T += V^T P^T (dims x heads), with a running maximum and sum per
+// head. Operands come from memory straight into registers: lane l = (g, i) = (l / 16, l % 16) loads 16 bytes of
+// row i for K (the order of dims inside a product is free, Q is laid out alike) and, for V, the dims of chunk i of
+// rows 4 g .. 4 g + 3 and 16 + 4 g .. of the tile: the rows whose weights the lane holds after S^T, so weights go into
+// the second product without leaving their lane, and V^T's pairs of rows are one byte permutation each.
+//
+// The tiles of all requests and heads are one line, cut into equal pieces (a piece a block, its four waves every
+// fourth tile), whatever the lengths; a piece's parts of a request's head that others go on with are joined by a
+// second kernel in the order of the pieces. No atomics: equal calls have equal bits.
 #include "kvcache.h"
 
 namespace pmpe {
 namespace {
 
 constexpr int WAVES = 4;
+constexpr int TILE = 32;        // cache rows of a wave's step
+constexpr int PIECES = 512;     // blocks: two for each CU
+constexpr float LOG2E = 1.4426950408889634f;
 
-__device__ __forceinline__ float cached(const void* cache, const uint8_t* scale, const CacheArgs& c, size_t hp, int row, int d) {
-  const size_t at = (hp * c.page_size + row) * c.dim + d;
-  if (c.fp8) {
-    const uint32_t e = scale[(hp * (c.dim / 32) + d / 32) * c.page_size + row];
-    const float s = __uint_as_float(e == 255 ? 0x7FC00000u : e ? e << 23 : 0x400000u);
-    return __builtin_amdgcn_cvt_f32_fp8(((const uint8_t*)cache)[at], 0) * s;
-  }
-  return c.act_bf16 ? bf16_to_f32(((const uint16_t*)cache)[at]) : ((const float*)cache)[at];
+enum { BF16 = 0, FP8 = 1, F32 = 2 };
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
+// max and sum over lanes l, l ^ 16, l ^ 32 and l ^ 48
+__device__ __forceinline__ float rows_max(float v) {
+  uint32_t u = __float_as_uint(v);
+  auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  u = __float_as_uint(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])));
+  s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float rows_sum(float v) {
+  uint32_t u = __float_as_uint(v);
+  auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  u = __float_as_uint(__uint_as_float(s[0]) + __uint_as_float(s[1]));
+  s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+// 2^(e - 127) of a biased exponent; 255 is NaN
+__device__ __forceinline__ float pow2_of(uint32_t e) { return __uint_as_float(e == 255 ? 0x7FC00000u : e ? e << 23 : 0x400000u); }
+// Two e4m3 values (the word's lower or upper half) times a power of two, to bf16: exact.
+template <bool HI>
+__device__ __forceinline__ uint32_t fp8_to_bf16x2(uint32_t q, float s) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, s, HI));
 }
 
-__global__ __launch_bounds__(64 * WAVES) void attn_kernel(AttnArgs a) {
-  __shared__ float s_m[WAVES], s_l[WAVES], s_o[WAVES][256];
-  const CacheArgs& c = a.c;
-  const int r = blockIdx.x / a.heads, head = blockIdx.x % a.heads, lane = lane_id(), w = threadIdx.x >> 6;
-  const int h = head / (a.heads / c.kv);
-  const int64_t end = a.len[r], first = max(0, a.first ? a.first[r] : 0);
-  const uint32_t want = request_tag(c, r);
-  float q[4], o[4] = {0, 0, 0, 0}, m = -INFINITY, l = 0;
-  uint32_t bad = 0;
-  for (int i = 0; i < 4; ++i) {
-    const int d = i * 64 + lane;
-    const size_t at = (size_t)r * a.q_stride + (size_t)head * c.dim + d;
-    q[i] = d < c.dim ? (c.act_bf16 ? bf16_to_f32(((const uint16_t*)a.q)[at]) : ((const float*)a.q)[at]) : 0.f;
+// The line of tiles: virtual heads (a kv head and up to 16 of its query heads) of request r follow one another.
+struct Split {
+  int groups, rows, vheads;  // parts of a kv head's query heads, heads of a part, virtual heads of a request
+};
+__host__ __device__ inline Split split_of(int heads, int kv) {
+  const int g = heads / kv, parts = (g + 15) / 16;
+  return {parts, (g + parts - 1) / parts, kv * parts};
+}
+// Rows of a request: [first, end), its tiles.
+struct Rows {
+  int first, end, t0, n;
+};
+__device__ __forceinline__ Rows rows_of(const AttnArgs& a, int r) {
+  const int most = a.c.max_pages * a.c.page_size, first = a.first ? max(0, a.first[r]) : 0, end = min(a.len[r], most);
+  if (end <= first) return {first, end, 0, 0};
+  return {first, end, first / TILE, (end + TILE - 1) / TILE - first / TILE};
+}
+
+struct Part {  // workspace of the pieces
+  float* o;     // [2 PIECES][16][dim]
+  float* ml;    // [2 PIECES][16][2]
+  int32_t* at;  // [R * vheads][2]: first and last piece of a request's virtual head
+};
+__host__ __device__ inline Part part_of(float* ws, int rows, int dim) {
+  float* ml = ws + (size_t)2 * PIECES * rows * dim;
+  return {ws, ml, (int32_t*)(ml + (size_t)2 * PIECES * rows * 2)};
+}
+
+template <int T, int NB>
+struct Tile {
+  static constexpr int D = 32 * NB;
+  static constexpr int NK = T == BF16 ? NB : T == FP8 ? (NB + 1) / 2 : 2 * NB;  // 16-byte loads of a K row's quarter
+  static constexpr int SEGS = NB / 4 + ((NB & 2) != 0) + (NB & 1);            // V: 128, 64 and 32 dims
+  static constexpr int VW = T == BF16 ? D / 32 : T == FP8 ? (D + 63) / 64 : D / 16;  // words of V per row and lane
+  u32x4 k[2][NK];
+  uint32_t ks[2][T == FP8 ? NK : 1];
+  uint32_t v[8][VW];
+  uint32_t vs[2][T == FP8 ? SEGS : 1];
+};
+// base dim and width of segment j
+template <int NB>
+__device__ constexpr int seg_base(int j) {
+  return j <= NB / 4 ? (j < NB / 4 ? 128 * j : 128 * (NB / 4)) : 128 * (NB / 4) + 64 * ((NB & 2) != 0);
+}
+template <int NB>
+__device__ constexpr int seg_width(int j) {
+  return j < NB / 4 ? 128 : (NB & 2) && j == NB / 4 ? 64 : 32;
+}
+
+template <int T, int NB, bool SPLIT_ROWS>
+struct Wave {
+  static constexpr int D = 32 * NB, EL = T == BF16 ? 2 : T == FP8 ? 1 : 4;
+  typedef Tile<T, NB> TileT;
+  const AttnArgs& a;
+  const int lane, i, g;
+  int r, h;             // request, kv head
+  Rows rows;
+  TileT t;
+  u32x4 q[T == F32 ? 2 * NB : NB];
+  f32x4 o[2 * NB];
+  float m, l;
+  int pages, prow;      // lane 2 n + u: page and row of half u of the wave's n-th tile from `from` on
+  int from;             // index of a tile (in steps of the wave)
+  uint32_t bad;
+
+  __device__ Wave(const AttnArgs& args) : a(args), lane(lane_id()), i(lane & 15), g(lane >> 4), bad(0) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int s = 0; s < TileT::NK; ++s) t.k[u][s] = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < (T == FP8 ? TileT::NK : 1); ++s) t.ks[u][s] = 0;
+#pragma unroll
+      for (int s = 0; s < (T == FP8 ? TileT::SEGS : 1); ++s) t.vs[u][s] = 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int w = 0; w < TileT::VW; ++w) t.v[j][w] = 0;
   }
-  const int64_t most = (int64_t)c.max_pages * c.page_size;
-  if (end > most) bad |= PMPE_DEV_CACHE_RANGE;
-  for (int64_t p = first + w; p < min(end, most); p += WAVES) {
-    const int page = page_at(c, r, p / c.page_size, want, bad);
-    if (page < 0) continue;
-    const int row = (int)(p % c.page_size);
-    const size_t hp = (size_t)page * c.kv + h;
-    float dot = 0;
-    for (int i = 0; i * 64 < c.dim; ++i)
-      if (i * 64 + lane < c.dim) dot += q[i] * cached(c.k, c.ks, c, hp, row, i * 64 + lane);
-    const float s = wave_sum(dot) * a.scale, mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - mn);
-    const float e = mn == -INFINITY ? 0.f : expf(s - mn);
-    l = l * f + e;
-    for (int i = 0; i * 64 < c.dim; ++i)
-      if (i * 64 + lane < c.dim) o[i] = o[i] * f + e * cached(c.v, c.vs, c, hp, row, i * 64 + lane);
-    m = mn;
+
+  // Q of the virtual head: column i is query head h0 + (i, or i % 8: its copy for the weights' lower parts).
+  __device__ void begin(int request, int kv_head, int head0, int n_heads) {
+    r = request;
+    h = kv_head;
+    rows = rows_of(a, r);
+    const int col = SPLIT_ROWS ? i & 7 : i;
+    const char* at = (const char*)a.q + ((size_t)r * a.q_stride + (size_t)(head0 + col) * D) * (T == F32 ? 4 : 2);
+#pragma unroll
+    for (int s = 0; s < (T == F32 ? 2 * NB : NB); ++s) {
+      int d;
+      if (T == BF16) d = s * 32 + g * 8;
+      else if (T == F32) d = s * 16 + g * 4;
+      else d = (NB & 1) && s == NB - 1 ? s * 32 + g * 8 : (s / 2) * 64 + g * 16 + (s & 1) * 8;
+      q[s] = col < n_heads ? *(const u32x4*)(at + (size_t)d * (T == F32 ? 4 : 2)) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * NB; ++j) o[j] = f32x4{0, 0, 0, 0};
+    m = -INFINITY;
+    l = 0.f;
   }
-  if (lane == 0) {
-    s_m[w] = m;
-    s_l[w] = l;
-    report(c, bad);
+
+  // Pages of the wave's tiles first_tile + 4 n, n = 0 .. 31.
+  __device__ void look_up(int first_tile) {
+    const CacheArgs& c = a.c;
+    const int p = (first_tile + WAVES * (lane >> 1)) * TILE + (lane & 1) * 16;
+    pages = -1;
+    prow = 0;
+    if (p < rows.end && p + 16 > rows.first) {
+      const int col = p / c.page_size;
+      pages = page_at(c, r, col, request_tag(c, r), bad);
+      prow = p - col * c.page_size;
+    }
   }
-  for (int i = 0; i < 4; ++i) s_o[w][i * 64 + lane] = o[i];
+
+  __device__ const char* half(const void* cache, int n, int u, int page) const {
+    const CacheArgs& c = a.c;
+    return (const char*)cache + (((size_t)page * c.kv + h) * c.page_size + __builtin_amdgcn_readlane(prow, 2 * n + u)) * (D * EL);
+  }
+  __device__ const uint8_t* scales(const uint8_t* s, int n, int u, int page) const {
+    const CacheArgs& c = a.c;
+    return s + ((size_t)page * c.kv + h) * NB * c.page_size + __builtin_amdgcn_readlane(prow, 2 * n + u);
+  }
+  __device__ void load_k(int n) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int page = __builtin_amdgcn_readlane(pages, 2 * n + u);
+      if (page < 0) continue;
+      const char* at = half(a.c.k, n, u, page);
+      const uint32_t off = i * (D * EL) + g * 16;
+#pragma unroll
+      for (int s = 0; s < TileT::NK; ++s) {
+        if (T == FP8 && (NB & 1) && s == TileT::NK - 1) {
+          const u32x2 x = *(const u32x2*)(at + (i * (D * EL) + g * 8 + s * 64));
+          t.k[u][s][0] = x[0];
+          t.k[u][s][1] = x[1];
+        } else {
+          t.k[u][s] = *(const u32x4*)(at + (off + s * 64));
+        }
+      }
+      if constexpr (T == FP8) {
+        const uint8_t* sc = scales(a.c.ks, n, u, page);
+#pragma unroll
+        for (int s = 0; s < TileT::NK; ++s)
+          t.ks[u][s] = sc[((NB & 1) && s == TileT::NK - 1 ? 2 * s : 2 * s + (g >> 1)) * a.c.page_size + i];
+      }
+    }
+  }
+  __device__ void load_v(int n) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int page = __builtin_amdgcn_readlane(pages, 2 * n + u);
+      if (page < 0) continue;
+      const char* at = half(a.c.v, n, u, page);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        int w = 0;
+#pragma unroll
+        for (int sg = 0; sg < TileT::SEGS; ++sg) {
+          const int width = seg_width<NB>(sg), per = width / 16 * EL;  // bytes of a lane
+          const char* p = at + ((uint32_t)((g * 4 + j) * (D * EL) + i * per) + seg_base<NB>(sg) * EL);
+          uint32_t* to = t.v[4 * u + j] + w;
+          if (per == 32) {
+            const u32x4 x = *(const u32x4*)p, y = *(const u32x4*)(p + 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              to[e] = x[e];
+              to[4 + e] = y[e];
+            }
+          } else if (per == 16) {
+            const u32x4 x = *(const u32x4*)p;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[e] = x[e];
+          } else if (per == 8) {
+            const u32x2 x = *(const u32x2*)p;
+            to[0] = x[0];
+            to[1] = x[1];
+          } else if (per == 4) {
+            to[0] = *(const uint32_t*)p;
+          } else {
+            to[0] = *(const uint16_t*)p;
+          }
+          w += (per + 3) / 4;
+        }
+      }
+      if constexpr (T == FP8) {
+        const uint8_t* sc = scales(a.c.vs, n, u, page);
+#pragma unroll
+        for (int sg = 0; sg < TileT::SEGS; ++sg) {
+          const int width = seg_width<NB>(sg);
+          const int blk = seg_base<NB>(sg) / 32 + (width == 128 ? i >> 2 : width == 64 ? i >> 3 : 0);
+          t.vs[u][sg] = *(const uint32_t*)(sc + (uint32_t)(blk * a.c.page_size + g * 4));
+        }
+      }
+    }
+  }
+
+  // S^T of half u: lane (g, i) gets rows 4 g .. 4 g + 3 of column i
+  __device__ f32x4 scores(int u) const {
+    f32x4 s = {0, 0, 0, 0};
+    if constexpr (T == BF16) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(t.k[u][j]), as_bf16x8(q[j]), s, 0, 0, 0);
+    } else if constexpr (T == FP8) {
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const float f = pow2_of(t.ks[u][j / 2]);
+        const uint32_t x = t.k[u][j / 2][(j & 1) * 2], y = t.k[u][j / 2][(j & 1) * 2 + 1];
+        const u32x4 k = {fp8_to_bf16x2<false>(x, f), fp8_to_bf16x2<true>(x, f), fp8_to_bf16x2<false>(y, f), fp8_to_bf16x2<true>(y, f)};
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k), as_bf16x8(q[j]), s, 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 2 * NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          s = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[u][j][e]), __uint_as_float(q[j][e]), s, 0, 0, 0);
+    }
+    return s;
+  }
+
+  // O^T += V^T P^T with weights p[u][e] of row 16 u + 4 g + e
+  __device__ void accumulate(const float (&p)[8]) {
+    if constexpr (T == F32) {
+      int w = 0, n = 0;
+#pragma unroll
+      for (int sg = 0; sg < TileT::SEGS; ++sg) {
+        const int per = seg_width<NB>(sg) / 16;
+#pragma unroll
+        for (int d = 0; d < per; ++d, ++n)
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            o[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[j][w + d]), p[j], o[n], 0, 0, 0);
+        w += per;
+      }
+    } else {
+      // A weight as the sum of two bf16 values: one alone is off by 2^-9, more than the sums and the output's rounding
+      // leave where many rows cancel. With up to 8 heads the lower parts are columns 8 .. 15 of the same product.
+      u32x4 hi, lo;
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = p[j] - (float)(__bf16)p[j];
+      if constexpr (SPLIT_ROWS) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = i < 8 ? p[j] : x[j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) hi[j] = pk_bf16(x[2 * j], x[2 * j + 1]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          hi[j] = pk_bf16(p[2 * j], p[2 * j + 1]);
+          lo[j] = pk_bf16(x[2 * j], x[2 * j + 1]);
+        }
+      }
+      int w = 0, n = 0;
+#pragma unroll
+      for (int sg = 0; sg < TileT::SEGS; ++sg) {
+        const int pairs = seg_width<NB>(sg) / 32;  // pairs of dims of a lane
+        uint32_t v[8][4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (T == BF16) {
+#pragma unroll
+            for (int e = 0; e < pairs; ++e) v[j][e] = t.v[j][w + e];
+          } else {
+            const float f = pow2_of((t.vs[j >> 2][sg] >> (8 * (j & 3))) & 0xFFu);
+#pragma unroll
+            for (int e = 0; e < pairs; ++e)
+              v[j][e] = e & 1 ? fp8_to_bf16x2<true>(t.v[j][w + e / 2], f) : fp8_to_bf16x2<false>(t.v[j][w + e / 2], f);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < pairs; ++e)
+#pragma unroll
+          for (int odd = 0; odd < 2; ++odd, ++n) {
+            u32x4 vt;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vt[j] = __builtin_amdgcn_perm(v[2 * j + 1][e], v[2 * j][e], odd ? 0x07060302u : 0x05040100u);
+            o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt), as_bf16x8(hi), o[n], 0, 0, 0);
+            if constexpr (!SPLIT_ROWS) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt), as_bf16x8(lo), o[n], 0, 0, 0);
+          }
+        w += T == BF16 ? pairs : (pairs + 1) / 2;
+      }
+    }
+  }
+
+  // Tile `tile` (the n-th looked up), whose K and V are loaded; loads those of tile n + 1 where there is one.
+  __device__ void step(int tile, int n, bool more) {
+    float s[8];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f32x4 x = scores(u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[4 * u + e] = x[e] * (a.scale * LOG2E);
+    }
+    const int p0 = tile * TILE, pg0 = __builtin_amdgcn_readlane(pages, 2 * n), pg1 = __builtin_amdgcn_readlane(pages, 2 * n + 1);
+    if (more) load_k(n + 1);
+    const bool whole = pg0 >= 0 && pg1 >= 0 && p0 >= rows.first && p0 + TILE <= rows.end;
+    if (!whole) {
+      // rows that take no part: their weights are 0, and so is V there (0 times what memory holds may be NaN)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int p = p0 + (j >> 2) * 16 + g * 4 + (j & 3);
+        const bool in = (j < 4 ? pg0 : pg1) >= 0 && p >= rows.first && p < rows.end;
+        s[j] = in ? s[j] : -INFINITY;
+#pragma unroll
+        for (int w = 0; w < TileT::VW; ++w) t.v[j][w] = in ? t.v[j][w] : 0u;
+        if constexpr (T == FP8) {
+#pragma unroll
+          for (int sg = 0; sg < TileT::SEGS; ++sg)
+            t.vs[j >> 2][sg] = in ? t.vs[j >> 2][sg] : t.vs[j >> 2][sg] & ~(0xFFu << (8 * (j & 3)));
+        }
+      }
+    }
+    float top = s[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+    top = rows_max(top);
+    if (__any(top > m)) {
+      const float mn = fmaxf(m, top), f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int j = 0; j < 2 * NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    float p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(s[j] - ref);
+    l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    accumulate(p);
+    if (more) load_v(n + 1);
+  }
+
+  // Tiles first, first + 4, .. below last.
+  __device__ void run(int first, int last) {
+    for (int tile = first; tile < last;) {
+      look_up(tile);
+      load_k(0);
+      load_v(0);
+      for (int n = 0; n < 32 && tile < last; ++n, tile += WAVES) step(tile, n, n < 31 && tile + WAVES < last);
+    }
+    l = rows_sum(l);
+    if constexpr (SPLIT_ROWS && T != F32) {
+#pragma unroll
+      for (int j = 0; j < 2 * NB; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[j][e] += __uint_as_float(xor_lanes(__float_as_uint(o[j][e]), 8));
+    }
+  }
+};
+
+template <int NB>
+struct Lds {
+  float ml[WAVES][16][2];
+  float o[WAVES][16][32 * NB + 4];
+};
+
+// The waves' parts of a virtual head joined: the output if `whole`, else the piece's part.
+template <int T, int NB, bool SPLIT_ROWS>
+__device__ void finish(Wave<T, NB, SPLIT_ROWS>& w, Lds<NB>& lds, int head0, int n_heads, bool whole, const Part& part, int slot, int slot_rows) {
+  constexpr int D = 32 * NB;
+  const AttnArgs& a = w.a;
+  const int wave = threadIdx.x >> 6;
+  if (w.g == 0) {
+    lds.ml[wave][w.i][0] = w.m;
+    lds.ml[wave][w.i][1] = w.l;
+  }
   __syncthreads();
-  float M = -INFINITY, L = 0, O = 0;
-  for (int i = 0; i < WAVES; ++i) M = fmaxf(M, s_m[i]);
-  for (int i = 0; i < WAVES; ++i) {
-    const float f = s_m[i] == -INFINITY ? 0.f : expf(s_m[i] - M);
-    L += s_l[i] * f;
-    O += s_o[i][threadIdx.x] * f;
+  float M = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < WAVES; ++j) M = fmaxf(M, lds.ml[j][w.i][0]);
+  const float f = w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m - M);
+  if (w.i < n_heads) {
+    float* to = lds.o[wave][w.i];
+    int n = 0;
+#pragma unroll
+    for (int sg = 0; sg < Tile<T, NB>::SEGS; ++sg) {
+      const int per = seg_width<NB>(sg) / 16;
+#pragma unroll
+      for (int d = 0; d < per; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[seg_base<NB>(sg) + (w.g * 4 + e) * per + d] = w.o[n + d][e] * f;
+      n += per;
+    }
   }
-  if ((int)threadIdx.x < c.dim) {
-    const size_t at = ((size_t)r * a.heads + head) * c.dim + threadIdx.x;
-    const float v = L == 0.f ? 0.f : O / L;
-    if (c.act_bf16) ((uint16_t*)a.out)[at] = (uint16_t)f32_to_bf16_rne(v);
-    else ((float*)a.out)[at] = v;
+  __syncthreads();
+  for (int x = threadIdx.x * 4; x < n_heads * D; x += 4 * 64 * WAVES) {
+    const int head = x / D, d = x % D;
+    float L = 0.f, Mh = -INFINITY;
+    f32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < WAVES; ++j) Mh = fmaxf(Mh, lds.ml[j][head][0]);
+#pragma unroll
+    for (int j = 0; j < WAVES; ++j) {
+      const float mj = lds.ml[j][head][0];
+      L += lds.ml[j][head][1] * (mj == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mj - Mh));
+      v += *(const f32x4*)&lds.o[j][head][d];
+    }
+    if (whole) {
+      const size_t at = ((size_t)w.r * a.heads + head0 + head) * D + d;
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      v = L == 0.f ? f32x4{0, 0, 0, 0} : v * inv;
+      if (T == F32) *(f32x4*)((float*)a.out + at) = v;
+      else *(u32x2*)((uint16_t*)a.out + at) = u32x2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+      if (a.lse && d == 0) a.lse[(size_t)w.r * a.heads + head0 + head] = L == 0.f ? -INFINITY : (Mh + log2f(L)) * 0.6931471805599453f;
+    } else {
+      *(f32x4*)(part.o + ((size_t)slot * slot_rows + head) * D + d) = v;
+      if (d == 0) {
+        part.ml[((size_t)slot * slot_rows + head) * 2] = Mh;
+        part.ml[((size_t)slot * slot_rows + head) * 2 + 1] = L;
+      }
+    }
   }
-  if (threadIdx.x == 0 && a.lse) a.lse[(size_t)r * a.heads + head] = L == 0.f ? -INFINITY : M + logf(L);
+  __syncthreads();  // read before the next virtual head's waves write
+}
+
+// DIRECT: a block has a whole virtual head.
+template <int T, int NB, bool SPLIT_ROWS, bool DIRECT>
+__global__ __launch_bounds__(64 * WAVES, (T == F32 ? NB <= 2 : NB <= 4) ? 2 : 1) void attn_kernel(AttnArgs a) {
+  __shared__ Lds<NB> lds;
+  __shared__ int64_t s_scan[WAVES], s_base;
+  __shared__ int s_r;
+  const Split sp = split_of(a.heads, a.c.kv);
+  const Part part = part_of(a.ws, sp.rows, 32 * NB);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
+  Wave<T, NB, SPLIT_ROWS> w(a);
+  const int group = a.heads / a.c.kv;
+  const auto heads_of = [&](int vh, int& kv, int& head0, int& n) {
+    kv = vh / sp.groups;
+    const int p = vh - kv * sp.groups;
+    head0 = kv * group + p * sp.rows;
+    n = min(sp.rows, group - p * sp.rows);
+  };
+  int kv, head0, n_heads;
+  if constexpr (DIRECT) {
+    const int r = blockIdx.x / sp.vheads;
+    heads_of(blockIdx.x - r * sp.vheads, kv, head0, n_heads);
+    w.begin(r, kv, head0, n_heads);
+    w.run(w.rows.t0 + wave, w.rows.t0 + w.rows.n);
+    finish<T, NB, SPLIT_ROWS>(w, lds, head0, n_heads, true, part, 0, sp.rows);
+  } else {
+    // tiles of the requests ahead: thread x sums those of requests [x c, (x + 1) c)
+    const int c = (a.c.R + 64 * WAVES - 1) / (64 * WAVES), r0 = threadIdx.x * c, r1 = min(a.c.R, r0 + c);
+    int64_t mine = 0;
+    for (int r = r0; r < r1; ++r) mine += rows_of(a, r).n;
+    int64_t upto = mine;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int64_t v = __shfl_up(upto, off, 64);
+      if (lane >= off) upto += v;
+    }
+    if (lane == 63) s_scan[wave] = upto;
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int j = 0; j < WAVES; ++j) {
+      if (j < wave) upto += s_scan[j];
+      total += s_scan[j];
+    }
+    total *= sp.vheads;
+    // a piece has a tile for each wave at least
+    int64_t per = (total + gridDim.x - 1) / gridDim.x;
+    per = max((int64_t)WAVES, (per + WAVES - 1) / WAVES * WAVES);
+    const int64_t x0 = blockIdx.x * per, x1 = min(total, x0 + per);
+    if (x0 >= x1) return;
+    if ((upto - mine) * sp.vheads <= x0 && x0 < upto * sp.vheads) {  // one thread
+      int64_t base = upto - mine;
+      int r = r0;
+      for (int n = rows_of(a, r).n; (base + n) * sp.vheads <= x0; n = rows_of(a, r).n) {
+        base += n;
+        ++r;
+      }
+      s_r = r;
+      s_base = base;
+    }
+    __syncthreads();
+    int r = s_r;
+    int64_t base = s_base * sp.vheads;  // first tile of request r
+    for (int64_t x = x0; x < x1;) {
+      const int n = rows_of(a, r).n;
+      if (x >= base + (int64_t)n * sp.vheads) {
+        base += (int64_t)n * sp.vheads;
+        ++r;
+        continue;
+      }
+      const int vh = (int)((x - base) / n);
+      const int64_t s0 = base + (int64_t)vh * n, s1 = s0 + n;  // the virtual head's tiles
+      const int64_t end = min(s1, x1);
+      heads_of(vh, kv, head0, n_heads);
+      w.begin(r, kv, head0, n_heads);
+      w.run(w.rows.t0 + (int)(x - s0) + wave, w.rows.t0 + (int)(end - s0));
+      const bool whole = x == s0 && end == s1;
+      finish<T, NB, SPLIT_ROWS>(w, lds, head0, n_heads, whole, part, 2 * blockIdx.x + (s0 >= x0), sp.rows);
+      if (x == s0 && threadIdx.x == 0) {
+        part.at[((size_t)r * sp.vheads + vh) * 2] = blockIdx.x;
+        part.at[((size_t)r * sp.vheads + vh) * 2 + 1] = (int)((s1 - 1) / per);
+      }
+      x = end;
+    }
+  }
+  if (lane == 0 && w.rows.end < a.len[w.r]) w.bad |= PMPE_DEV_CACHE_RANGE;
+  report(a.c, w.bad);
+}
+
+// The pieces' parts of one query head, in order; requests without a row get their zeros here.
+template <bool BF16_OUT>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  __shared__ float s_o[256][4], s_l[256];
+  const Split sp = split_of(a.heads, a.c.kv);
+  const int D = a.c.dim, r = blockIdx.x / a.heads, head = blockIdx.x - r * a.heads, tid = threadIdx.x;
+  const size_t at = (size_t)r * a.heads + head;
+  const auto store = [&](int d, f32x4 v) {
+    if (BF16_OUT) *(u32x2*)((uint16_t*)a.out + at * D + d) = u32x2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+    else *(f32x4*)((float*)a.out + at * D + d) = v;
+  };
+  const Rows rows = rows_of(a, r);
+  if (tid == 0 && head == 0 && a.len[r] > rows.end) report(a.c, PMPE_DEV_CACHE_RANGE);
+  if (rows.n == 0) {
+    if (tid * 4 < D) store(tid * 4, f32x4{0, 0, 0, 0});
+    if (tid == 0 && a.lse) a.lse[at] = -INFINITY;
+    return;
+  }
+  const Part part = part_of(a.ws, sp.rows, D);
+  const int group = a.heads / a.c.kv, kv = head / group, in_kv = head - kv * group, p = in_kv / sp.rows, row = in_kv - p * sp.rows;
+  const int32_t* which = part.at + ((size_t)r * sp.vheads + kv * sp.groups + p) * 2;
+  const int j0 = which[0], j1 = which[1];
+  if (j0 == j1) return;  // a piece had it whole
+  const int per = D / 4, lanes = 256 / per, mine = tid / per, d = (tid - mine * per) * 4;
+  float M = -INFINITY;
+  for (int j = j0; j <= j1; ++j) M = fmaxf(M, part.ml[((size_t)(2 * j + (j == j0)) * sp.rows + row) * 2]);
+  f32x4 v = {0, 0, 0, 0};
+  float L = 0.f;
+  if (mine < lanes)
+    for (int j = j0 + mine; j <= j1; j += lanes) {
+      const size_t slot = (size_t)(2 * j + (j == j0)) * sp.rows + row;
+      const float m = part.ml[slot * 2], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+      L += part.ml[slot * 2 + 1] * f;
+      v += *(const f32x4*)(part.o + slot * D + d) * f;
+    }
+  *(f32x4*)s_o[tid] = v;
+  s_l[tid] = L;
+  __syncthreads();
+  if (mine > 0) return;
+  for (int j = 1; j < lanes; ++j) {
+    v += *(const f32x4*)s_o[j * per + tid];
+    L += s_l[j * per + tid];
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  store(d, L == 0.f ? f32x4{0, 0, 0, 0} : v * inv);
+  if (tid == 0 && a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+}
+
+// Requests whose tables hold a tile for each wave at most are whole blocks; longer ones go by pieces.
+bool direct(int max_pages, int page_size) { return (int64_t)max_pages * page_size <= WAVES * TILE; }
+
+template <int T, int NB>
+hipError_t launch(const AttnArgs& a, hipStream_t s) {
+  const Split sp = split_of(a.heads, a.c.kv);
+  const bool d = direct(a.c.max_pages, a.c.page_size);
+  const int grid = d ? a.c.R * sp.vheads : PIECES;
+  if (sp.rows <= 8) {
+    if (d) attn_kernel<T, NB, true, true><<<grid, 64 * WAVES, 0, s>>>(a);
+    else attn_kernel<T, NB, true, false><<<grid, 64 * WAVES, 0, s>>>(a);
+  } else {
+    if (d) attn_kernel<T, NB, false, true><<<grid, 64 * WAVES, 0, s>>>(a);
+    else attn_kernel<T, NB, false, false><<<grid, 64 * WAVES, 0, s>>>(a);
+  }
+  if (!d) {
+    if (T == F32) attn_join_kernel<false><<<a.c.R * a.heads, 256, 0, s>>>(a);
+    else attn_join_kernel<true><<<a.c.R * a.heads, 256, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <int T>
+hipError_t launch_type(const AttnArgs& a, hipStream_t s) {
+  switch (a.c.dim / 32) {
+    case 1: return launch<T, 1>(a, s);
+    case 2: return launch<T, 2>(a, s);
+    case 3: return launch<T, 3>(a, s);
+    case 4: return launch<T, 4>(a, s);
+    case 5: return launch<T, 5>(a, s);
+    case 6: return launch<T, 6>(a, s);
+    case 7: return launch<T, 7>(a, s);
+    default: return launch<T, 8>(a, s);
+  }
 }
 
 }  // namespace
 
-size_t attn_decode_workspace(int, int, const pmpe_cache_desc*) { return 0; }
+size_t attn_decode_workspace(int R, int heads, const pmpe_cache_desc* c) {
+  if (R == 0 || direct(c->max_pages, c->page_size)) return 0;
+  const Split sp = split_of(heads, c->n_kv_heads);
+  return ((size_t)2 * PIECES * sp.rows * (c->head_dim + 2) + (size_t)R * sp.vheads * 2) * 4;
+}
 
 hipError_t launch_attn_decode(const AttnArgs& a, hipStream_t s) {
-  attn_kernel<<<a.c.R * a.heads, 64 * WAVES, 0, s>>>(a);
-  return hipGetLastError();
+  if (a.c.fp8) return launch_type<FP8>(a, s);
+  return a.c.act_bf16 ? launch_type<BF16>(a, s) : launch_type<F32>(a, s);
 }
 
 }  // namespace pmpe
