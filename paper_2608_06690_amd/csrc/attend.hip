@@ -19,7 +19,7 @@ namespace {
 
 constexpr int WAVES = 4;
 constexpr int TILE = 32;        // cache rows of a wave's step
-constexpr int PIECES = 512;     // blocks: two for each CU
+constexpr int PIECES = 1024;    // at most
 constexpr float LOG2E = 1.4426950408889634f;
 
 enum { BF16 = 0, FP8 = 1, F32 = 2 };
@@ -71,10 +71,25 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs& a, int r) {
   return {first, end, first / TILE, (end + TILE - 1) / TILE - first / TILE};
 }
 
+// Waves of a SIMD that the registers of a wave leave room for.
+__host__ __device__ constexpr int waves_per_simd(int type, int nb) {
+  return type == F32 ? (nb <= 1 ? 4 : nb == 2 ? 3 : nb == 3 ? 2 : 1) : nb <= 2 ? 4 : nb <= 4 ? 3 : nb <= 6 ? 2 : 1;
+}
+
+// The same of a request that the whole wave has, and a wave's own value of 64 bits, in scalar registers.
+__device__ __forceinline__ Rows uniform_rows_of(const AttnArgs& a, int r) {
+  const Rows v = rows_of(a, r);
+  return {__builtin_amdgcn_readfirstlane(v.first), __builtin_amdgcn_readfirstlane(v.end), __builtin_amdgcn_readfirstlane(v.t0),
+          __builtin_amdgcn_readfirstlane(v.n)};
+}
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+
 struct Part {  // workspace of the pieces
   float* o;     // [2 PIECES][16][dim]
   float* ml;    // [2 PIECES][16][2]
-  int32_t* at;  // [R * vheads][2]: first and last piece of a request's virtual head
+  int32_t* next;  // [PIECES][4]: request, virtual head and last piece of what a piece leaves unfinished (request -1: nothing)
 };
 __host__ __device__ inline Part part_of(float* ws, int rows, int dim) {
   float* ml = ws + (size_t)2 * PIECES * rows * dim;
@@ -138,7 +153,8 @@ struct Wave {
   __device__ void begin(int request, int kv_head, int head0, int n_heads) {
     r = request;
     h = kv_head;
-    rows = rows_of(a, r);
+    rows = uniform_rows_of(a, r);
+    if (rows.end < a.len[r]) bad |= PMPE_DEV_CACHE_RANGE;
     const int col = SPLIT_ROWS ? i & 7 : i;
     const char* at = (const char*)a.q + ((size_t)r * a.q_stride + (size_t)(head0 + col) * D) * (T == F32 ? 4 : 2);
 #pragma unroll
@@ -311,29 +327,28 @@ struct Wave {
 #pragma unroll
       for (int sg = 0; sg < TileT::SEGS; ++sg) {
         const int pairs = seg_width<NB>(sg) / 32;  // pairs of dims of a lane
-        uint32_t v[8][4];
+        float f[8];
+        if constexpr (T == FP8) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if constexpr (T == BF16) {
-#pragma unroll
-            for (int e = 0; e < pairs; ++e) v[j][e] = t.v[j][w + e];
-          } else {
-            const float f = pow2_of((t.vs[j >> 2][sg] >> (8 * (j & 3))) & 0xFFu);
-#pragma unroll
-            for (int e = 0; e < pairs; ++e)
-              v[j][e] = e & 1 ? fp8_to_bf16x2<true>(t.v[j][w + e / 2], f) : fp8_to_bf16x2<false>(t.v[j][w + e / 2], f);
-          }
+          for (int j = 0; j < 8; ++j) f[j] = pow2_of((t.vs[j >> 2][sg] >> (8 * (j & 3))) & 0xFFu);
         }
 #pragma unroll
-        for (int e = 0; e < pairs; ++e)
+        for (int e = 0; e < pairs; ++e) {
+          uint32_t v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            if constexpr (T == BF16) v[j] = t.v[j][w + e];
+            else v[j] = e & 1 ? fp8_to_bf16x2<true>(t.v[j][w + e / 2], f[j]) : fp8_to_bf16x2<false>(t.v[j][w + e / 2], f[j]);
+          }
 #pragma unroll
           for (int odd = 0; odd < 2; ++odd, ++n) {
             u32x4 vt;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) vt[j] = __builtin_amdgcn_perm(v[2 * j + 1][e], v[2 * j][e], odd ? 0x07060302u : 0x05040100u);
+            for (int j = 0; j < 4; ++j) vt[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], odd ? 0x07060302u : 0x05040100u);
             o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt), as_bf16x8(hi), o[n], 0, 0, 0);
             if constexpr (!SPLIT_ROWS) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt), as_bf16x8(lo), o[n], 0, 0, 0);
           }
+        }
         w += T == BF16 ? pairs : (pairs + 1) / 2;
       }
     }
@@ -474,7 +489,7 @@ __device__ void finish(Wave<T, NB, SPLIT_ROWS>& w, Lds<NB>& lds, int head0, int 
 
 // DIRECT: a block has a whole virtual head.
 template <int T, int NB, bool SPLIT_ROWS, bool DIRECT>
-__global__ __launch_bounds__(64 * WAVES, (T == F32 ? NB <= 2 : NB <= 4) ? 2 : 1) void attn_kernel(AttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES, waves_per_simd(T, NB)) void attn_kernel(AttnArgs a) {
   __shared__ Lds<NB> lds;
   __shared__ int64_t s_scan[WAVES], s_base;
   __shared__ int s_r;
@@ -515,11 +530,26 @@ __global__ __launch_bounds__(64 * WAVES, (T == F32 ? NB <= 2 : NB <= 4) ? 2 : 1)
       if (j < wave) upto += s_scan[j];
       total += s_scan[j];
     }
-    total *= sp.vheads;
+    total = uniform(total) * sp.vheads;
     // a piece has a tile for each wave at least
     int64_t per = (total + gridDim.x - 1) / gridDim.x;
     per = max((int64_t)WAVES, (per + WAVES - 1) / WAVES * WAVES);
     const int64_t x0 = blockIdx.x * per, x1 = min(total, x0 + per);
+    int32_t* next = part.next + 4 * blockIdx.x;
+    if (threadIdx.x == 0 && (x1 <= x0 || x1 == total)) next[0] = -1;
+    // requests without a row
+    for (int r = blockIdx.x; r < a.c.R; r += gridDim.x) {
+      const Rows rows = rows_of(a, r);
+      if (rows.n > 0) continue;
+      if (threadIdx.x == 0 && rows.end < a.len[r]) report(a.c, PMPE_DEV_CACHE_RANGE);
+      const size_t at = (size_t)r * a.heads;
+      for (int x = threadIdx.x * 4; x < a.heads * 32 * NB; x += 4 * 64 * WAVES) {
+        if (T == F32) *(f32x4*)((float*)a.out + at * 32 * NB + x) = f32x4{0, 0, 0, 0};
+        else *(u32x2*)((uint16_t*)a.out + at * 32 * NB + x) = u32x2{0, 0};
+      }
+      if (a.lse)
+        for (int x = threadIdx.x; x < a.heads; x += 64 * WAVES) a.lse[at + x] = -INFINITY;
+    }
     if (x0 >= x1) return;
     if ((upto - mine) * sp.vheads <= x0 && x0 < upto * sp.vheads) {  // one thread
       int64_t base = upto - mine;
@@ -532,10 +562,10 @@ __global__ __launch_bounds__(64 * WAVES, (T == F32 ? NB <= 2 : NB <= 4) ? 2 : 1)
       s_base = base;
     }
     __syncthreads();
-    int r = s_r;
-    int64_t base = s_base * sp.vheads;  // first tile of request r
+    int r = __builtin_amdgcn_readfirstlane(s_r);
+    int64_t base = uniform(s_base) * sp.vheads;  // first tile of request r
     for (int64_t x = x0; x < x1;) {
-      const int n = rows_of(a, r).n;
+      const int n = uniform_rows_of(a, r).n;
       if (x >= base + (int64_t)n * sp.vheads) {
         base += (int64_t)n * sp.vheads;
         ++r;
@@ -549,62 +579,74 @@ __global__ __launch_bounds__(64 * WAVES, (T == F32 ? NB <= 2 : NB <= 4) ? 2 : 1)
       w.run(w.rows.t0 + (int)(x - s0) + wave, w.rows.t0 + (int)(end - s0));
       const bool whole = x == s0 && end == s1;
       finish<T, NB, SPLIT_ROWS>(w, lds, head0, n_heads, whole, part, 2 * blockIdx.x + (s0 >= x0), sp.rows);
-      if (x == s0 && threadIdx.x == 0) {
-        part.at[((size_t)r * sp.vheads + vh) * 2] = blockIdx.x;
-        part.at[((size_t)r * sp.vheads + vh) * 2 + 1] = (int)((s1 - 1) / per);
+      if (end == x1 && threadIdx.x == 0 && x1 < total) {
+        next[0] = x == s0 && end < s1 ? r : -1;  // begun here, and not finished
+        next[1] = vh;
+        next[2] = (int)((s1 - 1) / per);
       }
       x = end;
     }
   }
-  if (lane == 0 && w.rows.end < a.len[w.r]) w.bad |= PMPE_DEV_CACHE_RANGE;
   report(a.c, w.bad);
 }
 
-// The pieces' parts of one query head, in order; requests without a row get their zeros here.
+// One query head of what piece j0 began and others finished: their parts, in order.
 template <bool BF16_OUT>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-  __shared__ float s_o[256][4], s_l[256];
+  __shared__ float s_o[256][4], s_w[PIECES], s_red[8];
   const Split sp = split_of(a.heads, a.c.kv);
-  const int D = a.c.dim, r = blockIdx.x / a.heads, head = blockIdx.x - r * a.heads, tid = threadIdx.x;
-  const size_t at = (size_t)r * a.heads + head;
-  const auto store = [&](int d, f32x4 v) {
-    if (BF16_OUT) *(u32x2*)((uint16_t*)a.out + at * D + d) = u32x2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
-    else *(f32x4*)((float*)a.out + at * D + d) = v;
-  };
-  const Rows rows = rows_of(a, r);
-  if (tid == 0 && head == 0 && a.len[r] > rows.end) report(a.c, PMPE_DEV_CACHE_RANGE);
-  if (rows.n == 0) {
-    if (tid * 4 < D) store(tid * 4, f32x4{0, 0, 0, 0});
-    if (tid == 0 && a.lse) a.lse[at] = -INFINITY;
-    return;
-  }
+  const int D = a.c.dim, j0 = blockIdx.x / sp.rows, row = blockIdx.x - j0 * sp.rows, tid = threadIdx.x;
   const Part part = part_of(a.ws, sp.rows, D);
-  const int group = a.heads / a.c.kv, kv = head / group, in_kv = head - kv * group, p = in_kv / sp.rows, row = in_kv - p * sp.rows;
-  const int32_t* which = part.at + ((size_t)r * sp.vheads + kv * sp.groups + p) * 2;
-  const int j0 = which[0], j1 = which[1];
-  if (j0 == j1) return;  // a piece had it whole
-  const int per = D / 4, lanes = 256 / per, mine = tid / per, d = (tid - mine * per) * 4;
-  float M = -INFINITY;
-  for (int j = j0; j <= j1; ++j) M = fmaxf(M, part.ml[((size_t)(2 * j + (j == j0)) * sp.rows + row) * 2]);
-  f32x4 v = {0, 0, 0, 0};
-  float L = 0.f;
-  if (mine < lanes)
-    for (int j = j0 + mine; j <= j1; j += lanes) {
-      const size_t slot = (size_t)(2 * j + (j == j0)) * sp.rows + row;
-      const float m = part.ml[slot * 2], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-      L += part.ml[slot * 2 + 1] * f;
-      v += *(const f32x4*)(part.o + slot * D + d) * f;
+  const int r = part.next[4 * j0], vh = part.next[4 * j0 + 1], n = part.next[4 * j0 + 2] - j0 + 1;
+  if (r < 0) return;
+  const int group = a.heads / a.c.kv, kv = vh / sp.groups, in_kv = (vh - kv * sp.groups) * sp.rows + row;
+  if (in_kv >= group) return;
+  const auto slot = [&](int i) { return (size_t)(2 * (j0 + i) + (i == 0)) * sp.rows + row; };
+  // maxima, weights of the parts (a thread has four of them at most), the sum
+  constexpr int E = PIECES / 256;
+  float m[E], l[E], M = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const int i = tid + 256 * e;
+    m[e] = -INFINITY;
+    l[e] = 0.f;
+    if (i < n) {
+      m[e] = part.ml[slot(i) * 2];
+      l[e] = part.ml[slot(i) * 2 + 1];
     }
+    M = fmaxf(M, m[e]);
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __uint_as_float(xor_lanes(__float_as_uint(M), off)));
+  if (lane_id() == 0) s_red[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
+  float L = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float f = m[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[e] - M);
+    s_w[tid + 256 * e] = f;
+    L += l[e] * f;
+  }
+  L = wave_sum(L);
+  if (lane_id() == 0) s_red[4 + (tid >> 6)] = L;
+  __syncthreads();
+  L = (s_red[4] + s_red[5]) + (s_red[6] + s_red[7]);
+  const int per = D / 4, lanes = 256 / per, mine = tid / per, d = (tid - mine * per) * 4;
+  f32x4 v = {0, 0, 0, 0};
+  if (mine < lanes) {
+#pragma unroll 4
+    for (int i = mine; i < n; i += lanes) v += *(const f32x4*)(part.o + slot(i) * D + d) * s_w[i];
+  }
   *(f32x4*)s_o[tid] = v;
-  s_l[tid] = L;
   __syncthreads();
   if (mine > 0) return;
-  for (int j = 1; j < lanes; ++j) {
-    v += *(const f32x4*)s_o[j * per + tid];
-    L += s_l[j * per + tid];
-  }
+  for (int j = 1; j < lanes; ++j) v += *(const f32x4*)s_o[j * per + tid];
   const float inv = L == 0.f ? 0.f : 1.f / L;
-  store(d, L == 0.f ? f32x4{0, 0, 0, 0} : v * inv);
+  v = L == 0.f ? f32x4{0, 0, 0, 0} : v * inv;
+  const size_t at = (size_t)r * a.heads + kv * group + in_kv;
+  if (BF16_OUT) *(u32x2*)((uint16_t*)a.out + at * D + d) = u32x2{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3])};
+  else *(f32x4*)((float*)a.out + at * D + d) = v;
   if (tid == 0 && a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
@@ -615,7 +657,7 @@ template <int T, int NB>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
   const Split sp = split_of(a.heads, a.c.kv);
   const bool d = direct(a.c.max_pages, a.c.page_size);
-  const int grid = d ? a.c.R * sp.vheads : PIECES;
+  const int pieces = 256 * waves_per_simd(T, NB), grid = d ? a.c.R * sp.vheads : pieces;
   if (sp.rows <= 8) {
     if (d) attn_kernel<T, NB, true, true><<<grid, 64 * WAVES, 0, s>>>(a);
     else attn_kernel<T, NB, true, false><<<grid, 64 * WAVES, 0, s>>>(a);
@@ -624,8 +666,8 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
     else attn_kernel<T, NB, false, false><<<grid, 64 * WAVES, 0, s>>>(a);
   }
   if (!d) {
-    if (T == F32) attn_join_kernel<false><<<a.c.R * a.heads, 256, 0, s>>>(a);
-    else attn_join_kernel<true><<<a.c.R * a.heads, 256, 0, s>>>(a);
+    if (T == F32) attn_join_kernel<false><<<pieces * sp.rows, 256, 0, s>>>(a);
+    else attn_join_kernel<true><<<pieces * sp.rows, 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -649,7 +691,7 @@ hipError_t launch_type(const AttnArgs& a, hipStream_t s) {
 size_t attn_decode_workspace(int R, int heads, const pmpe_cache_desc* c) {
   if (R == 0 || direct(c->max_pages, c->page_size)) return 0;
   const Split sp = split_of(heads, c->n_kv_heads);
-  return ((size_t)2 * PIECES * sp.rows * (c->head_dim + 2) + (size_t)R * sp.vheads * 2) * 4;
+  return ((size_t)2 * PIECES * sp.rows * (c->head_dim + 2) + (size_t)PIECES * 4) * 4;
 }
 
 hipError_t launch_attn_decode(const AttnArgs& a, hipStream_t s) {
