@@ -9,9 +9,12 @@
 // rows 4 g .. 4 g + 3 and 16 + 4 g .. of the tile: the rows whose weights the lane holds after S^T, so weights go into
 // the second product without leaving their lane, and V^T's pairs of rows are one byte permutation each.
 //
-// The tiles of all requests and heads are one line, cut into equal pieces (a piece a block, its four waves every
-// fourth tile), whatever the lengths; a piece's parts of a request's head that others go on with are joined by a
-// second kernel in the order of the pieces. No atomics: equal calls have equal bits.
+// A block has a request's virtual head (a kv head and up to 16 of its query heads), its four waves every fourth tile.
+// Where requests are long, a head's tiles are cut into equal parts of a length that all requests share, found from
+// their lengths by every block: PARTS parts in all, and one more at most for each head. A second kernel joins the
+// parts in order. No atomics: equal calls have equal bits.
+#include <algorithm>
+
 #include "kvcache.h"
 
 namespace pmpe {
@@ -19,7 +22,9 @@ namespace {
 
 constexpr int WAVES = 4;
 constexpr int TILE = 32;        // cache rows of a wave's step
-constexpr int PIECES = 1024;    // at most
+constexpr int PARTS = 1536;       // parts that all tiles would make: two rounds of the blocks that fit the card
+constexpr int WHOLE_TILES = 32;   // tables of at most so many tiles: no head is cut (8 steps, about as long as the search and the join)
+constexpr int MOST_HEADS = 8192;  // virtual heads from which none is cut
 constexpr float LOG2E = 1.4426950408889634f;
 
 enum { BF16 = 0, FP8 = 1, F32 = 2 };
@@ -29,6 +34,11 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
+// What is read once: past the caches.
+template <class V>
+__device__ __forceinline__ V once(const V* p) {
+  return __builtin_nontemporal_load(p);
 }
 // max and sum over lanes l, l ^ 16, l ^ 32 and l ^ 48
 __device__ __forceinline__ float rows_max(float v) {
@@ -53,7 +63,6 @@ __device__ __forceinline__ uint32_t fp8_to_bf16x2(uint32_t q, float s) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, s, HI));
 }
 
-// The line of tiles: virtual heads (a kv head and up to 16 of its query heads) of request r follow one another.
 struct Split {
   int groups, rows, vheads;  // parts of a kv head's query heads, heads of a part, virtual heads of a request
 };
@@ -76,24 +85,26 @@ __host__ __device__ constexpr int waves_per_simd(int type, int nb) {
   return type == F32 ? (nb <= 1 ? 4 : nb == 2 ? 3 : nb == 3 ? 2 : 1) : nb <= 2 ? 4 : nb <= 4 ? 3 : nb <= 6 ? 2 : 1;
 }
 
-// The same of a request that the whole wave has, and a wave's own value of 64 bits, in scalar registers.
+// The same of a request that the whole wave has, in scalar registers.
 __device__ __forceinline__ Rows uniform_rows_of(const AttnArgs& a, int r) {
   const Rows v = rows_of(a, r);
   return {__builtin_amdgcn_readfirstlane(v.first), __builtin_amdgcn_readfirstlane(v.end), __builtin_amdgcn_readfirstlane(v.t0),
           __builtin_amdgcn_readfirstlane(v.n)};
 }
-__device__ __forceinline__ int64_t uniform(int64_t v) {
-  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
-}
 
-struct Part {  // workspace of the pieces
-  float* o;     // [2 PIECES][16][dim]
-  float* ml;    // [2 PIECES][16][2]
-  int32_t* next;  // [PIECES][4]: request, virtual head and last piece of what a piece leaves unfinished (request -1: nothing)
+// Workspace: the parts of heads that are cut, in places side by side. At most SLOTS: a head of n > c tiles has
+// ceil(n / c) < 2 n / c of them.
+constexpr int SLOTS = 2 * PARTS;
+struct Part {
+  float* o;       // [SLOTS][rows][dim]
+  float* ml;      // [SLOTS][rows][2]
+  int32_t* what;  // [SLOTS][4]: request, virtual head and parts of the head that begins in a place (0 parts: none does)
+  int32_t* used;  // places in use
 };
 __host__ __device__ inline Part part_of(float* ws, int rows, int dim) {
-  float* ml = ws + (size_t)2 * PIECES * rows * dim;
-  return {ws, ml, (int32_t*)(ml + (size_t)2 * PIECES * rows * 2)};
+  float* ml = ws + (size_t)SLOTS * rows * dim;
+  int32_t* what = (int32_t*)(ml + (size_t)SLOTS * rows * 2);
+  return {ws, ml, what, what + SLOTS * 4};
 }
 
 template <int T, int NB>
@@ -184,29 +195,30 @@ struct Wave {
     }
   }
 
+  // (Rows that take no part are those of page 0: the loads are the same for every tile, so that their order is known
+  // where the next ones are waited for. With branches around them every step waited for all of them.)
   __device__ const char* half(const void* cache, int n, int u, int page) const {
     const CacheArgs& c = a.c;
-    return (const char*)cache + (((size_t)page * c.kv + h) * c.page_size + __builtin_amdgcn_readlane(prow, 2 * n + u)) * (D * EL);
+    return (const char*)cache + (((size_t)max(page, 0) * c.kv + h) * c.page_size + __builtin_amdgcn_readlane(prow, 2 * n + u)) * (D * EL);
   }
   __device__ const uint8_t* scales(const uint8_t* s, int n, int u, int page) const {
     const CacheArgs& c = a.c;
-    return s + ((size_t)page * c.kv + h) * NB * c.page_size + __builtin_amdgcn_readlane(prow, 2 * n + u);
+    return s + ((size_t)max(page, 0) * c.kv + h) * NB * c.page_size + __builtin_amdgcn_readlane(prow, 2 * n + u);
   }
   __device__ void load_k(int n) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int page = __builtin_amdgcn_readlane(pages, 2 * n + u);
-      if (page < 0) continue;
       const char* at = half(a.c.k, n, u, page);
       const uint32_t off = i * (D * EL) + g * 16;
 #pragma unroll
       for (int s = 0; s < TileT::NK; ++s) {
         if (T == FP8 && (NB & 1) && s == TileT::NK - 1) {
-          const u32x2 x = *(const u32x2*)(at + (i * (D * EL) + g * 8 + s * 64));
+          const u32x2 x = *((const u32x2*)(at + (i * (D * EL) + g * 8 + s * 64)));
           t.k[u][s][0] = x[0];
           t.k[u][s][1] = x[1];
         } else {
-          t.k[u][s] = *(const u32x4*)(at + (off + s * 64));
+          t.k[u][s] = *((const u32x4*)(at + (off + s * 64)));
         }
       }
       if constexpr (T == FP8) {
@@ -221,7 +233,6 @@ struct Wave {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int page = __builtin_amdgcn_readlane(pages, 2 * n + u);
-      if (page < 0) continue;
       const char* at = half(a.c.v, n, u, page);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -232,24 +243,24 @@ struct Wave {
           const char* p = at + ((uint32_t)((g * 4 + j) * (D * EL) + i * per) + seg_base<NB>(sg) * EL);
           uint32_t* to = t.v[4 * u + j] + w;
           if (per == 32) {
-            const u32x4 x = *(const u32x4*)p, y = *(const u32x4*)(p + 16);
+            const u32x4 x = once((const u32x4*)p), y = once((const u32x4*)(p + 16));
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               to[e] = x[e];
               to[4 + e] = y[e];
             }
           } else if (per == 16) {
-            const u32x4 x = *(const u32x4*)p;
+            const u32x4 x = once((const u32x4*)p);
 #pragma unroll
             for (int e = 0; e < 4; ++e) to[e] = x[e];
           } else if (per == 8) {
-            const u32x2 x = *(const u32x2*)p;
+            const u32x2 x = once((const u32x2*)p);
             to[0] = x[0];
             to[1] = x[1];
           } else if (per == 4) {
-            to[0] = *(const uint32_t*)p;
+            to[0] = once((const uint32_t*)p);
           } else {
-            to[0] = *(const uint16_t*)p;
+            to[0] = once((const uint16_t*)p);
           }
           w += (per + 3) / 4;
         }
@@ -354,8 +365,9 @@ struct Wave {
     }
   }
 
-  // Tile `tile` (the n-th looked up), whose K and V are loaded; loads those of tile n + 1 where there is one.
-  __device__ void step(int tile, int n, bool more) {
+  // Tile `tile` (the n-th looked up), whose K and V are loaded; with MORE, loads those of tile n + 1.
+  template <bool MORE>
+  __device__ void step(int tile, int n) {
     float s[8];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -364,7 +376,7 @@ struct Wave {
       for (int e = 0; e < 4; ++e) s[4 * u + e] = x[e] * (a.scale * LOG2E);
     }
     const int p0 = tile * TILE, pg0 = __builtin_amdgcn_readlane(pages, 2 * n), pg1 = __builtin_amdgcn_readlane(pages, 2 * n + 1);
-    if (more) load_k(n + 1);
+    if constexpr (MORE) load_k(n + 1);
     const bool whole = pg0 >= 0 && pg1 >= 0 && p0 >= rows.first && p0 + TILE <= rows.end;
     if (!whole) {
       // rows that take no part: their weights are 0, and so is V there (0 times what memory holds may be NaN)
@@ -401,7 +413,7 @@ struct Wave {
     for (int j = 0; j < 8; ++j) p[j] = __builtin_amdgcn_exp2f(s[j] - ref);
     l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     accumulate(p);
-    if (more) load_v(n + 1);
+    if constexpr (MORE) load_v(n + 1);
   }
 
   // Tiles first, first + 4, .. below last.
@@ -410,7 +422,10 @@ struct Wave {
       look_up(tile);
       load_k(0);
       load_v(0);
-      for (int n = 0; n < 32 && tile < last; ++n, tile += WAVES) step(tile, n, n < 31 && tile + WAVES < last);
+      int n = 0;
+      for (; n < 31 && tile + WAVES < last; ++n, tile += WAVES) step<true>(tile, n);
+      step<false>(tile, n);
+      tile += WAVES;
     }
     l = rows_sum(l);
     if constexpr (SPLIT_ROWS && T != F32) {
@@ -484,164 +499,158 @@ __device__ void finish(Wave<T, NB, SPLIT_ROWS>& w, Lds<NB>& lds, int head0, int 
       }
     }
   }
-  __syncthreads();  // read before the next virtual head's waves write
 }
 
-// DIRECT: a block has a whole virtual head.
+// Inclusive sums over the block's threads, and the total.
+__device__ __forceinline__ int scan_block(int v, int* s, int& total) {
+  const int wave = threadIdx.x >> 6;
+  v = wave_incl_scan(v);
+  __syncthreads();
+  if (lane_id() == 63) s[wave] = v;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int j = 0; j < WAVES; ++j) {
+    if (j < wave) v += s[j];
+    total += s[j];
+  }
+  return v;
+}
+
+// DIRECT: no head is cut.
 template <int T, int NB, bool SPLIT_ROWS, bool DIRECT>
 __global__ __launch_bounds__(64 * WAVES, waves_per_simd(T, NB)) void attn_kernel(AttnArgs a) {
   __shared__ Lds<NB> lds;
-  __shared__ int64_t s_scan[WAVES], s_base;
-  __shared__ int s_r;
+  __shared__ int64_t s_tiles[WAVES];
+  __shared__ int s_scan[WAVES], s_item[4];
   const Split sp = split_of(a.heads, a.c.kv);
-  const Part part = part_of(a.ws, sp.rows, 32 * NB);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = lane_id();
-  Wave<T, NB, SPLIT_ROWS> w(a);
-  const int group = a.heads / a.c.kv;
-  const auto heads_of = [&](int vh, int& kv, int& head0, int& n) {
-    kv = vh / sp.groups;
-    const int p = vh - kv * sp.groups;
-    head0 = kv * group + p * sp.rows;
-    n = min(sp.rows, group - p * sp.rows);
-  };
-  int kv, head0, n_heads;
+  int r, vh, part = 0, parts = 1, slot = 0;
   if constexpr (DIRECT) {
-    const int r = blockIdx.x / sp.vheads;
-    heads_of(blockIdx.x - r * sp.vheads, kv, head0, n_heads);
-    w.begin(r, kv, head0, n_heads);
-    w.run(w.rows.t0 + wave, w.rows.t0 + w.rows.n);
-    finish<T, NB, SPLIT_ROWS>(w, lds, head0, n_heads, true, part, 0, sp.rows);
+    r = blockIdx.x / sp.vheads;
+    vh = blockIdx.x - r * sp.vheads;
   } else {
-    // tiles of the requests ahead: thread x sums those of requests [x c, (x + 1) c)
+    // The length of a part; then the heads' parts ahead of this block's and, of them, those of heads that are cut.
+    // Thread x has requests [x c, (x + 1) c).
     const int c = (a.c.R + 64 * WAVES - 1) / (64 * WAVES), r0 = threadIdx.x * c, r1 = min(a.c.R, r0 + c);
-    int64_t mine = 0;
-    for (int r = r0; r < r1; ++r) mine += rows_of(a, r).n;
-    int64_t upto = mine;
+    int64_t tiles = 0;
+    for (int q = r0; q < r1; ++q) tiles += rows_of(a, q).n;
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int64_t v = __shfl_up(upto, off, 64);
-      if (lane >= off) upto += v;
-    }
-    if (lane == 63) s_scan[wave] = upto;
+    for (int off = 32; off > 0; off >>= 1) tiles += __shfl_xor(tiles, off, 64);
+    if (lane == 0) s_tiles[wave] = tiles;
     __syncthreads();
-    int64_t total = 0;
+    tiles = 0;
 #pragma unroll
-    for (int j = 0; j < WAVES; ++j) {
-      if (j < wave) upto += s_scan[j];
-      total += s_scan[j];
+    for (int j = 0; j < WAVES; ++j) tiles += s_tiles[j];
+    tiles *= sp.vheads;
+    // At least 32 tiles, or 8 where that leaves CUs without a part; a head of up to one and a half parts stays whole.
+    const int len = (int)max((tiles + PARTS - 1) / PARTS, min((int64_t)32, max((int64_t)8, (tiles + 255) / 256)));
+    const int whole = len + len / 2;
+    const auto parts_of = [&](int q) {
+      const int n = rows_of(a, q).n;
+      return n <= whole ? 1 : (n + len - 1) / len;
+    };
+    int mine = 0, cut = 0, total, used;
+    for (int q = r0; q < r1; ++q) {
+      const int k = parts_of(q);
+      mine += k;
+      cut += k > 1 ? k : 0;
     }
-    total = uniform(total) * sp.vheads;
-    // a piece has a tile for each wave at least
-    int64_t per = (total + gridDim.x - 1) / gridDim.x;
-    per = max((int64_t)WAVES, (per + WAVES - 1) / WAVES * WAVES);
-    const int64_t x0 = blockIdx.x * per, x1 = min(total, x0 + per);
-    int32_t* next = part.next + 4 * blockIdx.x;
-    if (threadIdx.x == 0 && (x1 <= x0 || x1 == total)) next[0] = -1;
-    // requests without a row
-    for (int r = blockIdx.x; r < a.c.R; r += gridDim.x) {
-      const Rows rows = rows_of(a, r);
-      if (rows.n > 0) continue;
-      if (threadIdx.x == 0 && rows.end < a.len[r]) report(a.c, PMPE_DEV_CACHE_RANGE);
-      const size_t at = (size_t)r * a.heads;
-      for (int x = threadIdx.x * 4; x < a.heads * 32 * NB; x += 4 * 64 * WAVES) {
-        if (T == F32) *(f32x4*)((float*)a.out + at * 32 * NB + x) = f32x4{0, 0, 0, 0};
-        else *(u32x2*)((uint16_t*)a.out + at * 32 * NB + x) = u32x2{0, 0};
+    const int upto = scan_block(mine, s_scan, total), cut_upto = scan_block(cut, s_scan, used);
+    const Part p = part_of(a.ws, sp.rows, 32 * NB);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.used = used * sp.vheads;
+    if ((int)blockIdx.x >= total * sp.vheads) return;
+    if ((upto - mine) * sp.vheads <= (int)blockIdx.x && (int)blockIdx.x < upto * sp.vheads) {  // one thread
+      int base = upto - mine, cuts = cut_upto - cut, q = r0, k;
+      for (k = parts_of(q); (base + k) * sp.vheads <= (int)blockIdx.x; k = parts_of(q)) {
+        base += k;
+        cuts += k > 1 ? k : 0;
+        ++q;
       }
-      if (a.lse)
-        for (int x = threadIdx.x; x < a.heads; x += 64 * WAVES) a.lse[at + x] = -INFINITY;
-    }
-    if (x0 >= x1) return;
-    if ((upto - mine) * sp.vheads <= x0 && x0 < upto * sp.vheads) {  // one thread
-      int64_t base = upto - mine;
-      int r = r0;
-      for (int n = rows_of(a, r).n; (base + n) * sp.vheads <= x0; n = rows_of(a, r).n) {
-        base += n;
-        ++r;
-      }
-      s_r = r;
-      s_base = base;
+      s_item[0] = q;
+      s_item[1] = blockIdx.x - base * sp.vheads;  // virtual head and part
+      s_item[2] = k;
+      s_item[3] = cuts * sp.vheads;
     }
     __syncthreads();
-    int r = __builtin_amdgcn_readfirstlane(s_r);
-    int64_t base = uniform(s_base) * sp.vheads;  // first tile of request r
-    for (int64_t x = x0; x < x1;) {
-      const int n = uniform_rows_of(a, r).n;
-      if (x >= base + (int64_t)n * sp.vheads) {
-        base += (int64_t)n * sp.vheads;
-        ++r;
-        continue;
-      }
-      const int vh = (int)((x - base) / n);
-      const int64_t s0 = base + (int64_t)vh * n, s1 = s0 + n;  // the virtual head's tiles
-      const int64_t end = min(s1, x1);
-      heads_of(vh, kv, head0, n_heads);
-      w.begin(r, kv, head0, n_heads);
-      w.run(w.rows.t0 + (int)(x - s0) + wave, w.rows.t0 + (int)(end - s0));
-      const bool whole = x == s0 && end == s1;
-      finish<T, NB, SPLIT_ROWS>(w, lds, head0, n_heads, whole, part, 2 * blockIdx.x + (s0 >= x0), sp.rows);
-      if (end == x1 && threadIdx.x == 0 && x1 < total) {
-        next[0] = x == s0 && end < s1 ? r : -1;  // begun here, and not finished
-        next[1] = vh;
-        next[2] = (int)((s1 - 1) / per);
-      }
-      x = end;
+    r = __builtin_amdgcn_readfirstlane(s_item[0]);
+    parts = __builtin_amdgcn_readfirstlane(s_item[2]);
+    const int x = __builtin_amdgcn_readfirstlane(s_item[1]);
+    vh = x / parts;
+    part = x - vh * parts;
+    slot = __builtin_amdgcn_readfirstlane(s_item[3]) + x;
+    if (parts > 1 && threadIdx.x == 0) {
+      p.what[4 * slot] = r;
+      p.what[4 * slot + 1] = vh;
+      p.what[4 * slot + 2] = part == 0 ? parts : 0;
     }
   }
+  const int kv = vh / sp.groups, in_kv = (vh - kv * sp.groups) * sp.rows, group = a.heads / a.c.kv;
+  const int head0 = kv * group + in_kv, n_heads = min(sp.rows, group - in_kv);
+  Wave<T, NB, SPLIT_ROWS> w(a);
+  w.begin(r, kv, head0, n_heads);
+  const int first = (int)((int64_t)w.rows.n * part / parts), last = (int)((int64_t)w.rows.n * (part + 1) / parts);
+  w.run(w.rows.t0 + first + wave, w.rows.t0 + last);
+  finish<T, NB, SPLIT_ROWS>(w, lds, head0, n_heads, parts == 1, part_of(a.ws, sp.rows, 32 * NB), slot, sp.rows);
   report(a.c, w.bad);
 }
 
-// One query head of what piece j0 began and others finished: their parts, in order.
-template <bool BF16_OUT>
+// One query head of a head that was cut: its parts, in order. It has W waves of the block: one where heads are many
+// and their parts few, all four where it is the other way round.
+template <bool BF16_OUT, int W>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-  __shared__ float s_o[256][4], s_w[PIECES], s_red[8];
+  __shared__ float s_o[W == 1 ? 1 : 256][4], s_red[8];
   const Split sp = split_of(a.heads, a.c.kv);
-  const int D = a.c.dim, j0 = blockIdx.x / sp.rows, row = blockIdx.x - j0 * sp.rows, tid = threadIdx.x;
+  const int lane = lane_id(), wave = threadIdx.x >> 6, D = a.c.dim;
+  const int x = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x, s0 = x / sp.rows, row = x - s0 * sp.rows;
   const Part part = part_of(a.ws, sp.rows, D);
-  const int r = part.next[4 * j0], vh = part.next[4 * j0 + 1], n = part.next[4 * j0 + 2] - j0 + 1;
-  if (r < 0) return;
+  if (s0 >= *part.used) return;
+  const int r = part.what[4 * s0], vh = part.what[4 * s0 + 1], n = part.what[4 * s0 + 2];
+  if (n == 0) return;
   const int group = a.heads / a.c.kv, kv = vh / sp.groups, in_kv = (vh - kv * sp.groups) * sp.rows + row;
   if (in_kv >= group) return;
-  const auto slot = [&](int i) { return (size_t)(2 * (j0 + i) + (i == 0)) * sp.rows + row; };
-  // maxima, weights of the parts (a thread has four of them at most), the sum
-  constexpr int E = PIECES / 256;
-  float m[E], l[E], M = -INFINITY;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int i = tid + 256 * e;
-    m[e] = -INFINITY;
-    l[e] = 0.f;
-    if (i < n) {
-      m[e] = part.ml[slot(i) * 2];
-      l[e] = part.ml[slot(i) * 2 + 1];
-    }
-    M = fmaxf(M, m[e]);
-  }
+  const auto slot = [&](int i) { return (size_t)(s0 + i) * sp.rows + row; };
+  const int tid = W == 1 ? lane : threadIdx.x, per = D / 4, lanes = 64 * W / per, mine = tid / per, d = (tid - mine * per) * 4;
+  // the first parts are under way while their weights are worked out
+  f32x4 v0 = {0, 0, 0, 0}, v1 = {0, 0, 0, 0};
+  if (mine < lanes && mine < n) v0 = *(const f32x4*)(part.o + slot(mine) * D + d);
+  if (mine < lanes && mine + lanes < n) v1 = *(const f32x4*)(part.o + slot(mine + lanes) * D + d);
+  float M = -INFINITY, L = 0.f;
+  for (int i = tid; i < n; i += 64 * W) M = fmaxf(M, part.ml[slot(i) * 2]);
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) M = fmaxf(M, __uint_as_float(xor_lanes(__float_as_uint(M), off)));
-  if (lane_id() == 0) s_red[tid >> 6] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-  float L = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const float f = m[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[e] - M);
-    s_w[tid + 256 * e] = f;
-    L += l[e] * f;
+  if constexpr (W > 1) {
+    if (lane == 0) s_red[wave] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
   }
+  const auto weight = [&](int i) {
+    const float m = part.ml[slot(i) * 2];
+    return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+  };
+  for (int i = tid; i < n; i += 64 * W) L += part.ml[slot(i) * 2 + 1] * weight(i);
   L = wave_sum(L);
-  if (lane_id() == 0) s_red[4 + (tid >> 6)] = L;
-  __syncthreads();
-  L = (s_red[4] + s_red[5]) + (s_red[6] + s_red[7]);
-  const int per = D / 4, lanes = 256 / per, mine = tid / per, d = (tid - mine * per) * 4;
   f32x4 v = {0, 0, 0, 0};
   if (mine < lanes) {
+    if (mine < n) v = v0 * weight(mine);
+    if (mine + lanes < n) v += v1 * weight(mine + lanes);
 #pragma unroll 4
-    for (int i = mine; i < n; i += lanes) v += *(const f32x4*)(part.o + slot(i) * D + d) * s_w[i];
+    for (int i = mine + 2 * lanes; i < n; i += lanes) v += *(const f32x4*)(part.o + slot(i) * D + d) * weight(i);
   }
-  *(f32x4*)s_o[tid] = v;
-  __syncthreads();
-  if (mine > 0) return;
-  for (int j = 1; j < lanes; ++j) v += *(const f32x4*)s_o[j * per + tid];
+  if constexpr (W > 1) {
+    if (lane == 0) s_red[4 + wave] = L;
+    *(f32x4*)s_o[tid] = v;
+    __syncthreads();
+    L = (s_red[4] + s_red[5]) + (s_red[6] + s_red[7]);
+    if (mine > 0) return;
+    for (int j = 1; j < lanes; ++j) v += *(const f32x4*)s_o[j * per + tid];
+  } else {
+    const f32x4 own = v;
+    for (int j = 1; j < lanes; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += __shfl(own[e], (lane + j * per) & 63, 64);
+    if (mine > 0) return;
+  }
   const float inv = L == 0.f ? 0.f : 1.f / L;
   v = L == 0.f ? f32x4{0, 0, 0, 0} : v * inv;
   const size_t at = (size_t)r * a.heads + kv * group + in_kv;
@@ -650,14 +659,17 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   if (tid == 0 && a.lse) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
 }
 
-// Requests whose tables hold a tile for each wave at most are whole blocks; longer ones go by pieces.
-bool direct(int max_pages, int page_size) { return (int64_t)max_pages * page_size <= WAVES * TILE; }
+// No head is cut where tables hold no more than an uncut one, or where heads are many anyway.
+bool direct(int64_t vheads, int max_pages, int page_size) {
+  return (int64_t)max_pages * page_size <= WHOLE_TILES * TILE || vheads >= MOST_HEADS;
+}
 
 template <int T, int NB>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
   const Split sp = split_of(a.heads, a.c.kv);
-  const bool d = direct(a.c.max_pages, a.c.page_size);
-  const int pieces = 256 * waves_per_simd(T, NB), grid = d ? a.c.R * sp.vheads : pieces;
+  const int64_t vheads = (int64_t)a.c.R * sp.vheads, rows = (int64_t)a.c.max_pages * a.c.page_size;
+  const bool d = direct(vheads, a.c.max_pages, a.c.page_size);
+  const int grid = (int)(d ? vheads : vheads + PARTS);
   if (sp.rows <= 8) {
     if (d) attn_kernel<T, NB, true, true><<<grid, 64 * WAVES, 0, s>>>(a);
     else attn_kernel<T, NB, true, false><<<grid, 64 * WAVES, 0, s>>>(a);
@@ -666,8 +678,10 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
     else attn_kernel<T, NB, false, false><<<grid, 64 * WAVES, 0, s>>>(a);
   }
   if (!d) {
-    if (T == F32) attn_join_kernel<false><<<pieces * sp.rows, 256, 0, s>>>(a);
-    else attn_join_kernel<true><<<pieces * sp.rows, 256, 0, s>>>(a);
+    // places that can be in use
+    const int slots = (int)std::min<int64_t>(SLOTS, vheads * ((rows + 8 * TILE - 1) / (8 * TILE) + 1));
+    if (vheads > 64) attn_join_kernel<T != F32, 1><<<(slots * sp.rows + 3) / 4, 256, 0, s>>>(a);
+    else attn_join_kernel<T != F32, 4><<<slots * sp.rows, 256, 0, s>>>(a);
   }
   return hipGetLastError();
 }
@@ -689,9 +703,9 @@ hipError_t launch_type(const AttnArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t attn_decode_workspace(int R, int heads, const pmpe_cache_desc* c) {
-  if (R == 0 || direct(c->max_pages, c->page_size)) return 0;
   const Split sp = split_of(heads, c->n_kv_heads);
-  return ((size_t)2 * PIECES * sp.rows * (c->head_dim + 2) + (size_t)PIECES * 4) * 4;
+  if (R == 0 || direct((int64_t)R * sp.vheads, c->max_pages, c->page_size)) return 0;
+  return ((size_t)SLOTS * (sp.rows * (c->head_dim + 2) + 4) + 4) * 4;
 }
 
 hipError_t launch_attn_decode(const AttnArgs& a, hipStream_t s) {
