@@ -6,11 +6,11 @@
 //
 // Two kernels. The first goes over the logits once, in pieces of a row that its blocks hold in registers:
 // the piece's maximum, the maxima of its chunks of 512, and a histogram by x = z / temperature in bins of 1/8 (512
-// of them from the maximum down: what lies lower has less than e^-64 of its mass) of counts and masses. The second
-// has a block per row: it adds up the histograms, finds the bins of the thresholds, and collects the tokens down to
-// the last bin that matters, from chunks that hold one. They are sorted, and everything is decided on the list.
-// Where they are more than a list (ties, flat rows without a cut) it looks into one bin at a time, by
-// histograms of the logits' bits in it.
+// of them from the maximum down: what lies lower has less than e^-63 of its mass) of counts and masses. The second
+// has a block per row: it adds up the histograms, finds the bins of the thresholds, and collects the tokens of the
+// bins that matter from the chunks that hold one, in LDS. A threshold's token is then found by histograms of the
+// order's bits inside its bin (9 bits a round) until 64 tokens are left, which one wave sorts. Bins with more tokens
+// than the list holds (ties, flat rows) have their first rounds over the logits themselves.
 //
 // Masses are exact integers inside a bin (units of 2^-44 of the mass at its centre), so their sums do not depend on
 // the order of the atomics; across bins they are fp64 in a fixed order.
@@ -26,11 +26,13 @@ constexpr int BINS = 512;
 constexpr int CHUNK = 512;      // logits that a wave loads at once, 8 a lane
 constexpr int HIST_THREADS = 512;
 constexpr int PIECE8 = HIST_THREADS * 8;
-constexpr int THREADS = 1024;   // of the second kernel
-constexpr int CAP = 2 * THREADS;  // tokens of a list
+constexpr int THREADS = 512;    // of the second kernel: a bin for each
+constexpr int CAP = 16 * THREADS;  // tokens of a list
 constexpr int MAX_CHUNKS = PMPE_MAX_VOCAB / CHUNK;
+constexpr int MAX_PIECES = PMPE_MAX_VOCAB / PIECE8;
+constexpr int ID_BITS = 19;
 // rows whose top_k is at most this are counted only: their list has the masses
-constexpr int COUNT_K = CAP / 2;
+constexpr int COUNT_K = CAP / 4;
 
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
@@ -106,7 +108,7 @@ struct Row {
   bool greedy, masses;  // takes the first token; its histogram has masses
   int k;                // 0: no cut
   float p, least;       // 1 and 0: no cut
-  double inv;
+  double t, inv;        // the temperature and its reciprocal
 };
 __device__ __forceinline__ Row row_of(const SampleArgs& a, int b) {
   Row r;
@@ -117,7 +119,8 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int b) {
   r.p = r.p < 1.f ? fmaxf(r.p, 0.f) : 1.f;
   r.least = a.min_p ? a.min_p[b] : 0.f;
   r.least = r.least > 0.f ? fminf(r.least, 1.f) : 0.f;
-  r.inv = r.greedy ? 1.0 : 1.0 / (double)t;
+  r.t = r.greedy ? 1.0 : (double)t;
+  r.inv = 1.0 / r.t;
   r.masses = !r.greedy && (r.k == 0 ? r.p < 1.f || r.least == 0.f : r.k > COUNT_K);
   return r;
 }
@@ -252,513 +255,536 @@ struct Lds {
   uint32_t count[BINS];
   unsigned long long sub_mass[BINS];
   uint32_t sub_count[BINS];
-  uint64_t list[CAP];    // (descending logit, id)
-  double upto[CAP];      // masses of the list up to and with a place
+  uint64_t list[CAP];    // places in the order
+  uint64_t few[64];
   uint16_t chunk[MAX_CHUNKS];
+  int shift[MAX_PIECES], used[MAX_PIECES];
   double wave_mass[THREADS / 64];
   uint64_t wave_u[THREADS / 64];
   uint32_t wave_count[THREADS / 64];
-  uint32_t chunks, n, at, id;
+  uint32_t chunks, n, at, pos;
+  uint64_t place, mass_at;
 };
 
-// Inclusive sums over the block's threads in order; `total` that of all.
-__device__ double scan_mass(double v, Lds& s, double& total) {
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double o = __shfl_up(v, off, 64);
-    if (lane >= off) v += o;
-  }
-  __syncthreads();
-  if (lane == 63) s.wave_mass[wave] = v;
-  __syncthreads();
-  double before = 0.0;
-  total = 0.0;
-  for (int w = 0; w < THREADS / 64; ++w) {
-    if (w == wave) before = total;
-    total += s.wave_mass[w];
-  }
-  return before + v;
-}
-__device__ uint32_t scan_count(uint32_t v, Lds& s, uint32_t& total) {
-  const int wave = threadIdx.x >> 6;
-  v = (uint32_t)wave_incl_scan((int)v);
-  __syncthreads();
-  if (lane_id() == 63) s.wave_count[wave] = v;
-  __syncthreads();
-  uint32_t before = 0;
-  total = 0;
-  for (int w = 0; w < THREADS / 64; ++w) {
-    if (w == wave) before = total;
-    total += s.wave_count[w];
-  }
-  return before + v;
-}
-__device__ uint64_t scan_u64(uint64_t v, Lds& s) {
-  const int lane = lane_id(), wave = threadIdx.x >> 6;
-#pragma unroll
+// What all threads have alike, in scalar registers.
+__device__ __forceinline__ uint32_t uni(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ int uni(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uni(float v) { return __uint_as_float(uni(__float_as_uint(v))); }
+__device__ __forceinline__ uint64_t uni(uint64_t v) { return ((uint64_t)uni((uint32_t)(v >> 32)) << 32) | uni((uint32_t)v); }
+__device__ __forceinline__ double uni(double v) { return __longlong_as_double((long long)uni((uint64_t)__double_as_longlong(v))); }
+
+__device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v) {
+  const int lane = lane_id();
+#pragma unroll 1
   for (int off = 1; off < 64; off <<= 1) {
     const uint64_t o = shfl_u64(v, max(lane - off, 0));
     if (lane >= off) v += o;
   }
-  __syncthreads();
-  if (lane == 63) s.wave_u[wave] = v;
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) v += s.wave_u[w];
   return v;
 }
-// The lowest thread number among those whose flag is set (THREADS if none).
-__device__ uint32_t first_of(bool flag, Lds& s) {
-  const uint64_t m = __ballot(flag);
+// Inclusive sums over the block's threads.
+__device__ __forceinline__ void scan_both(Lds& s, uint32_t& count, uint64_t& mass) {
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  count = (uint32_t)wave_incl_scan((int)count);
+  mass = wave_scan_u64(mass);
   __syncthreads();
-  if (threadIdx.x == 0) s.at = THREADS;
+  if (lane == 63) {
+    s.wave_count[wave] = count;
+    s.wave_u[wave] = mass;
+  }
   __syncthreads();
-  if (m && lane_id() == 0) atomicMin(&s.at, (uint32_t)((threadIdx.x & ~63u) + __builtin_ctzll(m)));
+#pragma unroll 1
+  for (int w = 0; w < wave; ++w) {
+    count += s.wave_count[w];
+    mass += s.wave_u[w];
+  }
+}
+// The bins' sums from the top down into s.count and s.mass.
+__device__ __forceinline__ void scan_bins(Lds& s, uint32_t count, double mass) {
+  const int lane = lane_id(), wave = threadIdx.x >> 6;
+  count = (uint32_t)wave_incl_scan((int)count);
+#pragma unroll 1
+  for (int off = 1; off < 64; off <<= 1) {
+    const double o = __shfl_up(mass, off, 64);
+    if (lane >= off) mass += o;
+  }
   __syncthreads();
-  return s.at;
+  if (lane == 63) {
+    s.wave_count[wave] = count;
+    s.wave_mass[wave] = mass;
+  }
+  __syncthreads();
+  uint32_t c = 0;
+  double m = 0.0;
+#pragma unroll 1
+  for (int w = 0; w < wave; ++w) {
+    c += s.wave_count[w];
+    m += s.wave_mass[w];
+  }
+  s.count[threadIdx.x] = c + count;
+  s.mass[threadIdx.x] = m + mass;
+  __syncthreads();
+}
+// The lowest thread number among those whose flag is set, else the highest among those whose second flag is set
+// (THREADS or more: none).
+__device__ __forceinline__ int first_of(Lds& s, bool flag, bool other) {
+  const uint64_t m = __ballot(flag), o = __ballot(other);
+  const uint32_t base = threadIdx.x & ~63u;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s.at = THREADS;
+    s.pos = THREADS;
+  }
+  __syncthreads();
+  if (lane_id() == 0) {
+    if (m) atomicMin(&s.at, base + (uint32_t)__builtin_ctzll(m));
+    if (o) atomicMin(&s.pos, (uint32_t)(THREADS - 1 - (base + 63 - __builtin_clzll(o))));
+  }
+  __syncthreads();
+  const uint32_t at = uni(s.at), pos = uni(s.pos);
+  return (int)(at < THREADS ? at : THREADS - 1 - pos);
 }
 
-template <bool BF16>
-struct Decide {
-  const SampleArgs& a;
-  const Layout& lay;
-  Lds& s;
-  const int b, tid, lane, wave;
-  const Row row;
+// A token's place in the order: descending logit, then id.
+__device__ __forceinline__ uint64_t place_of(float z, int id) { return ((uint64_t)~key_of(z) << ID_BITS) | (uint32_t)id; }
+__device__ __forceinline__ float place_z(uint64_t p) { return z_of(~(uint32_t)(p >> ID_BITS)); }
+__device__ __forceinline__ int place_id(uint64_t p) { return (int)(p & ((1u << ID_BITS) - 1)); }
+
+// One way over tokens: those of the list, or of the row's chunks that hold a logit of [zlo, zhi]. A token counts if its
+// bin is in b0 .. b1 or b2 .. b3 (BINS: below the bins), its place in lo .. hi and (z - top) / temperature at least
+// low. It is appended to the list, or counted, with its mass, in place (place - lo) >> sh, or its bin - b0, of the
+// sub-histogram.
+struct Pass {
+  bool listed, append, by_bin;
+  int b0, b1, b2, b3, sh;
+  float zlo, zhi;
+  uint64_t lo, hi;
+  double low;
+  // the row
+  float top;
+  double tb, inv;
   const char* z;
-  const char* ws;
-  float top;   // the row's largest logit
-  double tb;   // its bin
-
-  __device__ Decide(const SampleArgs& args, const Layout& l, Lds& lds)
-      : a(args), lay(l), s(lds), b(blockIdx.x), tid(threadIdx.x), lane(lane_id()), wave(threadIdx.x >> 6), row(row_of(args, blockIdx.x)) {
-    z = (const char*)a.z + (size_t)b * a.stride * (BF16 ? 2 : 4);
-    ws = (const char*)a.ws + (size_t)b * lay.row;
+  const float* chunk_top;
+  int V, chunks;
+};
+__device__ __forceinline__ void take(Lds& s, const Pass& p, bool in, float x, uint64_t at) {
+  const double bin = bin_of(x, p.inv);
+  const int i = below(p.tb, bin);
+  in = in && ((i >= p.b0 && i <= p.b1) || (i >= p.b2 && i <= p.b3)) && at >= p.lo && at <= p.hi && ((double)x - (double)p.top) * p.inv >= p.low;
+  if (p.append) {
+    const uint64_t mask = __ballot(in);
+    if (!mask) return;
+    uint32_t to = 0;
+    if (lane_id() == 0) to = atomicAdd(&s.n, (uint32_t)__builtin_popcountll(mask));
+    to = uni(to) + __builtin_popcountll(mask & ((1ull << lane_id()) - 1));
+    if (in && to < CAP) s.list[to] = at;
+  } else if (in) {
+    const uint32_t q = p.by_bin ? (uint32_t)(i - p.b0) : (uint32_t)((at - p.lo) >> p.sh);
+    if (q < BINS) {
+      atomicAdd(&s.sub_count[q], 1u);
+      if (i < BINS) atomicAdd(&s.sub_mass[q], (unsigned long long)mass_in_bin(x, p.inv, bin));
+    }
   }
-
-  // The chunks with a logit of bin `last` or above it.
-  __device__ void pick_chunks(int last) {
-    __syncthreads();
-    if (tid == 0) s.chunks = 0;
-    __syncthreads();
-    for (int c0 = 0; c0 < lay.chunks; c0 += THREADS) {
+}
+template <bool BF16>
+__device__ __forceinline__ void go_over(Lds& s, const Pass& p) {
+  const int tid = threadIdx.x, lane = lane_id(), wave = uni(tid >> 6);
+  constexpr int WAVES = THREADS / 64, U = 2;  // chunks that a wave takes at once, as many more under way
+  __syncthreads();
+  if (p.append) {
+    if (tid == 0) s.n = 0;
+  } else {
+    s.sub_mass[tid] = 0;
+    s.sub_count[tid] = 0;
+  }
+  if (tid == 0) s.chunks = 0;
+  __syncthreads();
+  // the chunks that hold one
+  if (!p.listed) {
+#pragma unroll 1
+    for (int c0 = 0; c0 < p.chunks; c0 += THREADS) {
       const int c = c0 + tid;
-      const float m = c < lay.chunks ? ((const float*)(ws + lay.max_at))[c] : -INFINITY;
-      const bool in = m > -INFINITY && below(tb, bin_of(m, row.inv)) <= last;
+      const bool in = c < p.chunks && p.chunk_top[c] >= p.zlo;
       const uint64_t mask = __ballot(in);
       uint32_t at = 0;
       if (lane == 0 && mask) at = atomicAdd(&s.chunks, (uint32_t)__builtin_popcountll(mask));
-      at = __builtin_amdgcn_readfirstlane(at);
+      at = uni(at);
       if (in) s.chunk[at + __builtin_popcountll(mask & ((1ull << lane) - 1))] = (uint16_t)c;
     }
     __syncthreads();
   }
-  // f(z, id, bin index) for every token of the picked chunks that is not masked; lanes without one have in = false.
-  template <class F>
-  __device__ void each(F f) {
-    for (uint32_t n = wave; n < s.chunks; n += THREADS / 64) {
-      const int i = s.chunk[n] * CHUNK + lane * 8;
-      float v[8];
-      load8<BF16>(z, i, a.V, v);
+  // (the list goes through the same steps, one of its places a lane)
+  const uint32_t n = uni(p.listed ? s.n : s.chunks);
+  float next[U][8];
+  int next_at[U];
+  const auto load = [&](uint32_t c) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = canon(v[j]);
-        const double bin = bin_of(x, row.inv);
-        f(x, i + j, x > -INFINITY ? below(tb, bin) : BINS + 1, bin);
+    for (int u = 0; u < U; ++u) {
+      next_at[u] = c + u < n ? s.chunk[c + u] * CHUNK + lane * 8 : p.V;
+      load8<BF16>(p.z, next_at[u], p.V, next[u]);
+    }
+  };
+  if (!p.listed) load(wave * U);
+  const uint32_t step = p.listed ? THREADS : WAVES * U;
+#pragma unroll 1
+  for (uint32_t c = p.listed ? wave * 64 : wave * U; c < n; c += step) {
+    float v[U * 8];
+    int at[U];
+    uint64_t place = 0;
+    uint32_t left = 0;
+    if (p.listed) {
+      if (c + lane < n) {
+        place = s.list[c + lane];
+        left = 1;
       }
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        at[u] = next_at[u];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u * 8 + j] = canon(next[u][j]);
+      }
+      load(c + step);
+#pragma unroll
+      for (int j = 0; j < 8 * U; ++j) left |= v[j] >= p.zlo && v[j] <= p.zhi ? 1u << j : 0u;
+    }
+    while (__any(left != 0)) {
+      const int j = left ? __builtin_ctz(left) : 0;
+      float x = place_z(place);
+      if (!p.listed) {
+        x = v[0];
+#pragma unroll
+        for (int q = 1; q < 8 * U; ++q) x = j == q ? v[q] : x;
+        int id = at[0];
+#pragma unroll
+        for (int u = 1; u < U; ++u) id = j >= 8 * u ? at[u] : id;
+        place = place_of(x, id + (j & 7));
+      }
+      take(s, p, left != 0, x, place);
+      left &= left - 1;
     }
   }
-  // The picked chunks' tokens that f takes, sorted, into the list: at most CAP. Returns their number.
-  template <class F>
-  __device__ int collect(F f) {
-    if (tid == 0) s.n = 0;
-    __syncthreads();
-    each([&](float x, int id, int i, double) {
-      const bool in = f(x, i);
-      const uint64_t mask = __ballot(in);
-      if (!mask) return;
-      uint32_t at = 0;
-      if (lane == 0) at = atomicAdd(&s.n, (uint32_t)__builtin_popcountll(mask));
-      at = __builtin_amdgcn_readfirstlane(at) + __builtin_popcountll(mask & ((1ull << lane) - 1));
-      if (in && at < CAP) s.list[at] = ((uint64_t)~key_of(x) << 32) | (uint32_t)id;
-    });
-    __syncthreads();
-    const int n = min((int)s.n, CAP);
-    int n2 = 2;
-    while (n2 < n) n2 <<= 1;
-    for (int i = n + tid; i < n2; i += THREADS) s.list[i] = ~0ull;
-    __syncthreads();
-    for (int size = 2; size <= n2; size <<= 1)
-      for (int step = size >> 1; step > 0; step >>= 1) {
-        if (tid < n2 / 2) {
-          const int i = 2 * tid - (tid & (step - 1)), j = i + step;
-          const uint64_t x = s.list[i], y = s.list[j];
-          if ((x > y) == ((i & size) == 0)) {
-            s.list[i] = y;
-            s.list[j] = x;
-          }
-        }
-        __syncthreads();
-      }
-    return n;
-  }
-  __device__ float list_z(int i) const { return z_of(~(uint32_t)(s.list[i] >> 32)); }
-  __device__ int list_id(int i) const { return (int)(uint32_t)s.list[i]; }
-  // Mass relative to the largest logit's.
-  __device__ double mass_of(float x) const { return exp64(((double)x - (double)top) * row.inv); }
+  __syncthreads();
+  if (p.append && tid == 0) s.n = min(s.n, (uint32_t)CAP);
+  __syncthreads();
+}
 
-  __device__ void answer(int token, double prob, int64_t kept) {
+enum { COUNT, REACH, EXCEED };  // what crosses a value: the count, the mass reaching or exceeding it
+__device__ __forceinline__ bool crossed(int mode, double value, uint32_t count, double mass) {
+  return mode == COUNT ? (double)count >= value : mode == REACH ? mass >= value : mass > value;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout lay) {
+  __shared__ Lds s;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = lane_id(), wave = uni(tid >> 6);
+  const Row row = row_of(a, b);
+  const char* ws = (const char*)a.ws + (size_t)b * lay.row;
+  const auto answer = [&](int token, double prob, int64_t kept) {
     if (tid != 0) return;
     a.token[b] = token;
     if (a.prob) a.prob[b] = (float)prob;
     if (a.kept) a.kept[b] = (int)kept;
-  }
-  __device__ double number() const {
-    const float u = a.u[b];
-    return u > 0.f ? (double)u : 0.0;
-  }
-
-  // ---- one bin at a time, where the tokens down to the last bin that matters are more than a list
-
-  enum { COUNT, REACH, EXCEED };  // what crosses: the count, the mass reaching or exceeding a value
-  struct Place {
-    Sum sum;  // up to and with the token
-    float z;
-    int id;
   };
-  // The first token of bin i at which the sums of the row cross `value`; the last one of the bin if none does.
-  __device__ Place cross(int i, int mode, double value) {
-    const uint32_t count0 = i ? s.count[i - 1] : 0;
-    const double mass0 = i ? s.mass[i - 1] : 0.0, unit = exp64(-0.125 * i) * 0x1p-44;
-    const double bin = tb - i;
-    const auto crossed = [&](uint32_t n, uint64_t m) {
-      const double mass = mass0 + unit * (double)m;
-      return mode == COUNT ? (double)(count0 + n) >= value : mode == REACH ? mass >= value : mass > value;
-    };
-    // keys of the bin's logits lie in [lo, hi]: its edges, a little wider
-    uint32_t hi = key_of(top), lo = key_of(-FLT_MAX);
-    if (row.inv > 1e-60 && fabs(bin) < 0x1p52) {
-      const double z0 = bin * 0.125 / row.inv, z1 = (bin + 1.0) * 0.125 / row.inv, w = (fabs(z0) + fabs(z1)) * 0x1p-20 + 1e-40;
-      if (z1 + w < (double)top) hi = key_of((float)(z1 + w) + 0.f);
-      if (z0 - w > -(double)FLT_MAX) lo = key_of((float)(z0 - w) + 0.f);
-      if (hi < lo) hi = lo;
-      hi = min(hi + 2, key_of(top));
-      lo = lo > 2 ? lo - 2 : 0;
-    }
-    uint32_t n0 = 0, n = s.count[i] - count0;  // tokens of the bin above hi, and in [lo, hi]
-    uint64_t m0 = 0;
-    pick_chunks(i);
-    for (;;) {
-      const auto in = [=](float x, int j) { return j == i && key_of(x) >= lo && key_of(x) <= hi; };
-      if (n <= (uint32_t)CAP) {
-        const int len = collect(in);
-        if (len == 0) return Place{{count0 + n0, mass0}, top, -1};  // (the logits have changed since the first kernel)
-        // two neighbouring places a thread
-        const int p = 2 * tid;
-        const uint64_t e0 = p < len ? mass_in_bin(list_z(p), row.inv, bin) : 0, e1 = p + 1 < len ? mass_in_bin(list_z(p + 1), row.inv, bin) : 0;
-        const uint64_t m1 = m0 + scan_u64(e0 + e1, s), mp = m1 - e1;
-        const bool c0 = p < len && crossed(n0 + p + 1, mp), c1 = p + 1 < len && crossed(n0 + p + 2, m1);
-        uint32_t who = first_of(c0 || c1, s);
-        int at;
-        if (who == THREADS) {
-          at = len - 1;
-          who = at / 2;
-        } else {
-          if ((uint32_t)tid == who) s.n = c0 ? p : p + 1;
-          __syncthreads();
-          at = s.n;
-        }
-        if ((uint32_t)tid == who) s.wave_u[0] = at == p ? mp : m1;
-        __syncthreads();
-        const Place r{{count0 + n0 + at + 1, mass0 + unit * (double)s.wave_u[0]}, list_z(at), list_id(at)};
-        __syncthreads();
-        return r;
-      }
-      if (lo == hi) {  // more tokens of one logit than a list: they have one mass
-        const float x = z_of(lo);
-        const uint64_t e = mass_in_bin(x, row.inv, bin);
-        uint32_t l = 0, h = n;  // crossed at h, not at l
-        while (h - l > 1) {
-          const uint32_t mid = (l + h) / 2;
-          if (crossed(n0 + mid, m0 + mid * e)) h = mid;
-          else l = mid;
-        }
-        return Place{{count0 + n0 + h, mass0 + unit * (double)(m0 + h * e)}, x, nth(x, h)};
-      }
-      const uint32_t span = hi - lo;
-      const int sh = max(0, 32 - (int)__builtin_clz(span) - 9);
-      __syncthreads();
-      if (tid < BINS) {
-        s.sub_mass[tid] = 0;
-        s.sub_count[tid] = 0;
-      }
-      __syncthreads();
-      each([&](float x, int, int j, double) {
-        if (!in(x, j)) return;
-        const uint32_t q = (hi - key_of(x)) >> sh;
-        atomicAdd(&s.sub_count[q], 1u);
-        atomicAdd(&s.sub_mass[q], (unsigned long long)mass_in_bin(x, row.inv, bin));
-      });
-      __syncthreads();
-      const uint32_t mine = tid < BINS ? s.sub_count[tid] : 0;
-      const uint64_t mass = tid < BINS ? s.sub_mass[tid] : 0;
-      uint32_t total;
-      const uint32_t c = n0 + scan_count(mine, s, total);
-      const uint64_t m = m0 + scan_u64(mass, s);
-      uint32_t who = first_of(mine > 0 && crossed(c, m), s);
-      if (who == THREADS) {  // (the last one that is not empty)
-        who = THREADS - 1 - first_of_reversed(mine > 0);
-        if (who >= THREADS) return Place{{count0 + n0, mass0}, top, -1};
-      }
-      __syncthreads();
-      if ((uint32_t)tid == who) {
-        s.n = c - mine;
-        s.at = mine;
-        s.wave_u[0] = m - mass;
-      }
-      __syncthreads();
-      n0 = s.n;
-      n = s.at;
-      m0 = s.wave_u[0];
-      hi -= who << sh;
-      lo = max(lo, hi - min(hi, (1u << sh) - 1));
-      __syncthreads();
-    }
-  }
-  __device__ uint32_t first_of_reversed(bool flag) {
-    const uint64_t m = __ballot(flag);
-    __syncthreads();
-    if (tid == 0) s.at = THREADS;
-    __syncthreads();
-    if (m && lane == 0) atomicMin(&s.at, (uint32_t)(THREADS - 1 - ((tid & ~63) + 63 - __builtin_clzll(m))));
-    __syncthreads();
-    return s.at;
-  }
-  // Id of the n-th token (from 1) whose logit is x.
-  __device__ int nth(float x, uint32_t n) {
-    uint32_t before = 0;
-    __syncthreads();
-    if (tid == 0) s.id = 0;
-    for (int base = 0; base < a.V; base += THREADS * 8) {
-      float v[8];
-      load8<BF16>(z, base + tid * 8, a.V, v);
-      uint32_t mine = 0, total;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) mine += canon(v[j]) == x ? 1 : 0;
-      const uint32_t upto = before + scan_count(mine, s, total);
-      if (upto - mine < n && n <= upto) {
-        uint32_t at = upto - mine;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (canon(v[j]) == x && ++at == n) s.id = base + tid * 8 + j;
-      }
-      before += total;
-      if (before >= n) break;
-    }
-    __syncthreads();
-    return (int)s.id;
-  }
-  // First bin whose sums cross; the last one that is not empty if none does.
-  __device__ int bin_where(int mode, double value) {
-    const bool in = tid < BINS && (tid == 0 || s.count[tid] > s.count[tid - 1]);
-    const bool yes = in && (mode == COUNT ? (double)s.count[tid] >= value : mode == REACH ? s.mass[tid] >= value : s.mass[tid] > value);
-    const uint32_t i = first_of(yes, s);
-    return i < THREADS ? (int)i : (int)(THREADS - 1 - first_of_reversed(in));
-  }
-  // Count and mass (relative to the first bin's centre) of the row's tokens with (z - top) / temperature >= low.
-  __device__ Sum at_least(double low) {
-    Sum v{0, 0.0};
-    for (int c = wave; c < lay.chunks; c += THREADS / 64) {
-      if (!(((const float*)(ws + lay.max_at))[c] > -INFINITY)) continue;
-      const int i = c * CHUNK + lane * 8;
-      float x[8];
-      load8<BF16>(z, i, a.V, x);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float y = canon(x[j]);
-        const double d = ((double)y - (double)top) * row.inv;
-        if (y > -INFINITY && d >= low) {
-          v.count += 1;
-          v.mass += exp64(d);
-        }
-      }
-    }
-    double mass;
-    uint32_t count;
-    scan_mass(v.mass, s, mass);
-    scan_count(v.count, s, count);
-    return Sum{count, mass / from_centre()};
-  }
-  // The mass at the centre of the first bin relative to the largest logit's.
-  __device__ double from_centre() const {
-    const double c = fabs(tb) < 0x1p52 ? -__builtin_fma((double)top, row.inv, -(tb + 0.5) * 0.125) : 0.0;
-    return c < 0 ? exp64(c) : 1.0 / exp64(-c);
-  }
 
-  __device__ void run();
-};
-
-template <bool BF16>
-__device__ void Decide<BF16>::run() {
   // the row's largest logit and its tokens
-  const Head* heads = (const Head*)ws;
-  float m = -INFINITY;
-  uint32_t live = 0;
-  for (int i = tid; i < lay.pieces; i += THREADS) {
-    m = fmaxf(m, heads[i].top);
-    live += heads[i].live;
+  static_assert(MAX_PIECES <= THREADS && BINS == THREADS, "a piece and a bin for each thread");
+  Head head{-INFINITY, 0xFFFFFFFFu, 0u, 0u};
+  if (tid < lay.pieces) head = ((const Head*)ws)[tid];
+  {
+    const float m = wave_max(head.top);
+    const int n = wave_sum_int((int)head.live);
+    if (lane == 0) {
+      s.wave_mass[wave] = (double)m;
+      s.wave_count[wave] = (uint32_t)n;
+    }
+    if (tid == 0) s.pos = 0xFFFFFFFFu;
   }
-  m = wave_max(m);
-  if (lane == 0) s.wave_mass[wave] = (double)m;
-  uint32_t total;
+  uint32_t live = 0;
+  float top = -INFINITY;
   __syncthreads();
-  top = -INFINITY;
-  for (int w = 0; w < THREADS / 64; ++w) top = fmaxf(top, (float)s.wave_mass[w]);
-  scan_count(live, s, total);
-  live = total;
+#pragma unroll 1
+  for (int w = 0; w < (lay.pieces + 63) / 64; ++w) {
+    top = fmaxf(top, (float)s.wave_mass[w]);
+    live += s.wave_count[w];
+  }
+  top = uni(top);
+  live = uni(live);
   if (top == -INFINITY) {
     answer(-1, 0.0, 0);
     return;
   }
   if (row.greedy) {
-    if (tid == 0) s.id = 0xFFFFFFFFu;
+    if (head.top == top) atomicMin(&s.pos, head.first);
     __syncthreads();
-    for (int i = tid; i < lay.pieces; i += THREADS)
-      if (heads[i].top == top) atomicMin(&s.id, heads[i].first);
-    __syncthreads();
-    answer((int)s.id, 1.0, 1);
+    answer((int)s.pos, 1.0, 1);
     return;
   }
-  tb = bin_of(top, row.inv);
+  const double inv = row.inv, tb = uni(bin_of(top, inv));
+  const auto index_of = [&](float x) { return below(tb, bin_of(x, inv)); };
+
   // the pieces' histograms, each from its own maximum's bin down
-  uint32_t n = 0;
-  uint64_t fixed = 0;
-  if (tid < BINS)
-    for (int p = 0; p < lay.pieces; ++p) {
-      if (heads[p].top == -INFINITY) continue;
-      const int i = tid - below(tb, bin_of(heads[p].top, row.inv));
-      if (i < 0 || (uint32_t)i >= heads[p].used) continue;
-      n += ((const uint32_t*)(ws + lay.count_at))[p * BINS + i];
-      if (row.masses) fixed += ((const uint64_t*)(ws + lay.mass_at))[p * BINS + i];
-    }
-  bool masses = row.masses;
-  const double unit = tid < BINS ? exp64(-0.125 * tid) * 0x1p-44 : 0.0;
-  double all;
-  const double mass = scan_mass((double)fixed * unit, s, all);
-  uint32_t binned;
-  const uint32_t count = scan_count(n, s, binned);
-  if (tid < BINS) {
-    s.count[tid] = count;
-    s.mass[tid] = mass;
+  if (tid < lay.pieces) {
+    const bool some = head.top > -INFINITY;
+    s.shift[tid] = some ? index_of(head.top) : BINS;
+    s.used[tid] = some ? (int)head.used : 0;
   }
   __syncthreads();
-  const int64_t K = row.k > 0 ? min((int64_t)row.k, (int64_t)live) : (int64_t)live;
-  const bool cut_k = K < (int64_t)live && K <= (int64_t)binned;
-  const double low = row.least > 0.f ? log((double)row.least) : -INFINITY;
+  const double unit = exp64(-0.125 * tid) * 0x1p-44;
+  {
+    uint32_t n = 0;
+    uint64_t fixed = 0;
+#pragma unroll 4
+    for (int p = 0; p < lay.pieces; ++p) {
+      const int i = tid - s.shift[p];
+      const bool in = i >= 0 && i < s.used[p];
+      const int at = p * BINS + (in ? i : 0);
+      const uint32_t c = ((const uint32_t*)(ws + lay.count_at))[at];
+      const uint64_t m = row.masses ? ((const uint64_t*)(ws + lay.mass_at))[at] : 0;
+      n += in ? c : 0;
+      fixed += in ? m : 0;
+    }
+    scan_bins(s, n, (double)fixed * unit);
+  }
+  // First bin at which the sums cross; the last one that is not empty if none does.
+  const auto bin_where = [&](int mode, double value) {
+    const bool in = tid == 0 || s.count[tid] > s.count[tid - 1];
+    return first_of(s, in && crossed(mode, value, s.count[tid], s.mass[tid]), in);
+  };
+  const uint32_t binned = uni(s.count[BINS - 1]), K = row.k > 0 ? min((uint32_t)row.k, live) : live;
+  const bool cut_k = K < live && K <= binned;
+  const double low = row.least > 0.f ? uni(log((double)row.least)) : -INFINITY;
+  const float uf = a.u[b];
+  const double u = uf > 0.f ? (double)uf : 0.0;
+  const double low_bin = tb - floor(((double)top * inv + low) * 8.0);  // (0 or more; inf without min_p)
 
   // the last bin that matters
   const int bk = cut_k ? bin_where(COUNT, (double)K) : BINS - 1;
-  int last = bk;
-  if (row.p == 1.f || (masses && !cut_k)) {  // (else top-p's sum is that of the list)
-    if (row.least > 0.f) {
-      const double d = tb - floor(((double)top * row.inv + low) * 8.0) + 1.0;
-      if (d < (double)last) last = (int)d;
-    }
+  int last = bk, bp = -1;
+  if (row.p == 1.f || (row.masses && !cut_k)) {  // (else top-p's sum is that of the list)
+    if (low_bin + 1.0 < (double)last) last = uni((int)low_bin + 1);
     // (a little beyond the threshold, whose last bits are another sum's)
-    if (masses && row.p < 1.f) last = min(last, bin_where(REACH, (double)row.p * s.mass[BINS - 1] * (1.0 + 0x1p-40)));
+    if (row.masses && row.p < 1.f) {
+      bp = bin_where(REACH, (double)row.p * uni(s.mass[BINS - 1]) * (1.0 + 0x1p-40));
+      last = min(last, bp);
+    }
   }
-  if (s.count[last] <= (uint32_t)CAP) {
-    pick_chunks(last);
-    const int len = collect([=](float, int i) { return i <= last; });
-    if (len == 0) {  // (the logits have changed since the first kernel)
-      answer(-1, 0.0, 0);
-      return;
-    }
-    const int p = 2 * tid;
-    const double e0 = p < len ? mass_of(list_z(p)) : 0.0, e1 = p + 1 < len ? mass_of(list_z(p + 1)) : 0.0;
-    double sum;
-    const double m1 = scan_mass(e0 + e1, s, sum), m0 = m1 - e1;
-    s.upto[p] = p < len ? m0 : sum;
-    s.upto[p + 1] = m1;
-    __syncthreads();
-    int cut = (int)min((int64_t)len, K);
-    bool short_of = false;  // of the tokens below the bins, which have no mass
-    if (row.p < 1.f) {
-      double whole = s.upto[cut - 1];
-      if (masses && !cut_k) whole = s.mass[BINS - 1] * from_centre();
-      const double want = (double)row.p * whole;
-      const uint32_t who = first_of((p < cut && m0 >= want) || (p + 1 < cut && m1 >= want), s);
-      if (who < THREADS) {
-        cut = min(cut, (int)(2 * who + (s.upto[2 * who] >= want ? 1 : 2)));
-        short_of = true;
-      }
-    }
-    int64_t kept = short_of ? cut : cut == len && last == BINS - 1 ? K : cut;
-    if (row.least > 0.f) {
-      uint32_t c;
-      scan_count((p < len && ((double)list_z(p) - (double)top) * row.inv >= low ? 1u : 0u) +
-                     (p + 1 < len && ((double)list_z(p + 1) - (double)top) * row.inv >= low ? 1u : 0u),
-                 s, c);
-      if (kept > (int64_t)len && low < -60.0) c = at_least(low).count;  // (tokens below the bins may be above low)
-      kept = min(kept, (int64_t)max(c, 1u));
-      cut = min(cut, (int)min(kept, (int64_t)len));
-    }
-    const double part = s.upto[cut - 1], want = number() * part;
-    const uint32_t who = first_of((p < cut && m0 > want) || (p + 1 < cut && m1 > want), s);
-    const int at = who < THREADS ? (int)(2 * who + (s.upto[2 * who] > want ? 0 : 1)) : cut - 1;
-    answer(list_id(at), mass_of(list_z(at)) / part, kept);
-    return;
+  const bool whole = uni(s.count[last]) <= (uint32_t)CAP;
+  int f0 = 0, f1 = last, f2 = 1, f3 = 0;  // bins for the list
+  bool fits = whole;
+  if (!whole && row.masses && !cut_k && row.least == 0.f) {
+    // top-p's bin and those that the draw may fall into, if they fit
+    const double most = uni(s.mass[BINS - 1]), part = row.p < 1.f ? (double)row.p * most * (1.0 - 0x1p-40) : most;
+    f0 = bin_where(EXCEED, u * part);
+    f1 = row.p < 1.f ? bin_where(EXCEED, u * uni(s.mass[bp])) : f0;
+    if (bp > f1) f2 = f3 = bp;
+    const uint32_t total = s.count[f1] - (f0 ? s.count[f0 - 1] : 0) + (bp > f1 ? s.count[bp] - s.count[bp - 1] : 0);
+    fits = uni(total) <= (uint32_t)CAP;
   }
 
-  if (!masses) {  // counted only, and too many for a list after all
-    __syncthreads();
-    if (tid < BINS) s.sub_mass[tid] = 0;
-    pick_chunks(BINS - 1);
-    each([&](float x, int, int i, double bin) {
-      if (i < BINS) atomicAdd(&s.sub_mass[i], (unsigned long long)mass_in_bin(x, row.inv, bin));
-    });
-    __syncthreads();
-    const double v = scan_mass(tid < BINS ? (double)s.sub_mass[tid] * unit : 0.0, s, all);
-    if (tid < BINS) s.mass[tid] = v;
-    __syncthreads();
-  }
-  // top-k, top-p, min-p, the draw, and (where rounding has put it behind the cut) the last token before the cut
-  Sum cut{(uint32_t)K, s.mass[BINS - 1]};
-  Place at{{0, 0.0}, top, -1};
-  for (int step = 0; step < 5; ++step) {
-    int mode = COUNT;
-    double value = (double)K;
-    if (step == 0) {
-      if (!cut_k) continue;
-    } else if (step == 1) {
-      if (!(row.p < 1.f)) continue;
-      mode = REACH;
-      value = (double)row.p * cut.mass;
-    } else if (step == 2) {
-      if (row.least > 0.f) {
-        const Sum c = at_least(low);
-        if (c.count < cut.count) cut = c;
+  // Top-k, top-p, min-p, the draw, and (where rounding has put it behind the cut) the last token before the cut, as
+  // one sequence of passes over tokens.
+  enum { LIST, MASSES, NEXT, FIND, LEAST };
+  Pass p{};
+  p.top = top;
+  p.tb = tb;
+  p.inv = inv;
+  p.z = (const char*)a.z + (size_t)b * a.stride * (BF16 ? 2 : 4);
+  p.chunk_top = (const float*)(ws + lay.max_at);
+  p.V = a.V;
+  p.chunks = lay.chunks;
+  int state = fits ? LIST : row.masses ? NEXT : MASSES, step = -1;
+  bool in_list = fits;              // bins f0 .. f1 and f2 .. f3 are in it
+  Sum cut{K, 0.0};
+  uint32_t at_count = 0;            // of the draw's token: the count up to it, its logit, its id
+  float at_z = top;
+  int at_id = -1;
+  // the search of FIND: bin i, tokens and units of it ahead of places lo .. hi, tokens in them
+  int i = 0, mode = COUNT;
+  double value = 0.0, mass0 = 0.0, scale = 0.0;
+  uint32_t count0 = 0, n0 = 0, n = 0;
+  uint64_t m0 = 0, lo = 0, hi = 0;
+  bool listed = false;
+#pragma unroll 1
+  for (;;) {
+    if (state == NEXT) {
+      if (++step == 0) cut.mass = uni(s.mass[BINS - 1]);
+      if (step == 5) break;
+      mode = step == 1 ? REACH : step == 3 ? EXCEED : COUNT;
+      value = step == 0 ? (double)K : step == 1 ? (double)row.p * cut.mass : step == 3 ? u * cut.mass : (double)cut.count;
+      if (step == 0 && !cut_k) continue;
+      if (step == 0 && uni(s.count[bk]) == K) {
+        cut.mass = uni(s.mass[bk]);
+        continue;
       }
-      continue;
-    } else if (step == 3) {
-      mode = EXCEED;
-      value = number() * cut.mass;
+      if (step == 1 && row.p == 1.f) continue;
+      if (step == 2) {
+        if (row.least > 0.f) state = LEAST;
+        else continue;
+      } else {
+        if (step == 4 && at_count <= cut.count) break;
+        i = bin_where(mode, value);
+        count0 = uni(i ? s.count[i - 1] : 0u);
+        mass0 = uni(i ? s.mass[i - 1] : 0.0);
+        scale = uni(exp64(-0.125 * i) * 0x1p-44);
+        n = uni(s.count[i]) - count0;
+        n0 = 0;
+        m0 = 0;
+        listed = in_list && ((i >= f0 && i <= f1) || (i >= f2 && i <= f3));
+        lo = 0;
+        hi = ~0ull;
+        state = FIND;
+      }
+    }
+    // the pass
+    p.listed = p.append = p.by_bin = false;
+    p.b2 = 1;
+    p.b3 = p.sh = 0;
+    p.lo = 0;
+    p.hi = ~0ull;
+    p.low = -INFINITY;
+    if (state == LIST) {
+      p.append = true;
+      p.b0 = f0;
+      p.b1 = f1;
+      p.b2 = f2;
+      p.b3 = f3;
+    } else if (state == MASSES) {
+      p.listed = whole;
+      p.by_bin = true;
+      p.b0 = 0;
+      p.b1 = last;
+    } else if (state == LEAST) {
+      // the bin of the threshold and (for roundings) its neighbours, token by token; BINS: tokens without a mass
+      const int mid = low_bin < (double)BINS ? (int)low_bin : BINS;
+      p.b0 = uni(min(max(mid - 1, 0), BINS - 1));
+      p.b1 = uni(mid + 1 < BINS ? mid + 1 : BINS);
+      p.listed = in_list && f0 == 0 && p.b1 <= f1;
+      p.by_bin = true;
+      p.low = low;
     } else {
-      if (at.sum.count <= cut.count) continue;
-      value = (double)cut.count;
+      p.b0 = p.b1 = i;
     }
-    const Place p = cross(bin_where(mode, value), mode, value);
-    if (step >= 3) at = p;
-    else if (step == 0 || p.sum.count < cut.count) cut = p.sum;
-  }
-  answer(at.id, mass_of(at.z) / (cut.mass * from_centre()), cut.count);
-}
+    // The logits of those bins, a little wider than the roundings of the bins' formula and of these bounds.
+    {
+      const int first = p.b3 >= p.b2 ? min(p.b0, p.b2) : p.b0, end = max(p.b1, p.b3);
+      const double e0 = tb - end, e1 = tb - first, w = 0.125 * row.t * 0x1p-20;
+      const double z0 = e0 * 0.125 * row.t, z1 = (e1 + 1.0) * 0.125 * row.t;
+      const double l = z0 - fabs(z0) * 0x1p-20 - w - 1e-40, h = z1 + fabs(z1) * 0x1p-20 + w + 1e-40;
+      const bool fine = row.t < 1e60 && fabs(e0) < 0x1p52 && fabs(e1) < 0x1p52;
+      p.zlo = uni(fine && end < BINS && l > -(double)FLT_MAX ? (float)l : -FLT_MAX);
+      p.zhi = uni(fine && h < (double)top ? (float)h + 0.f : top);
+    }
+    if (state == FIND) {
+      lo = max(lo, place_of(p.zhi, 0));
+      hi = min(hi, place_of(p.zlo, (1 << ID_BITS) - 1));
+      p.append = !listed && n <= (uint32_t)CAP;
+      p.listed = listed;
+      p.lo = lo;
+      p.hi = hi;
+      p.sh = max(0, 64 - (int)__builtin_clzll((hi - lo) | 1) - 9);
+    }
+    if (state != FIND || !listed || n > 64) go_over<BF16>(s, p);
 
-template <bool BF16>
-__global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout lay) {
-  __shared__ Lds lds;
-  Decide<BF16> d(a, lay, lds);
-  d.run();
+    if (state == LIST) {
+      state = row.masses ? NEXT : MASSES;
+    } else if (state == MASSES) {  // counted only until now
+      const uint32_t c = s.count[tid] - (tid ? s.count[tid - 1] : 0);
+      scan_bins(s, c, (double)s.sub_mass[tid] * unit);
+      state = NEXT;
+    } else if (state == LEAST) {
+      uint32_t c = p.b0 ? s.count[p.b0 - 1] : 0;
+      double m = p.b0 ? s.mass[p.b0 - 1] : 0.0;
+#pragma unroll 1
+      for (int q = 0; q <= p.b1 - p.b0; ++q) {
+        c += s.sub_count[q];
+        m += (double)s.sub_mass[q] * (exp64(-0.125 * (p.b0 + q)) * 0x1p-44);
+      }
+      __syncthreads();
+      if (uni(c) < cut.count) cut = Sum{uni(c), uni(m)};
+      state = NEXT;
+    } else if (p.append) {
+      in_list = false;  // (this bin's tokens only)
+      listed = true;
+    } else if (!listed || n > 64) {
+      const uint32_t mine = s.sub_count[tid];
+      const uint64_t mass = s.sub_mass[tid];
+      uint32_t c = mine;
+      uint64_t m = mass;
+      scan_both(s, c, m);
+      const int who = first_of(s, mine > 0 && crossed(mode, value, count0 + n0 + c, mass0 + scale * (double)(m0 + m)), mine > 0);
+      if (who >= THREADS) {  // (the logits have changed since the first kernel)
+        state = NEXT;
+        continue;
+      }
+      __syncthreads();
+      if (tid == who) {
+        s.at = mine;
+        s.pos = c - mine;
+        s.mass_at = m - mass;
+      }
+      __syncthreads();
+      n = uni(s.at);
+      n0 += uni(s.pos);
+      m0 += uni(s.mass_at);
+      lo += (uint64_t)who << p.sh;
+      hi = min(hi, lo + ((1ull << p.sh) - 1));
+    } else {
+      // the last few, in one wave
+      __syncthreads();
+      if (tid == 0) s.pos = 0;
+      __syncthreads();
+#pragma unroll 1
+      for (uint32_t t = tid; t < s.n; t += THREADS) {
+        const uint64_t q = s.list[t];
+        if (q >= lo && q <= hi && index_of(place_z(q)) == i) {
+          const uint32_t to = atomicAdd(&s.pos, 1u);
+          if (to < 64) s.few[to] = q;
+        }
+      }
+      __syncthreads();
+      const int len = (int)min(uni(s.pos), 64u);
+      state = NEXT;
+      if (len == 0) continue;
+      __syncthreads();
+      if (wave == 0) {
+        // a token's rank is the number of those ahead of it, and so are its sums
+        const uint64_t q = lane < len ? s.few[lane] : ~0ull;
+        const uint64_t e = lane < len ? mass_in_bin(place_z(q), inv, bin_of(place_z(q), inv)) : 0;
+        uint32_t rank = 0;
+        uint64_t m = m0 + e;
+#pragma unroll 1
+        for (int x = 0; x < len; ++x) {
+          const uint64_t other = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(q >> 32), x) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)q, x);
+          const uint64_t units = ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(e >> 32), x) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)e, x);
+          rank += other < q ? 1 : 0;
+          m += other < q ? units : 0;
+        }
+        const uint64_t yes = __ballot(lane < len && crossed(mode, value, count0 + n0 + rank + 1, mass0 + scale * (double)m));
+        // (once crossed, all later ones are: the first of them is as many from the end as there are)
+        const uint32_t at = len - (yes ? __builtin_popcountll(yes) : 1);
+        if (lane < len && rank == at) {
+          s.place = q;
+          s.mass_at = m;
+          s.pos = n0 + rank + 1;
+        }
+      }
+      __syncthreads();
+      const Sum sum{count0 + uni(s.pos), mass0 + scale * (double)uni(s.mass_at)};
+      const uint64_t found = uni(s.place);
+      if (step >= 3) {
+        at_count = sum.count;
+        at_z = place_z(found);
+        at_id = place_id(found);
+      } else if (step == 0 || sum.count < cut.count) {
+        cut = sum;
+      }
+    }
+  }
+  // the mass at the centre of the first bin relative to the largest logit's
+  const double c = fabs(tb) < 0x1p52 ? -__builtin_fma((double)top, inv, -(tb + 0.5) * 0.125) : 0.0;
+  const double e = exp64(-fabs(c)), mine = exp64(((double)at_z - (double)top) * inv);
+  answer(at_id, c < 0 ? mine / (cut.mass * e) : mine * e / cut.mass, cut.count);
 }
 
 template <bool BF16>
