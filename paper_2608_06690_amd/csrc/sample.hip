@@ -35,7 +35,6 @@ constexpr int ID_BITS = 19;
 constexpr int COUNT_K = CAP / 4;
 
 typedef u32x4 u32x4_a2 __attribute__((aligned(2)));
-typedef f32x4 f32x4_a4 __attribute__((aligned(4)));
 
 __device__ __forceinline__ uint32_t key_of(float z) {
   const uint32_t b = __float_as_uint(z);
@@ -45,31 +44,51 @@ __device__ __forceinline__ float z_of(uint32_t k) { return __uint_as_float((k >>
 // A logit as it counts: masked ones (also NaN) -inf, +inf the largest finite value, -0 as 0.
 __device__ __forceinline__ float canon(float v) { return v > -INFINITY ? fminf(v, FLT_MAX) + 0.f : -INFINITY; }
 
-// Logits [i, i + 8) of a row of n (past it: -inf).
+// Logits [i, i + 8) of a row of n as they lie in memory: the last 8 of the row where those reach past its end, so that
+// every load is whole and none waits for a branch. Rows of fewer than 8 are read one by one.
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* row, int i, int n, float (&v)[8]) {
-  if (i + 8 <= n) {
-    if constexpr (BF16) {
-      const u32x4 q = *(const u32x4_a2*)((const uint16_t*)row + i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[2 * j] = bf16_to_f32(q[j] & 0xFFFFu);
-        v[2 * j + 1] = __uint_as_float(q[j] & 0xFFFF0000u);
-      }
-    } else {
-      const f32x4 a = *(const f32x4_a4*)((const float*)row + i), b = *(const f32x4_a4*)((const float*)row + i + 4);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = a[j];
-        v[4 + j] = b[j];
-      }
-    }
+struct Eight {
+  u32x4 q[BF16 ? 1 : 2];
+  int at;    // index of the first of them
+  int skip;  // so many of them are ahead of i
+};
+template <bool BF16>
+__device__ __forceinline__ Eight<BF16> load8(const char* row, int i, int n) {
+  Eight<BF16> e;
+  e.at = min(i, n - 8);
+  e.skip = i - e.at;
+  if (n >= 8) {
+    const char* p = row + (size_t)e.at * (BF16 ? 2 : 4);
+    e.q[0] = *(const u32x4_a2*)p;
+    if constexpr (!BF16) e.q[1] = *(const u32x4_a2*)(p + 16);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] = -INFINITY;
-      if (i + j < n) v[j] = BF16 ? bf16_to_f32(((const uint16_t*)row)[i + j]) : ((const float*)row)[i + j];
+    for (int j = 0; j < (BF16 ? 4 : 8); ++j) {
+      const int k = e.at + (BF16 ? 2 * j : j);
+      uint32_t w = 0;
+      if constexpr (BF16) {
+        if (k >= 0) w = ((const uint16_t*)row)[k];
+        if (k >= -1) w |= (uint32_t)((const uint16_t*)row)[k + 1] << 16;
+      } else {
+        if (k >= 0) w = ((const uint32_t*)row)[k];
+      }
+      e.q[j / 4][j & 3] = w;
     }
+    e.skip = max(e.skip, -e.at);
+  }
+  return e;
+}
+template <bool BF16>
+__device__ __forceinline__ float value_of(const Eight<BF16>& e, int j) {
+  const uint32_t w = BF16 ? e.q[0][j / 2] : e.q[BF16 ? 0 : j / 4][j & 3];
+  return __uint_as_float(BF16 ? (j & 1) ? w & 0xFFFF0000u : w << 16 : w);
+}
+// Their values as they count; -inf for those ahead of i.
+template <bool BF16>
+__device__ __forceinline__ void values8(const Eight<BF16>& e, float (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] = j >= e.skip ? canon(value_of<BF16>(e, j)) : -INFINITY;
   }
 }
 
@@ -165,8 +184,9 @@ __global__ __launch_bounds__(HIST_THREADS) void sample_hist_kernel(SampleArgs a,
   char* ws = (char*)a.ws + (size_t)b * lay.row;
   const int base = piece * (G8 * PIECE8) + tid * 8;
   float v[G8][8];
+  Eight<BF16> raw[G8];
 #pragma unroll
-  for (int g = 0; g < G8; ++g) load8<BF16>(z, base + g * PIECE8, a.V, v[g]);
+  for (int g = 0; g < G8; ++g) raw[g] = load8<BF16>(z, base + g * PIECE8, a.V);
   for (int i = tid; i < BINS; i += HIST_THREADS) {
     s_mass[i] = 0;
     s_count[i] = 0;
@@ -180,11 +200,9 @@ __global__ __launch_bounds__(HIST_THREADS) void sample_hist_kernel(SampleArgs a,
 #pragma unroll
   for (int g = 0; g < G8; ++g) {
     float m = -INFINITY;
+    values8<BF16>(raw[g], v[g]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[g][j] = canon(v[g][j]);
-      m = fmaxf(m, v[g][j]);
-    }
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, v[g][j]);
     m = wave_max(m);
     top = fmaxf(top, m);
     const int chunk = (base + g * PIECE8) / CHUNK;
@@ -201,7 +219,7 @@ __global__ __launch_bounds__(HIST_THREADS) void sample_hist_kernel(SampleArgs a,
     for (int g = G8 - 1; g >= 0; --g)
 #pragma unroll
       for (int j = 7; j >= 0; --j)
-        if (v[g][j] == top) first = base + g * PIECE8 + j;
+        if (v[g][j] == top) first = raw[g].at + j;
     if (first != 0xFFFFFFFFu) atomicMin(&s_first, first);
     __syncthreads();
     if (tid == 0) *head = Head{top, s_first, top == -INFINITY ? 0u : 1u, 0u};
@@ -262,7 +280,7 @@ struct Lds {
   double wave_mass[THREADS / 64];
   uint64_t wave_u[THREADS / 64];
   uint32_t wave_count[THREADS / 64];
-  uint32_t chunks, n, at, pos;
+  uint32_t chunks, n, at, pos, rest;
   uint64_t place, mass_at;
 };
 
@@ -350,16 +368,14 @@ __device__ __forceinline__ uint64_t place_of(float z, int id) { return ((uint64_
 __device__ __forceinline__ float place_z(uint64_t p) { return z_of(~(uint32_t)(p >> ID_BITS)); }
 __device__ __forceinline__ int place_id(uint64_t p) { return (int)(p & ((1u << ID_BITS) - 1)); }
 
-// One way over tokens: those of the list, or of the row's chunks that hold a logit of [zlo, zhi]. A token counts if its
-// bin is in b0 .. b1 or b2 .. b3 (BINS: below the bins), its place in lo .. hi and (z - top) / temperature at least
-// low. It is appended to the list, or counted, with its mass, in place (place - lo) >> sh, or its bin - b0, of the
-// sub-histogram.
+// One way over tokens: those of the list, or of the row's chunks that hold a logit of z0 .. z1 or z2 .. z3. Of these,
+// tokens count whose place is in lo .. hi. They are appended to the list, or counted, with their masses, in place
+// (place - lo) >> sh, or (by_bin) in their bin's, of the sub-histogram (`rest`: below the bins).
 struct Pass {
   bool listed, append, by_bin;
-  int b0, b1, b2, b3, sh;
-  float zlo, zhi;
+  int sh;
+  float z0, z1, z2, z3;
   uint64_t lo, hi;
-  double low;
   // the row
   float top;
   double tb, inv;
@@ -367,25 +383,6 @@ struct Pass {
   const float* chunk_top;
   int V, chunks;
 };
-__device__ __forceinline__ void take(Lds& s, const Pass& p, bool in, float x, uint64_t at) {
-  const double bin = bin_of(x, p.inv);
-  const int i = below(p.tb, bin);
-  in = in && ((i >= p.b0 && i <= p.b1) || (i >= p.b2 && i <= p.b3)) && at >= p.lo && at <= p.hi && ((double)x - (double)p.top) * p.inv >= p.low;
-  if (p.append) {
-    const uint64_t mask = __ballot(in);
-    if (!mask) return;
-    uint32_t to = 0;
-    if (lane_id() == 0) to = atomicAdd(&s.n, (uint32_t)__builtin_popcountll(mask));
-    to = uni(to) + __builtin_popcountll(mask & ((1ull << lane_id()) - 1));
-    if (in && to < CAP) s.list[to] = at;
-  } else if (in) {
-    const uint32_t q = p.by_bin ? (uint32_t)(i - p.b0) : (uint32_t)((at - p.lo) >> p.sh);
-    if (q < BINS) {
-      atomicAdd(&s.sub_count[q], 1u);
-      if (i < BINS) atomicAdd(&s.sub_mass[q], (unsigned long long)mass_in_bin(x, p.inv, bin));
-    }
-  }
-}
 template <bool BF16>
 __device__ __forceinline__ void go_over(Lds& s, const Pass& p) {
   const int tid = threadIdx.x, lane = lane_id(), wave = uni(tid >> 6);
@@ -397,14 +394,18 @@ __device__ __forceinline__ void go_over(Lds& s, const Pass& p) {
     s.sub_mass[tid] = 0;
     s.sub_count[tid] = 0;
   }
-  if (tid == 0) s.chunks = 0;
+  if (tid == 0) {
+    s.chunks = 0;
+    s.rest = 0;
+  }
   __syncthreads();
   // the chunks that hold one
   if (!p.listed) {
+    const float least = fminf(p.z0, p.z2);
 #pragma unroll 1
     for (int c0 = 0; c0 < p.chunks; c0 += THREADS) {
       const int c = c0 + tid;
-      const bool in = c < p.chunks && p.chunk_top[c] >= p.zlo;
+      const bool in = c < p.chunks && p.chunk_top[c] >= least;
       const uint64_t mask = __ballot(in);
       uint32_t at = 0;
       if (lane == 0 && mask) at = atomicAdd(&s.chunks, (uint32_t)__builtin_popcountll(mask));
@@ -415,14 +416,10 @@ __device__ __forceinline__ void go_over(Lds& s, const Pass& p) {
   }
   // (the list goes through the same steps, one of its places a lane)
   const uint32_t n = uni(p.listed ? s.n : s.chunks);
-  float next[U][8];
-  int next_at[U];
+  Eight<BF16> next[U];
   const auto load = [&](uint32_t c) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      next_at[u] = c + u < n ? s.chunk[c + u] * CHUNK + lane * 8 : p.V;
-      load8<BF16>(p.z, next_at[u], p.V, next[u]);
-    }
+    for (int u = 0; u < U; ++u) next[u] = load8<BF16>(p.z, c + u < n ? s.chunk[c + u] * CHUNK + lane * 8 : p.V, p.V);
   };
   if (!p.listed) load(wave * U);
   const uint32_t step = p.listed ? THREADS : WAVES * U;
@@ -435,18 +432,35 @@ __device__ __forceinline__ void go_over(Lds& s, const Pass& p) {
     if (p.listed) {
       if (c + lane < n) {
         place = s.list[c + lane];
-        left = 1;
+        left = place >= p.lo && place <= p.hi && place_z(place) >= p.z0 && place_z(place) <= p.z1 ? 1u : 0u;
       }
     } else {
+      // (a bit for each of the lane's logits that counts; NaN does in no comparison, and without an upper end +inf does)
+      Eight<BF16> now[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        at[u] = next_at[u];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[u * 8 + j] = canon(next[u][j]);
-      }
+      for (int u = 0; u < U; ++u) now[u] = next[u];
       load(c + step);
 #pragma unroll
-      for (int j = 0; j < 8 * U; ++j) left |= v[j] >= p.zlo && v[j] <= p.zhi ? 1u << j : 0u;
+      for (int u = 0; u < U; ++u) {
+        at[u] = now[u].at;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u * 8 + j] = value_of<BF16>(now[u], j);
+      }
+#pragma unroll
+      for (int j = 0; j < 8 * U; ++j) left |= v[j] >= p.z0 ? 1u << j : 0u;
+      if (p.z1 < p.top) {
+        uint32_t above = 0;
+#pragma unroll
+        for (int j = 0; j < 8 * U; ++j) above |= v[j] > p.z1 ? 1u << j : 0u;
+        left &= ~above;
+      }
+      if (p.z2 <= p.z3) {
+#pragma unroll
+        for (int j = 0; j < 8 * U; ++j) left |= v[j] >= p.z2 && v[j] <= p.z3 ? 1u << j : 0u;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (now[u].skip > 0) left &= ~(((1u << min(now[u].skip, 8)) - 1) << (8 * u));
     }
     while (__any(left != 0)) {
       const int j = left ? __builtin_ctz(left) : 0;
@@ -458,15 +472,61 @@ __device__ __forceinline__ void go_over(Lds& s, const Pass& p) {
         int id = at[0];
 #pragma unroll
         for (int u = 1; u < U; ++u) id = j >= 8 * u ? at[u] : id;
+        x = canon(x);
         place = place_of(x, id + (j & 7));
       }
-      take(s, p, left != 0, x, place);
+      const bool in = left != 0 && place >= p.lo && place <= p.hi;
+      if (p.append) {
+        const uint64_t mask = __ballot(in);
+        uint32_t to = 0;
+        if (lane == 0) to = atomicAdd(&s.n, (uint32_t)__builtin_popcountll(mask));
+        to = uni(to) + __builtin_popcountll(mask & ((1ull << lane) - 1));
+        if (in && to < CAP) s.list[to] = place;
+      } else if (in) {
+        const double bin = bin_of(x, p.inv);
+        const int i = below(p.tb, bin);
+        const uint32_t q = p.by_bin ? (uint32_t)i : (uint32_t)((place - p.lo) >> p.sh);
+        atomicAdd(q < BINS ? &s.sub_count[q] : &s.rest, 1u);
+        if (q < BINS && i < BINS) atomicAdd(&s.sub_mass[q], (unsigned long long)mass_in_bin(x, p.inv, bin));
+      }
       left &= left - 1;
     }
   }
   __syncthreads();
   if (p.append && tid == 0) s.n = min(s.n, (uint32_t)CAP);
   __syncthreads();
+}
+
+// The smallest logit of [-FLT_MAX, top] that `ok` holds for, where it holds for all larger ones and for top: a wave tries
+// 64 logits at a time, first those around `near`.
+template <class F>
+__device__ __forceinline__ float smallest(float near, float top, F ok) {
+  uint32_t a = key_of(-FLT_MAX), b = key_of(top);
+  const uint32_t from = min(max(key_of(near), a + 32) - 32, b);
+  uint32_t k = min(from + lane_id(), b);
+  uint64_t yes = __ballot(ok(z_of(k)));
+  if (yes == 0) {
+    a = min(uni(from) + 64, b);
+  } else if (yes & 1) {
+    b = uni(from);
+  } else {
+    return z_of(uni(from) + (uint32_t)__builtin_ctzll(yes));
+  }
+#pragma unroll 1
+  while (a < b) {
+    const uint32_t step = ((b - a) >> 6) + 1;
+    k = b - a < step * lane_id() ? b : a + step * lane_id();
+    yes = __ballot(ok(z_of(k)) || k == b);
+    const int f = yes ? __builtin_ctzll(yes) : 63;
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)k, f);
+    if (f == 0) {
+      b = a;
+    } else {
+      a = min(at, (uint32_t)__builtin_amdgcn_readlane((int)k, f - 1) + 1);
+      b = at;
+    }
+  }
+  return z_of(a);
 }
 
 enum { COUNT, REACH, EXCEED };  // what crosses a value: the count, the mass reaching or exceeding it
@@ -522,6 +582,12 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
   }
   const double inv = row.inv, tb = uni(bin_of(top, inv));
   const auto index_of = [&](float x) { return below(tb, bin_of(x, inv)); };
+  // The smallest logit of bin i or a nearer one, and the largest of bin i or a farther one.
+  const auto low_edge = [&](int i) {
+    if (i >= BINS) return -FLT_MAX;
+    return smallest((float)fmin(fmax((tb - i) * 0.125 * row.t, -(double)FLT_MAX), (double)top), top, [&](float x) { return index_of(x) <= i; });
+  };
+  const auto high_edge = [&](int i) { return i == 0 ? top : z_of(key_of(low_edge(i - 1)) - 1); };
 
   // the pieces' histograms, each from its own maximum's bin down
   if (tid < lay.pieces) {
@@ -553,16 +619,22 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
   };
   const uint32_t binned = uni(s.count[BINS - 1]), K = row.k > 0 ? min((uint32_t)row.k, live) : live;
   const bool cut_k = K < live && K <= binned;
-  const double low = row.least > 0.f ? uni(log((double)row.least)) : -INFINITY;
+  // the smallest logit that min-p leaves, and its bin
+  float least = -INFINITY;
+  int bm = BINS;
+  if (row.least > 0.f) {
+    const double low = uni(log((double)row.least));
+    least = smallest((float)fmax((double)top + low * row.t, -(double)FLT_MAX), top, [&](float x) { return ((double)x - (double)top) * inv >= low; });
+    bm = uni(index_of(least));
+  }
   const float uf = a.u[b];
   const double u = uf > 0.f ? (double)uf : 0.0;
-  const double low_bin = tb - floor(((double)top * inv + low) * 8.0);  // (0 or more; inf without min_p)
 
   // the last bin that matters
   const int bk = cut_k ? bin_where(COUNT, (double)K) : BINS - 1;
   int last = bk, bp = -1;
   if (row.p == 1.f || (row.masses && !cut_k)) {  // (else top-p's sum is that of the list)
-    if (low_bin + 1.0 < (double)last) last = uni((int)low_bin + 1);
+    last = min(last, bm);
     // (a little beyond the threshold, whose last bits are another sum's)
     if (row.masses && row.p < 1.f) {
       bp = bin_where(REACH, (double)row.p * uni(s.mass[BINS - 1]) * (1.0 + 0x1p-40));
@@ -604,7 +676,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
   double value = 0.0, mass0 = 0.0, scale = 0.0;
   uint32_t count0 = 0, n0 = 0, n = 0;
   uint64_t m0 = 0, lo = 0, hi = 0;
-  bool listed = false;
+  bool listed = false, fresh = false;
 #pragma unroll 1
   for (;;) {
     if (state == NEXT) {
@@ -631,53 +703,43 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
         n0 = 0;
         m0 = 0;
         listed = in_list && ((i >= f0 && i <= f1) || (i >= f2 && i <= f3));
-        lo = 0;
-        hi = ~0ull;
+        fresh = true;
         state = FIND;
       }
     }
     // the pass
-    p.listed = p.append = p.by_bin = false;
-    p.b2 = 1;
-    p.b3 = p.sh = 0;
+    int b0 = i, b1 = i;
+    if (state == LIST) {
+      b0 = f0;
+      b1 = f1;
+    } else if (state == MASSES) {
+      b0 = 0;
+      b1 = last;
+    } else if (state == LEAST) {
+      b0 = b1 = bm;  // (BINS: tokens without a mass)
+    }
+    p.append = state == LIST;
+    p.by_bin = state == MASSES || state == LEAST;
+    p.listed = state == MASSES ? whole : state == LEAST ? in_list && f0 == 0 && bm <= f1 : false;
     p.lo = 0;
     p.hi = ~0ull;
-    p.low = -INFINITY;
-    if (state == LIST) {
-      p.append = true;
-      p.b0 = f0;
-      p.b1 = f1;
-      p.b2 = f2;
-      p.b3 = f3;
-    } else if (state == MASSES) {
-      p.listed = whole;
-      p.by_bin = true;
-      p.b0 = 0;
-      p.b1 = last;
-    } else if (state == LEAST) {
-      // the bin of the threshold and (for roundings) its neighbours, token by token; BINS: tokens without a mass
-      const int mid = low_bin < (double)BINS ? (int)low_bin : BINS;
-      p.b0 = uni(min(max(mid - 1, 0), BINS - 1));
-      p.b1 = uni(mid + 1 < BINS ? mid + 1 : BINS);
-      p.listed = in_list && f0 == 0 && p.b1 <= f1;
-      p.by_bin = true;
-      p.low = low;
-    } else {
-      p.b0 = p.b1 = i;
-    }
-    // The logits of those bins, a little wider than the roundings of the bins' formula and of these bounds.
-    {
-      const int first = p.b3 >= p.b2 ? min(p.b0, p.b2) : p.b0, end = max(p.b1, p.b3);
-      const double e0 = tb - end, e1 = tb - first, w = 0.125 * row.t * 0x1p-20;
-      const double z0 = e0 * 0.125 * row.t, z1 = (e1 + 1.0) * 0.125 * row.t;
-      const double l = z0 - fabs(z0) * 0x1p-20 - w - 1e-40, h = z1 + fabs(z1) * 0x1p-20 + w + 1e-40;
-      const bool fine = row.t < 1e60 && fabs(e0) < 0x1p52 && fabs(e1) < 0x1p52;
-      p.zlo = uni(fine && end < BINS && l > -(double)FLT_MAX ? (float)l : -FLT_MAX);
-      p.zhi = uni(fine && h < (double)top ? (float)h + 0.f : top);
+    if (state != FIND || fresh) {
+      p.z0 = low_edge(b1);
+      p.z1 = high_edge(b0);
+      p.z2 = INFINITY;
+      p.z3 = -INFINITY;
+      if (state == LIST && f3 >= f2) {
+        p.z2 = low_edge(f3);
+        p.z3 = high_edge(f2);
+      }
+      if (state == LEAST) p.z0 = least;
     }
     if (state == FIND) {
-      lo = max(lo, place_of(p.zhi, 0));
-      hi = min(hi, place_of(p.zlo, (1 << ID_BITS) - 1));
+      if (fresh) {
+        lo = place_of(p.z1, 0);
+        hi = place_of(p.z0, (1 << ID_BITS) - 1);
+        fresh = false;
+      }
       p.append = !listed && n <= (uint32_t)CAP;
       p.listed = listed;
       p.lo = lo;
@@ -693,13 +755,9 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
       scan_bins(s, c, (double)s.sub_mass[tid] * unit);
       state = NEXT;
     } else if (state == LEAST) {
-      uint32_t c = p.b0 ? s.count[p.b0 - 1] : 0;
-      double m = p.b0 ? s.mass[p.b0 - 1] : 0.0;
-#pragma unroll 1
-      for (int q = 0; q <= p.b1 - p.b0; ++q) {
-        c += s.sub_count[q];
-        m += (double)s.sub_mass[q] * (exp64(-0.125 * (p.b0 + q)) * 0x1p-44);
-      }
+      // (tokens below the bins are counted in none of them)
+      const uint32_t c = bm == BINS ? binned + s.rest : (bm ? s.count[bm - 1] : 0) + s.sub_count[bm];
+      const double m = bm == BINS ? s.mass[BINS - 1] : (bm ? s.mass[bm - 1] : 0.0) + (double)s.sub_mass[bm] * (exp64(-0.125 * bm) * 0x1p-44);
       __syncthreads();
       if (uni(c) < cut.count) cut = Sum{uni(c), uni(m)};
       state = NEXT;
@@ -737,7 +795,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
 #pragma unroll 1
       for (uint32_t t = tid; t < s.n; t += THREADS) {
         const uint64_t q = s.list[t];
-        if (q >= lo && q <= hi && index_of(place_z(q)) == i) {
+        if (q >= lo && q <= hi) {
           const uint32_t to = atomicAdd(&s.pos, 1u);
           if (to < 64) s.few[to] = q;
         }
