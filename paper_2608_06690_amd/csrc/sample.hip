@@ -42,7 +42,7 @@ __device__ __forceinline__ uint32_t key_of(float z) {
 }
 __device__ __forceinline__ float z_of(uint32_t k) { return __uint_as_float((k >> 31) ? k ^ 0x80000000u : ~k); }
 // A logit as it counts: masked ones (also NaN) -inf, +inf the largest finite value, -0 as 0.
-__device__ __forceinline__ float canon(float v) { return v > -INFINITY ? fminf(v, FLT_MAX) + 0.f : -INFINITY; }
+__device__ __forceinline__ float canon(float v) { return fminf(fmaxf(v, -INFINITY), FLT_MAX) + 0.f; }  // (a maximum leaves NaN out)
 
 // Logits [i, i + 8) of a row of n as they lie in memory: the last 8 of the row where those reach past its end, so that
 // every load is whole and none waits for a branch. Rows of fewer than 8 are read one by one.
@@ -144,21 +144,49 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int b) {
   return r;
 }
 
-// The bin of a logit, counted in eighths from 0 up, and its place from its centre.
-__device__ __forceinline__ double bin_of(float z, double inv) { return floor((double)z * inv * 8.0); }
-__device__ __forceinline__ int below(double top, double bin) {
-  const double d = top - bin;
-  return d < (double)BINS ? (int)d : BINS;
+// The bins of a row: floor(fl(z 8 / T)) in fp32, counted down from that of the row's (or a piece's) largest logit. What
+// counts is that this never falls with z; a logit may lie beyond its bin's edges by 2^-23 of 8 z / T, and its mass is that
+// of its exact place. Where 8 z / T is 2^20 or more at the top (temperatures next to 0, say), fp64 makes the bins.
+struct Bins {
+  double inv;   // 1 / T
+  float inv8;   // 8 / T
+  bool far;
+  double top;   // the first bin (a whole number)
+};
+__device__ __forceinline__ Bins bins_of(const Row& r, float top) {
+  Bins b;
+  b.inv = r.inv;
+  b.inv8 = (float)(8.0 * r.inv);
+  b.far = !(fabsf(top * b.inv8) < 0x1p20f);
+  b.top = b.far ? floor((double)top * r.inv * 8.0) : (double)floorf(top * b.inv8);
+  return b;
 }
-// exp of the place in units of 2^-44. |place| <= 1/16: the Taylor sum up to r^8 is off by 2^-54. (Far
-// out, where eighths are below the spacing of fp64, every logit has a bin of its own and the place is 0.)
-__device__ __forceinline__ uint64_t mass_in_bin(float z, double inv, double bin) {
-  const double r = fabs(bin) < 0x1p52 ? __builtin_fma((double)z, inv, -(bin + 0.5) * 0.125) : 0.0;
-  double p = 1.0 / 40320.0;
-  p = __builtin_fma(p, r, 1.0 / 5040.0);
-  p = __builtin_fma(p, r, 1.0 / 720.0);
-  p = __builtin_fma(p, r, 1.0 / 120.0);
-  p = __builtin_fma(p, r, 1.0 / 24.0);
+// BINS where a logit lies below them.
+__device__ __forceinline__ int bin_of(const Bins& b, float z) {
+  if (b.far) {
+    const double d = b.top - floor((double)z * b.inv * 8.0);
+    return d < (double)BINS ? (int)d : BINS;
+  }
+  const float d = (float)b.top - floorf(z * b.inv8);
+  return d < (float)BINS ? (int)d : BINS;
+}
+// The logit's place from the centre of bin i over the temperature, at most 0.08. (Far out, where eighths are below the
+// spacing of fp64, every logit has a bin of its own and the place is 0.)
+__device__ __forceinline__ double place_in_bin(const Bins& b, float z, int i) {
+  if (b.far && !(fabs(b.top) < 0x1p51)) return 0.0;
+  return __builtin_fma((double)z, b.inv, -((b.top - i) + 0.5) * 0.125);
+}
+// exp of that in units of 2^-44. The terms from r^4 on are below 2^-19 and come from fp32, off by 2^-43; with r^9
+// and later left out, by 2^-51.
+__device__ __forceinline__ uint64_t units_in_bin(const Bins& b, float z, int i) {
+  const double r = place_in_bin(b, z, i);
+  const float f = (float)r;
+  float q = 1.f / 40320.f;
+  q = __builtin_fmaf(q, f, 1.f / 5040.f);
+  q = __builtin_fmaf(q, f, 1.f / 720.f);
+  q = __builtin_fmaf(q, f, 1.f / 120.f);
+  q = __builtin_fmaf(q, f, 1.f / 24.f);
+  double p = (double)q;
   p = __builtin_fma(p, r, 1.0 / 6.0);
   p = __builtin_fma(p, r, 0.5);
   p = __builtin_fma(p, r, 1.0);
@@ -225,22 +253,28 @@ __global__ __launch_bounds__(HIST_THREADS) void sample_hist_kernel(SampleArgs a,
     if (tid == 0) *head = Head{top, s_first, top == -INFINITY ? 0u : 1u, 0u};
     return;
   }
-  const double tb = bin_of(top, row.inv);
+  const Bins bins = bins_of(row, top);
   uint32_t rest = 0;
+  if (bins.far) {  // the second kernel does without this histogram
 #pragma unroll
-  for (int g = 0; g < G8; ++g)
+    for (int g = 0; g < G8; ++g)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (v[g][j] == -INFINITY) continue;
-      const double bin = bin_of(v[g][j], row.inv);
-      const int i = below(tb, bin);
-      if (i < BINS) {
-        atomicAdd(&s_count[i], 1u);
-        if (row.masses) atomicAdd(&s_mass[i], (unsigned long long)mass_in_bin(v[g][j], row.inv, bin));
-      } else {
-        ++rest;
+      for (int j = 0; j < 8; ++j) rest += v[g][j] > -INFINITY ? 1 : 0;
+  } else {
+#pragma unroll
+    for (int g = 0; g < G8; ++g)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float z = v[g][j], d = (float)bins.top - floorf(z * bins.inv8);
+        if (d < (float)BINS) {
+          const int i = (int)d;
+          atomicAdd(&s_count[i], 1u);
+          if (row.masses) atomicAdd(&s_mass[i], (unsigned long long)units_in_bin(bins, z, i));
+        } else {
+          rest += z > -INFINITY ? 1 : 0;
+        }
       }
-    }
+  }
   rest = (uint32_t)wave_sum_int((int)rest);
   if (lane == 0 && rest) atomicAdd(&s_live, rest);
   __syncthreads();
@@ -378,7 +412,7 @@ struct Pass {
   uint64_t lo, hi;
   // the row
   float top;
-  double tb, inv;
+  Bins bins;
   const char* z;
   const float* chunk_top;
   int V, chunks;
@@ -483,11 +517,10 @@ __device__ __forceinline__ void go_over(Lds& s, const Pass& p) {
         to = uni(to) + __builtin_popcountll(mask & ((1ull << lane) - 1));
         if (in && to < CAP) s.list[to] = place;
       } else if (in) {
-        const double bin = bin_of(x, p.inv);
-        const int i = below(p.tb, bin);
+        const int i = bin_of(p.bins, x);
         const uint32_t q = p.by_bin ? (uint32_t)i : (uint32_t)((place - p.lo) >> p.sh);
         atomicAdd(q < BINS ? &s.sub_count[q] : &s.rest, 1u);
-        if (q < BINS && i < BINS) atomicAdd(&s.sub_mass[q], (unsigned long long)mass_in_bin(x, p.inv, bin));
+        if (q < BINS && i < BINS) atomicAdd(&s.sub_mass[q], (unsigned long long)units_in_bin(p.bins, x, i));
       }
       left &= left - 1;
     }
@@ -580,18 +613,22 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
     answer((int)s.pos, 1.0, 1);
     return;
   }
-  const double inv = row.inv, tb = uni(bin_of(top, inv));
-  const auto index_of = [&](float x) { return below(tb, bin_of(x, inv)); };
+  const double inv = row.inv;
+  Bins bins = bins_of(row, top);
+  bins.inv8 = uni(bins.inv8);
+  bins.top = uni(bins.top);
+  bins.far = uni((int)bins.far) != 0;
+  const auto index_of = [&](float x) { return bin_of(bins, x); };
   // The smallest logit of bin i or a nearer one, and the largest of bin i or a farther one.
   const auto low_edge = [&](int i) {
     if (i >= BINS) return -FLT_MAX;
-    return smallest((float)fmin(fmax((tb - i) * 0.125 * row.t, -(double)FLT_MAX), (double)top), top, [&](float x) { return index_of(x) <= i; });
+    return smallest((float)fmin(fmax((bins.top - i) * 0.125 * row.t, -(double)FLT_MAX), (double)top), top, [&](float x) { return index_of(x) <= i; });
   };
   const auto high_edge = [&](int i) { return i == 0 ? top : z_of(key_of(low_edge(i - 1)) - 1); };
 
   // the pieces' histograms, each from its own maximum's bin down
   if (tid < lay.pieces) {
-    const bool some = head.top > -INFINITY;
+    const bool some = head.top > -INFINITY && !bins.far;
     s.shift[tid] = some ? index_of(head.top) : BINS;
     s.used[tid] = some ? (int)head.used : 0;
   }
@@ -617,56 +654,29 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
     const bool in = tid == 0 || s.count[tid] > s.count[tid - 1];
     return first_of(s, in && crossed(mode, value, s.count[tid], s.mass[tid]), in);
   };
-  const uint32_t binned = uni(s.count[BINS - 1]), K = row.k > 0 ? min((uint32_t)row.k, live) : live;
-  const bool cut_k = K < live && K <= binned;
-  // the smallest logit that min-p leaves, and its bin
-  float least = -INFINITY;
-  int bm = BINS;
-  if (row.least > 0.f) {
-    const double low = uni(log((double)row.least));
-    least = smallest((float)fmax((double)top + low * row.t, -(double)FLT_MAX), top, [&](float x) { return ((double)x - (double)top) * inv >= low; });
-    bm = uni(index_of(least));
-  }
+  const uint32_t K = row.k > 0 ? min((uint32_t)row.k, live) : live;
+  const bool masses = row.masses || bins.far;  // (whether the histogram has them)
   const float uf = a.u[b];
   const double u = uf > 0.f ? (double)uf : 0.0;
 
-  // the last bin that matters
-  const int bk = cut_k ? bin_where(COUNT, (double)K) : BINS - 1;
-  int last = bk, bp = -1;
-  if (row.p == 1.f || (row.masses && !cut_k)) {  // (else top-p's sum is that of the list)
-    last = min(last, bm);
-    // (a little beyond the threshold, whose last bits are another sum's)
-    if (row.masses && row.p < 1.f) {
-      bp = bin_where(REACH, (double)row.p * uni(s.mass[BINS - 1]) * (1.0 + 0x1p-40));
-      last = min(last, bp);
-    }
-  }
-  const bool whole = uni(s.count[last]) <= (uint32_t)CAP;
-  int f0 = 0, f1 = last, f2 = 1, f3 = 0;  // bins for the list
-  bool fits = whole;
-  if (!whole && row.masses && !cut_k && row.least == 0.f) {
-    // top-p's bin and those that the draw may fall into, if they fit
-    const double most = uni(s.mass[BINS - 1]), part = row.p < 1.f ? (double)row.p * most * (1.0 - 0x1p-40) : most;
-    f0 = bin_where(EXCEED, u * part);
-    f1 = row.p < 1.f ? bin_where(EXCEED, u * uni(s.mass[bp])) : f0;
-    if (bp > f1) f2 = f3 = bp;
-    const uint32_t total = s.count[f1] - (f0 ? s.count[f0 - 1] : 0) + (bp > f1 ? s.count[bp] - s.count[bp - 1] : 0);
-    fits = uni(total) <= (uint32_t)CAP;
-  }
-
   // Top-k, top-p, min-p, the draw, and (where rounding has put it behind the cut) the last token before the cut, as
   // one sequence of passes over tokens.
-  enum { LIST, MASSES, NEXT, FIND, LEAST };
+  enum { FILL, PLAN, LIST, MASSES, NEXT, FIND, LEAST };
   Pass p{};
   p.top = top;
-  p.tb = tb;
-  p.inv = inv;
+  p.bins = bins;
   p.z = (const char*)a.z + (size_t)b * a.stride * (BF16 ? 2 : 4);
   p.chunk_top = (const float*)(ws + lay.max_at);
   p.V = a.V;
   p.chunks = lay.chunks;
-  int state = fits ? LIST : row.masses ? NEXT : MASSES, step = -1;
-  bool in_list = fits;              // bins f0 .. f1 and f2 .. f3 are in it
+  int state = bins.far ? FILL : PLAN, step = -1;
+  uint32_t binned = 0;
+  bool cut_k = false, whole = false;
+  float least = -INFINITY;          // the smallest logit that min-p leaves, and its bin
+  int bm = BINS;
+  int bk = BINS - 1, last = 0;      // bins of top-k's cut, and the last one that matters
+  int f0 = 0, f1 = 0, f2 = 1, f3 = 0;
+  bool in_list = false;             // bins f0 .. f1 and f2 .. f3 are in the list
   Sum cut{K, 0.0};
   uint32_t at_count = 0;            // of the draw's token: the count up to it, its logit, its id
   float at_z = top;
@@ -679,6 +689,42 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
   bool listed = false, fresh = false;
 #pragma unroll 1
   for (;;) {
+    if (state == PLAN) {
+      binned = uni(s.count[BINS - 1]);
+      cut_k = K < live && K <= binned;
+      if (row.least > 0.f) {
+        const double low = uni(log((double)row.least));
+        least = smallest((float)fmax((double)top + low * row.t, -(double)FLT_MAX), top, [&](float x) { return ((double)x - (double)top) * inv >= low; });
+        bm = uni(index_of(least));
+      }
+      // the last bin that matters
+      if (cut_k) bk = bin_where(COUNT, (double)K);
+      last = bk;
+      int bp = -1;
+      if (row.p == 1.f || (masses && !cut_k)) {  // (else top-p's sum is that of the list)
+        last = min(last, bm);
+        // (a little beyond the threshold, whose last bits are another sum's)
+        if (masses && row.p < 1.f) {
+          bp = bin_where(REACH, (double)row.p * uni(s.mass[BINS - 1]) * (1.0 + 0x1p-40));
+          last = min(last, bp);
+        }
+      }
+      whole = uni(s.count[last]) <= (uint32_t)CAP;
+      f0 = 0;
+      f1 = last;
+      in_list = whole;
+      if (!whole && masses && !cut_k && row.least == 0.f) {
+        // top-p's bin and those that the draw may fall into, if they fit
+        const double most = uni(s.mass[BINS - 1]), part = row.p < 1.f ? (double)row.p * most * (1.0 - 0x1p-40) : most;
+        f0 = bin_where(EXCEED, u * part);
+        f1 = row.p < 1.f ? bin_where(EXCEED, u * uni(s.mass[bp])) : f0;
+        if (bp > f1) f2 = f3 = bp;
+        const uint32_t total = s.count[f1] - (f0 ? s.count[f0 - 1] : 0) + (bp > f1 ? s.count[bp] - s.count[bp - 1] : 0);
+        in_list = uni(total) <= (uint32_t)CAP;
+      }
+      state = in_list ? LIST : masses ? NEXT : MASSES;
+      if (state == NEXT) continue;
+    }
     if (state == NEXT) {
       if (++step == 0) cut.mass = uni(s.mass[BINS - 1]);
       if (step == 5) break;
@@ -717,9 +763,12 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
       b1 = last;
     } else if (state == LEAST) {
       b0 = b1 = bm;  // (BINS: tokens without a mass)
+    } else if (state == FILL) {
+      b0 = 0;
+      b1 = BINS;
     }
     p.append = state == LIST;
-    p.by_bin = state == MASSES || state == LEAST;
+    p.by_bin = state == MASSES || state == LEAST || state == FILL;
     p.listed = state == MASSES ? whole : state == LEAST ? in_list && f0 == 0 && bm <= f1 : false;
     p.lo = 0;
     p.hi = ~0ull;
@@ -748,8 +797,11 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
     }
     if (state != FIND || !listed || n > 64) go_over<BF16>(s, p);
 
-    if (state == LIST) {
-      state = row.masses ? NEXT : MASSES;
+    if (state == FILL) {
+      scan_bins(s, s.sub_count[tid], (double)s.sub_mass[tid] * unit);
+      state = PLAN;
+    } else if (state == LIST) {
+      state = masses ? NEXT : MASSES;
     } else if (state == MASSES) {  // counted only until now
       const uint32_t c = s.count[tid] - (tid ? s.count[tid - 1] : 0);
       scan_bins(s, c, (double)s.sub_mass[tid] * unit);
@@ -808,7 +860,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
       if (wave == 0) {
         // a token's rank is the number of those ahead of it, and so are its sums
         const uint64_t q = lane < len ? s.few[lane] : ~0ull;
-        const uint64_t e = lane < len ? mass_in_bin(place_z(q), inv, bin_of(place_z(q), inv)) : 0;
+        const uint64_t e = lane < len ? units_in_bin(bins, place_z(q), i) : 0;
         uint32_t rank = 0;
         uint64_t m = m0 + e;
 #pragma unroll 1
@@ -840,7 +892,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
     }
   }
   // the mass at the centre of the first bin relative to the largest logit's
-  const double c = fabs(tb) < 0x1p52 ? -__builtin_fma((double)top, inv, -(tb + 0.5) * 0.125) : 0.0;
+  const double c = -place_in_bin(bins, top, 0);
   const double e = exp64(-fabs(c)), mine = exp64(((double)at_z - (double)top) * inv);
   answer(at_id, c < 0 ? mine / (cut.mass * e) : mine * e / cut.mass, cut.count);
 }
