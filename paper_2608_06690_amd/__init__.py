@@ -23,6 +23,7 @@ from ._native import (PMPE_BF16, PMPE_F32, PMPE_GATE_POOL_SOFTMAX, PMPE_GATE_REN
                       pmpe_expert_ffn_mx_workspace_bytes, PMPE_DEV_CACHE_RANGE, PMPE_DEV_CACHE_REFUSED, CacheDesc,
                       make_cache_desc, pmpe_kv_write, pmpe_kv_read, pmpe_attn_decode, pmpe_attn_decode_workspace_bytes,
                       pmpe_sample, pmpe_sample_workspace_bytes)
+from .cache import PagedCache, Sampler  # noqa: F401
 from .layer import (AuditBuffers, BlockBuffers, GradBuffers, LayerBuffers, NormedMoE, PolicyMaskedMoE,  # noqa: F401
                     PrivateAdamW, step_clipped)
 from .policy import policy_word, request_offsets, resolve_policy, token_policy_words  # noqa: F401
