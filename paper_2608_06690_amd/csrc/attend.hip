@@ -55,9 +55,9 @@ __device__ __forceinline__ float rows_sum(float v) {
   s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
-// 2^(e - 127) of a biased exponent; 255 is NaN
-__device__ __forceinline__ float pow2_of(uint32_t e) { return __uint_as_float(e == 255 ? 0x7FC00000u : e ? e << 23 : 0x400000u); }
-// Two e4m3 values (the word's lower or upper half) times a power of two, to bf16: exact.
+// Two e4m3 values (the word's lower or upper half) times a power of two, to bf16: exact. The instruction takes the
+// exponent field of its scale as the biased exponent, 255 being NaN.
+__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
 template <bool HI>
 __device__ __forceinline__ uint32_t fp8_to_bf16x2(uint32_t q, float s) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q, s, HI));
@@ -286,7 +286,7 @@ struct Wave {
     } else if constexpr (T == FP8) {
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        const float f = pow2_of(t.ks[u][j / 2]);
+        const float f = scale_of(t.ks[u][j / 2]);
         const uint32_t x = t.k[u][j / 2][(j & 1) * 2], y = t.k[u][j / 2][(j & 1) * 2 + 1];
         const u32x4 k = {fp8_to_bf16x2<false>(x, f), fp8_to_bf16x2<true>(x, f), fp8_to_bf16x2<false>(y, f), fp8_to_bf16x2<true>(y, f)};
         s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(k), as_bf16x8(q[j]), s, 0, 0, 0);
@@ -341,7 +341,7 @@ struct Wave {
         float f[8];
         if constexpr (T == FP8) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] = pow2_of((t.vs[j >> 2][sg] >> (8 * (j & 3))) & 0xFFu);
+          for (int j = 0; j < 8; ++j) f[j] = scale_of((t.vs[j >> 2][sg] >> (8 * (j & 3))) & 0xFFu);
         }
 #pragma unroll
         for (int e = 0; e < pairs; ++e) {

@@ -255,3 +255,26 @@ def test_two_streams_with_workspaces_of_their_own():
             P.pmpe_attn_decode(c.desc, q, None, ln, *dev[0], *dev[1], 0.09, o, None, None, w, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, outs))
+
+
+@pytest.mark.parametrize("heads", [2, 18, 24])
+def test_scales_at_their_ends(heads):
+    log(f"scales at their ends {heads}")
+    # one row: the output is that row, whatever its scales; NaN scales show in their block of 32 only
+    ends = [1, 2, 60, 127, 200, 245, 246, 255]
+    c = Cache([1], 2, 256, 16, BF16, True, tags=False)
+    p = int(c.table[0, 0])
+    c.vs[p, 0, :, 0] = torch.tensor(ends, dtype=torch.uint8)
+    c.vs[p, 1, :, 0] = 127
+    out, _, _ = call(c, randn((1, heads, 256), 5, 0.01, BF16).cuda(), None, [1], 0.01)
+    want = c.rows("v", 0, 0, 1)[0].repeat_interleave(heads // 2, dim=0).to(BF16)
+    got = out[0].cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want))
+    small = want.double().abs() < 2.0 ** -120
+    assert torch.equal(torch.nan_to_num(got)[~small], torch.nan_to_num(want)[~small])
+    assert bool(((got.double() - want.double()).abs()[small] <= 2.0 ** -126).all())
+    # a key of NaN spoils the heads that read it
+    c.ks[p, 1, 3, 0] = 255
+    out, lse, _ = call(c, randn((1, heads, 256), 5, 0.01, BF16).cuda(), None, [1], 0.01)
+    assert bool(torch.isnan(out[0, heads // 2:]).all()) and bool(torch.isnan(lse[0, heads // 2:]).all())
+    assert bool(torch.isfinite(lse[0, :heads // 2]).all())
