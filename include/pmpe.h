@@ -875,7 +875,8 @@ pmpe_status pmpe_expert_ffn_mx(const pmpe_layer_desc* d, int32_t T, const uint8_
  *   policy_word       [R] uint32 or NULL (every request denies); read with page_tag only
  *   dev_status        optional: PMPE_DEV_CACHE_REFUSED, PMPE_DEV_CACHE_RANGE
  *
- * A row that a request may not use takes no part: not written, not attended to, read back as zeros. Two
+ * A row that a request may not use takes no part: not written, not attended to, read back as zeros (the kernels
+ * may load page 0 in its place and drop the values, so page 0 is always memory that can be read). Two
  * requests may read one page; a page that a call writes belongs to one request of the batch.
  */
 typedef struct {
@@ -933,8 +934,8 @@ pmpe_status pmpe_kv_read(const pmpe_cache_desc* c, int32_t T, int32_t R, void* k
  *   seq_first    [R] int32 or NULL (0): positions before it are out of the window
  *   seq_len      [R] int32: rows of the request, the new token's among them (0 or less: none)
  *   lse          [R, n_heads] fp32 out or NULL
- *   ws           pmpe_attn_decode_workspace_bytes(c, R, n_heads) bytes, 16-byte aligned; the size does not
- *                depend on lengths. Two calls equal in all inputs have equal bits
+ *   ws           pmpe_attn_decode_workspace_bytes(c, R, n_heads) bytes, 16-byte aligned; the size depends on
+ *                the table's width and the heads, not on lengths. Two calls equal in all inputs have equal bits
  * Errors: as pmpe_kv_write, and PMPE_ERR_WORKSPACE.
  */
 size_t pmpe_attn_decode_workspace_bytes(const pmpe_cache_desc* c, int32_t R, int32_t n_heads);
@@ -958,8 +959,8 @@ pmpe_status pmpe_attn_decode(const pmpe_cache_desc* c, int32_t R, int32_t n_head
  *   min_p        of these the ones with m >= min_p, at least one (0 or less, or NaN: no cut)
  *   token        the first whose cumulated mass exceeds u times the sum of those left
  * A temperature of 0 (or less, or NaN) takes the first token of the order. Masses and their sums are 64-bit,
- * a mass resolved to 2^-44 of its neighbourhood's: the choice is that of 64-bit arithmetic but where a sum
- * comes as near to its threshold as that. A logit of -inf (or NaN) masks its token; +inf counts as the largest
+ * a mass right to 2^-43 of itself: the choice is that of 64-bit arithmetic but where a sum comes as near to its
+ * threshold as that. A logit of -inf (or NaN) masks its token; +inf counts as the largest
  * finite value. A row without any token left has token -1, prob 0 and kept 0.
  *
  *   logits       [B, V] of logits_dtype (PMPE_F32 or PMPE_BF16), rows `stride` elements apart; V 1..PMPE_MAX_VOCAB

@@ -13,6 +13,13 @@
 // Where requests are long, a head's tiles are cut into equal parts of a length that all requests share, found from
 // their lengths by every block: PARTS parts in all, and one more at most for each head. A second kernel joins the
 // parts in order. No atomics: equal calls have equal bits.
+//
+// Bound by HBM, and by the pattern in which it is read: 256 requests of up to 4096 rows over 4 kv heads of 128 in 8 bits
+// (1.1 GB) take 213 us, 5.0 TB/s, and as long with all products left out; 64 of 8000 rows in bf16 324 us, 6.4 TB/s. A K
+// operand of 8-bit rows is 64 bytes at a time, half a line, and scales are lines of their own; plain reads of whole
+// lines reach 6.6 to 7.1 TB/s, of half lines 5.7 to 6.0. Single requests are bound by latency: 700 rows 10.5 us,
+// 131,000 rows 43 us in 1,536 parts and 11 us to join them. Loads are never under a branch (a row that may not
+// be used is read from page 0 and dropped): with branches each step waited for all loads of the one before it.
 #include <algorithm>
 
 #include "kvcache.h"

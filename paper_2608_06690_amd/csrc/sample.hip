@@ -9,11 +9,16 @@
 // of them from the maximum down: what lies lower has less than e^-63 of its mass) of counts and masses. The second
 // has a block per row: it adds up the histograms, finds the bins of the thresholds, and collects the tokens of the
 // bins that matter from the chunks that hold one, in LDS. A threshold's token is then found by histograms of the
-// order's bits inside its bin (9 bits a round) until 64 tokens are left, which one wave sorts. Bins with more tokens
+// order's bits inside its bin (9 bits a round) until 64 tokens are left, which one wave ranks. Bins with more tokens
 // than the list holds (ties, flat rows) have their first rounds over the logits themselves.
 //
-// Masses are exact integers inside a bin (units of 2^-44 of the mass at its centre), so their sums do not depend on
-// the order of the atomics; across bins they are fp64 in a fixed order.
+// Both are bound by issue and latency, not by memory: 256 rows of 131,072 bf16 logits (67 MB, 13 us at a large
+// copy's rate) take 36 us in the first kernel, whose bins and masses are about 20 vector operations a logit, and 94 to
+// 114 us in the second, whose time is its longest row's: a CU goes over a row alone, about 2 us for 8192
+// logits, once more for every threshold whose bins the list did not hold. One row of 131,071: 5 + 70 us at most.
+//
+// Masses are integers inside a bin (units of 2^-44 of the mass at its centre, right to 2^-43), so their sums do not
+// depend on the order of the atomics; across bins they are fp64 in a fixed order.
 #include <cfloat>
 
 #include "exp64.h"
