@@ -84,6 +84,8 @@ class PagedCache:
         """Request r, open and empty, begins with the rows of the whole pages among the first `rows` of `source`. tag:
         the cache tag that these rows were made under (default: the source's). Returns the number of rows it has then;
         raises PmpeError where the tags differ."""
+        if rows < 0:
+            raise ValueError(f"{rows} rows cannot be shared")
         if self.lengths[r] or r == source:
             raise ValueError(f"request {r} must be empty and another than its source")
         if not N.pmpe_cache_tag_check(self.tag(source) if tag is None else tag, self.tag(r)):

@@ -97,3 +97,27 @@ def test_closed_requests_have_no_tag_and_digests_have_32_bytes():
         c.tag(0)
     with pytest.raises(ValueError):
         cache(model_revision=b"x")
+
+
+@pytest.mark.parametrize("rows", [-1, -16, -17])
+def test_sharing_a_negative_number_of_rows_is_refused(rows):
+    c = cache()
+    for r in range(2):
+        c.open(r, None)
+    grow(c, [40, 0, 0])
+    users = list(c._users)
+    with pytest.raises(ValueError):
+        c.share(1, 0, rows)
+    assert c._users == users and c._pages[1] == [] and c.lengths == [40, 0, 0]
+
+
+def test_shared_pages_come_back_once():
+    c = cache()
+    for r in range(2):
+        c.open(r, None)
+    grow(c, [40, 0, 0])
+    assert c.share(1, 0, 40) == 32
+    c.close(0)
+    assert len(c._free) == 6 and all(int(c.page_tag[p]) == 0 for p in c._pages[1])
+    c.close(1)
+    assert sorted(c._free) == list(range(8)) and c.page_tag.tolist() == [-1] * 8
