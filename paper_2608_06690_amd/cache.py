@@ -68,17 +68,22 @@ class PagedCache:
 
     def close(self, r: int) -> None:
         """Request r gives its pages back; those that no other request has belong to no decision then."""
+        self._give_back(r, 0)
+        self.lengths[r], self.decision[r] = 0, None
+        self.words[r] = 0
+        self.seq_len[r] = 0
+
+    def _give_back(self, r: int, keep: int) -> None:
+        """The pages of request r but the first `keep`."""
         free = []
-        for p in self._pages[r]:
+        for p in self._pages[r][keep:]:
             self._users[p] -= 1
             if self._users[p] == 0:
                 free.append(p)
         if free:
             self._free.extend(reversed(free))
             self.page_tag[torch.tensor(free, device=self.page_tag.device)] = _FREE
-        self._pages[r], self.lengths[r], self.decision[r] = [], 0, None
-        self.words[r] = 0
-        self.seq_len[r] = 0
+        del self._pages[r][keep:]
 
     def share(self, r: int, source: int, rows: int, tag: Optional[N.CacheTag] = None) -> int:
         """Request r, open and empty, begins with the rows of the whole pages among the first `rows` of `source`. tag:
@@ -142,16 +147,22 @@ class PagedCache:
             if t.shape != (k.shape[0], self.desc.n_kv_heads, self.desc.head_dim) or t.dtype != act or t.device != self.k.device:
                 raise ValueError(f"k and v must be {[k.shape[0], self.desc.n_kv_heads, self.desc.head_dim]} of {act} on {self.k.device}")
         with torch.cuda.stream(stream):
-            self._reserve(counts)
             if req_offset is None:
                 req_offset = request_offsets(counts, self.seq_len.device)
-            if all(n == counts[0] for n in counts):
-                self.seq_len.add_(counts[0])
-            else:
-                self.seq_len.add_(req_offset[1:] - req_offset[:-1])
+            elif req_offset.shape != (self.requests + 1,) or req_offset.dtype != torch.int32 or req_offset.device != self.k.device:
+                raise ValueError(f"req_offset must be [{self.requests + 1}] of torch.int32 on {self.k.device}")
+            self._reserve(counts)
+            more = counts[0] if all(n == counts[0] for n in counts) else req_offset[1:] - req_offset[:-1]
+            self.seq_len.add_(more)
+            try:
+                N.pmpe_kv_write(self.desc, k, v, req_offset, self.seq_len, self.block_table, self.page_tag, self.words, self.k,
+                                self.v, self.k_scale, self.v_scale, self.dev_status)
+            except Exception:  # nothing was written: a length ahead of the rows would show what the pages held before
+                self.seq_len.sub_(more)
+                for r, n in enumerate(self.lengths):
+                    self._give_back(r, -(-n // self.desc.page_size))
+                raise
             self.lengths = [a + b for a, b in zip(self.lengths, counts)]
-            N.pmpe_kv_write(self.desc, k, v, req_offset, self.seq_len, self.block_table, self.page_tag, self.words, self.k,
-                            self.v, self.k_scale, self.v_scale, self.dev_status)
             if stream is not None:
                 req_offset.record_stream(stream)
 

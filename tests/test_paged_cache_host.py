@@ -99,6 +99,39 @@ def test_closed_requests_have_no_tag_and_digests_have_32_bytes():
         cache(model_revision=b"x")
 
 
+def test_a_refused_write_leaves_the_books_as_they_were(monkeypatch):
+    # (the pages' memory may hold another decision's rows: a length without a write would show them)
+    def refuse(*args):
+        raise P.PmpeError(-5, "pmpe_kv_write")
+
+    monkeypatch.setattr("paper_2608_06690_amd._native.pmpe_kv_write", refuse)
+    for counts in ([3, 3, 3], [17, 0, 1]):
+        c = cache()
+        for r in range(3):
+            c.open(r, None)
+        grow(c, [4, 0, 0])
+        c.seq_len[0] = 4
+        mine = [list(p) for p in c._pages]
+        k = torch.zeros(sum(counts), 2, 64, dtype=torch.bfloat16)
+        with pytest.raises(P.PmpeError):
+            c.write(k, k, counts)
+        assert c.lengths == [4, 0, 0] and c.seq_len.tolist() == [4, 0, 0]
+        assert c._pages == mine and len(c._free) == 7
+        assert all(int(c.page_tag[p]) == -1 for p in c._free)
+        assert sorted(c._free + mine[0]) == list(range(8))
+
+
+def test_offsets_that_do_not_fit_the_counts_are_refused():
+    c = cache()
+    for r in range(3):
+        c.open(r, None)
+    k = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
+    for offset in (torch.zeros(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int64), torch.zeros(4, 1, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            c.write(k, k, [1, 1, 2], offset)
+        assert c.lengths == [0, 0, 0] and c.seq_len.tolist() == [0, 0, 0] and len(c._free) == 8
+
+
 @pytest.mark.parametrize("rows", [-1, -16, -17])
 def test_sharing_a_negative_number_of_rows_is_refused(rows):
     c = cache()
