@@ -169,13 +169,15 @@ class PagedCache:
     def attend(self, q: torch.Tensor, scale: float, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                first: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Attention of each request's newest row: q [requests, n_heads, head_dim]; first [requests] int32: positions
-        before it are out of the window. A request without rows has zeros."""
+        before it are out of the window. A request without rows has zeros. The workspace is the object's: its calls,
+        and graphs that hold one, follow one another."""
         heads = q.shape[1]
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if heads not in self._ws:  # (kept: a captured step may hold it)
-            self._ws[heads] = torch.empty(max(16, N.pmpe_attn_decode_workspace_bytes(self.desc, self.requests, heads)),
-                                          dtype=torch.uint8, device=q.device)
+        with torch.cuda.stream(stream):  # (new memory belongs to the stream that writes it)
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            if heads not in self._ws:  # (kept: a captured step may hold it)
+                self._ws[heads] = torch.empty(max(16, N.pmpe_attn_decode_workspace_bytes(self.desc, self.requests, heads)),
+                                              dtype=torch.uint8, device=q.device)
         N.pmpe_attn_decode(self.desc, q, first, self.seq_len, self.block_table, self.page_tag, self.words, self.k, self.v,
                            self.k_scale, self.v_scale, scale, out, lse, self.dev_status, self._ws[heads], stream)
         return out
@@ -196,7 +198,8 @@ class PagedCache:
 
 
 class Sampler:
-    """Draws a token per row of logits with parameters of each row (pmpe_sample); its buffers hold the last draw.
+    """Draws a token per row of logits with parameters of each row (pmpe_sample); its buffers hold the last draw, so
+    its calls, and graphs that hold one, follow one another.
     Parameters [rows]: temperature, top_p and min_p fp32, top_k int32, each may be None."""
 
     def __init__(self, rows: int, vocab: int, temperature=None, top_k=None, top_p=None, min_p=None, device="cuda"):

@@ -150,6 +150,32 @@ def test_a_step_on_another_stream():
     assert torch.equal(*outs)
 
 
+def test_new_output_belongs_to_the_stream_that_writes_it(monkeypatch):
+    # (memory of another stream may be given away while the call still writes it)
+    log("output on another stream")
+    s = torch.cuda.Stream()
+    cache = P.PagedCache(2, 16, 16, KV, DIM, 4, REV, FP)
+    for r in range(2):
+        cache.open(r, None)
+    k, v = (randn((30, KV, DIM), i, 1.0, torch.bfloat16).cuda() for i in (1, 2))
+    q = randn((2, HEADS, DIM), 3, 1.0, torch.bfloat16).cuda()
+    cache.write(k, v, [12, 18])
+    want = cache.attend(q, 0.125)
+    torch.cuda.synchronize()
+    made, empty = [], torch.empty
+
+    def spy(*args, **kw):
+        made.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*args, **kw)
+
+    cache._ws.clear()
+    monkeypatch.setattr(torch, "empty", spy)
+    got = cache.attend(q, 0.125, stream=s)
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert made == [s.cuda_stream] * 2 and torch.equal(got, want)
+
+
 def test_captured_step():
     log("captured step")
     R = 3
