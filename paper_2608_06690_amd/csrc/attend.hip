@@ -323,15 +323,22 @@ struct Wave {
         w += per;
       }
     } else {
-      // A weight as the sum of two bf16 values: one alone is off by 2^-9, more than the sums and the output's rounding
-      // leave where many rows cancel. With up to 8 heads the lower parts are columns 8 .. 15 of the same product.
-      u32x4 hi, lo;
-      float x[8];
+      // A weight as the sum of three bf16 values, which leaves 2^-27 of it (two leave 2^-18, and four times as many
+      // outputs rounded to the other side as fp32 weights do). With up to 8 heads the second parts are columns 8 .. 15 of
+      // the first parts' product.
+      u32x4 hi, lo, rest;
+      float x[8], y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = p[j] - (float)(__bf16)p[j];
+      for (int j = 0; j < 8; ++j) {
+        x[j] = p[j] - (float)(__bf16)p[j];
+        y[j] = x[j] - (float)(__bf16)x[j];
+      }
       if constexpr (SPLIT_ROWS) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = i < 8 ? p[j] : x[j];
+        for (int j = 0; j < 8; ++j) {
+          x[j] = i < 8 ? p[j] : x[j];
+          y[j] = i < 8 ? y[j] : 0.f;
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) hi[j] = pk_bf16(x[2 * j], x[2 * j + 1]);
       } else {
@@ -341,6 +348,8 @@ struct Wave {
           lo[j] = pk_bf16(x[2 * j], x[2 * j + 1]);
         }
       }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) rest[j] = pk_bf16(y[2 * j], y[2 * j + 1]);
       int w = 0, n = 0;
 #pragma unroll
       for (int sg = 0; sg < TileT::SEGS; ++sg) {
@@ -365,6 +374,7 @@ struct Wave {
             for (int j = 0; j < 4; ++j) vt[j] = __builtin_amdgcn_perm(v[2 * j + 1], v[2 * j], odd ? 0x07060302u : 0x05040100u);
             o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt), as_bf16x8(hi), o[n], 0, 0, 0);
             if constexpr (!SPLIT_ROWS) o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt), as_bf16x8(lo), o[n], 0, 0, 0);
+            o[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(vt), as_bf16x8(rest), o[n], 0, 0, 0);
           }
         }
         w += T == BF16 ? pairs : (pairs + 1) / 2;
