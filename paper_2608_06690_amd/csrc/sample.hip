@@ -152,18 +152,21 @@ __device__ __forceinline__ Row row_of(const SampleArgs& a, int b) {
 
 // The bins of a row: floor(fl(z 8 / T)) in fp32, counted down from that of the row's (or a piece's) largest logit. What
 // counts is that this never falls with z; a logit may lie beyond its bin's edges by 2^-23 of 8 z / T, and its mass is that
-// of its exact place. Where 8 z / T is 2^20 or more at the top (temperatures next to 0, say), fp64 makes the bins.
+// of its exact place. Where 8 z / T is FAR or more at the row's top (temperatures next to 0, say), fp64 makes the bins. A
+// piece whose top is among the row's bins may lie BINS below it: its own limit is so much larger that it has its histogram
+// in every row that needs it.
+constexpr float FAR = 0x1p20f, FAR_PIECE = FAR + 2 * BINS;
 struct Bins {
   double inv;   // 1 / T
   float inv8;   // 8 / T
   bool far;
   double top;   // the first bin (a whole number)
 };
-__device__ __forceinline__ Bins bins_of(const Row& r, float top) {
+__device__ __forceinline__ Bins bins_of(const Row& r, float top, float limit) {
   Bins b;
   b.inv = r.inv;
   b.inv8 = (float)(8.0 * r.inv);
-  b.far = !(fabsf(top * b.inv8) < 0x1p20f);
+  b.far = !(fabsf(top * b.inv8) < limit);
   b.top = b.far ? floor((double)top * r.inv * 8.0) : (double)floorf(top * b.inv8);
   return b;
 }
@@ -259,9 +262,9 @@ __global__ __launch_bounds__(HIST_THREADS) void sample_hist_kernel(SampleArgs a,
     if (tid == 0) *head = Head{top, s_first, top == -INFINITY ? 0u : 1u, 0u};
     return;
   }
-  const Bins bins = bins_of(row, top);
+  const Bins bins = bins_of(row, top, FAR_PIECE);
   uint32_t rest = 0;
-  if (bins.far) {  // the second kernel does without this histogram
+  if (bins.far) {  // too far from its row's top for the histogram, or all of the row is
 #pragma unroll
     for (int g = 0; g < G8; ++g)
 #pragma unroll
@@ -620,7 +623,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
     return;
   }
   const double inv = row.inv;
-  Bins bins = bins_of(row, top);
+  Bins bins = bins_of(row, top, FAR);
   bins.inv8 = uni(bins.inv8);
   bins.top = uni(bins.top);
   bins.far = uni((int)bins.far) != 0;
