@@ -559,7 +559,11 @@ __device__ __forceinline__ float smallest(float near, float top, F ok) {
     const uint32_t step = ((b - a) >> 6) + 1;
     k = b - a < step * lane_id() ? b : a + step * lane_id();
     yes = __ballot(ok(z_of(k)) || k == b);
-    const int f = yes ? __builtin_ctzll(yes) : 63;
+    if (yes == 0) {  // (64 steps of the rounded width may end ahead of b)
+      a = (uint32_t)__builtin_amdgcn_readlane((int)k, 63) + 1;
+      continue;
+    }
+    const int f = __builtin_ctzll(yes);
     const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)k, f);
     if (f == 0) {
       b = a;

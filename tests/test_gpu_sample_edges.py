@@ -28,3 +28,34 @@ def test_largest_logits_next_to_the_border_of_fp32_bins(V, t):
     for par in ({}, dict(top_k=[V // 3] * B), dict(top_p=[0.9] * B), dict(min_p=[0.02] * B), dict(top_k=[50] * B),
                 dict(top_k=[V - 5] * B, top_p=[0.97] * B, min_p=[0.001] * B)):
         check(z, dict(par, temperature=[t] * B), u)
+
+
+# (largest logit, temperature, min_p) with top + T ln(min_p) between -1e-10 and 0, 5e-11 of the two terms or less
+CANCEL = [(1.2379502058029175, 2.248124122619629, 0.5765696167945862), (1.7185120582580566, 1.4391342401504517, 0.30296769738197327),
+          (2.1257972717285156, 0.9267536997795105, 0.10088133066892624), (2.1620967388153076, 1.1297087669372559, 0.14751090109348297)]
+
+
+def test_least_mass_next_to_a_logit_of_zero():
+    """The smallest logit that min-p leaves lies many numbers of fp32 below where the logarithm puts it."""
+    log("least mass at a logit of zero")
+    z = torch.full((len(CANCEL), 300), -1.0)
+    z[:, 5] = torch.tensor([c[0] for c in CANCEL])
+    z[:, 7:107] = -torch.linspace(1.3e-10, 5.5e-10, 100)  # below the least mass by 2^-33 to 2^-30 of it
+    z[:, 200] = 0.0
+    par = dict(temperature=[c[1] for c in CANCEL], min_p=[c[2] for c in CANCEL])
+    _, _, kept = check(z, par, [0.1, 0.99, 0.5, 0.9])
+    assert kept.tolist() == [2] * 4
+
+
+@pytest.mark.parametrize("t", [100793200.0, 105422080.0, 118912304.0, 1e8, 1e30])
+def test_bins_that_meet_at_zero(t):
+    """8 z / T of logits next to 0 is 0 in fp32: a bin's edge lies many numbers below it."""
+    log(f"bins that meet at zero t {t}")
+    B, V = 8, 9000
+    z = torch.empty(B, V)
+    z[:, :100] = torch.rand(B, 100, generator=gen(1))
+    z[:, 100:8000] = -torch.logspace(-39, -37, 7900)
+    z[:, 8000:] = -1.0 - torch.rand(B, 1000, generator=gen(2))
+    u = [0.0, 0.01, 0.02, 0.3, 0.5, 0.8, 0.95, 1.0 - 2.0 ** -24]
+    for par in ({}, dict(top_k=[6000] * B), dict(top_p=[0.6] * B), dict(top_k=[60] * B), dict(min_p=[0.9999999] * B)):
+        check(z, dict(par, temperature=[t] * B), u)
