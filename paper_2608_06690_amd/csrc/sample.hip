@@ -694,7 +694,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
   uint32_t at_count = 0;            // of the draw's token: the count up to it, its logit, its id
   float at_z = top;
   int at_id = -1;
-  // the search of FIND: bin i, tokens and units of it ahead of places lo .. hi, tokens in them
+  // the search of FIND: bin i (BINS: what lies below them), tokens and units of it ahead of places lo .. hi, tokens in them
   int i = 0, mode = COUNT;
   double value = 0.0, mass0 = 0.0, scale = 0.0;
   uint32_t count0 = 0, n0 = 0, n = 0;
@@ -741,8 +741,9 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
     if (state == NEXT) {
       if (++step == 0) cut.mass = uni(s.mass[BINS - 1]);
       if (step == 5) break;
-      mode = step == 1 ? REACH : step == 3 ? EXCEED : COUNT;
-      value = step == 0 ? (double)K : step == 1 ? (double)row.p * cut.mass : step == 3 ? u * cut.mass : (double)cut.count;
+      // (u of 1 or more: the last token before the cut, which may lie below the bins)
+      mode = step == 1 ? REACH : step == 3 && u < 1.0 ? EXCEED : COUNT;
+      value = step == 0 ? (double)K : step == 1 ? (double)row.p * cut.mass : mode == EXCEED ? u * cut.mass : (double)cut.count;
       if (step == 0 && !cut_k) continue;
       if (step == 0 && uni(s.count[bk]) == K) {
         cut.mass = uni(s.mass[bk]);
@@ -754,11 +755,11 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleArgs a, Layout la
         else continue;
       } else {
         if (step == 4 && at_count <= cut.count) break;
-        i = bin_where(mode, value);
+        i = mode == COUNT && value > (double)binned ? BINS : bin_where(mode, value);
         count0 = uni(i ? s.count[i - 1] : 0u);
         mass0 = uni(i ? s.mass[i - 1] : 0.0);
         scale = uni(exp64(-0.125 * i) * 0x1p-44);
-        n = uni(s.count[i]) - count0;
+        n = (i < BINS ? uni(s.count[i]) : live) - count0;
         n0 = 0;
         m0 = 0;
         listed = in_list && ((i >= f0 && i <= f1) || (i >= f2 && i <= f3));

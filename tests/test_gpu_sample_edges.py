@@ -59,3 +59,19 @@ def test_bins_that_meet_at_zero(t):
     u = [0.0, 0.01, 0.02, 0.3, 0.5, 0.8, 0.95, 1.0 - 2.0 ** -24]
     for par in ({}, dict(top_k=[6000] * B), dict(top_p=[0.6] * B), dict(top_k=[60] * B), dict(min_p=[0.9999999] * B)):
         check(z, dict(par, temperature=[t] * B), u)
+
+
+@pytest.mark.parametrize("V", [300, 8193, 20011, 70001])
+def test_uniform_numbers_of_one_and_more_take_the_last_token(V):
+    """The last token before the cut, also where its mass is less than e^-64 of the largest's."""
+    log(f"u of one and more V {V}")
+    rows = [torch.linspace(-300, 300, V), torch.linspace(40, -60, V), torch.randn(V, generator=gen(1)),
+            torch.cat([torch.tensor([80.0]), torch.randn(V - 1, generator=gen(2))]), torch.randn(V, generator=gen(3)) * 100,
+            torch.randn(V, generator=gen(4)) * 3e37, torch.cat([torch.tensor([200.0]), torch.full((V - 1,), -1.0)]),
+            torch.where(torch.arange(V) % 3 == 0, float("-inf"), torch.linspace(0, -500, V))]
+    for u in (1.0, 2.0, float("inf"), 1.0 - 2.0 ** -24):
+        for dt in (torch.float32, torch.bfloat16):
+            z = torch.stack(rows).to(dt)
+            for par in ({}, dict(top_k=[V - 30] * 8), dict(min_p=[1e-35] * 8), dict(top_p=[0.9] * 8), dict(top_k=[5] * 8),
+                        dict(temperature=[0.3] * 8, top_k=[V // 2] * 8, min_p=[1e-38] * 8)):
+                check(z, par, [u] * 8)
