@@ -956,7 +956,8 @@ pmpe_status pmpe_attn_decode(const pmpe_cache_desc* c, int32_t R, int32_t n_head
  *   top_k        the first top_k (0 or less: no cut)
  *   top_p        of these the fewest whose masses reach top_p times the sum of all of them, at least one
  *                (1 or more, or NaN: no cut)
- *   min_p        of these the ones with m >= min_p, at least one (0 or less, or NaN: no cut)
+ *   min_p        of these the ones with m >= min_p, so the largest and its ties at least (0 or less, or NaN: no
+ *                cut; more than 1 counts as 1)
  *   token        the first whose cumulated mass exceeds u times the sum of those left
  * A temperature of 0 (or less, or NaN) takes the first token of the order. Masses and their sums are 64-bit,
  * a mass right to 2^-43 of itself: the choice is that of 64-bit arithmetic but where a sum comes as near to its

@@ -200,7 +200,7 @@ class PagedCache:
 class Sampler:
     """Draws a token per row of logits with parameters of each row (pmpe_sample); its buffers hold the last draw, so
     its calls, and graphs that hold one, follow one another.
-    Parameters [rows]: temperature, top_p and min_p fp32, top_k int32, each may be None."""
+    Parameters [rows]: temperature, top_p and min_p (more than 1 counts as 1) fp32, top_k int32, each may be None."""
 
     def __init__(self, rows: int, vocab: int, temperature=None, top_k=None, top_p=None, min_p=None, device="cuda"):
         self.temperature, self.top_k, self.top_p, self.min_p = temperature, top_k, top_p, min_p
