@@ -1,0 +1,45 @@
+"""PagedCache on the GPU: captured steps, their pages and lengths, and what they may not touch."""
+import pytest
+import torch
+
+import paper_2608_06690_amd as P
+from tests.decode_cases import log, randn
+
+pytestmark = pytest.mark.gpu
+REV, FP = bytes(32), bytes(range(32))
+KV, DIM, HEADS = 2, 64, 8
+BF16 = torch.bfloat16
+
+
+def rows(n, seed):
+    return randn((n, KV, DIM), seed, 1.0, BF16).cuda()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_replays_past_the_pages_leave_other_requests_alone(fp8):
+    log(f"replays past the pages fp8 {fp8}")
+    cache = P.PagedCache(3, 8, 16, KV, DIM, 4, REV, FP, fp8=fp8)
+    for r in range(3):
+        cache.open(r, None)             # of one decision: no tag keeps their pages apart
+    cache.write(rows(16, 1), rows(16, 2), [0, 16, 0])  # (page 0 is request 1's)
+    cache.write(rows(26, 7), rows(26, 8), [14, 0, 12])
+    cache.close(2)
+    cache.open(2, None)
+    cache.write(rows(20, 3), rows(20, 4), [0, 20, 0])  # (with the page that was request 2's)
+    k, v, off = rows(1, 5), rows(1, 6), torch.tensor([0, 1, 1, 1], dtype=torch.int32, device="cuda")
+    cache.write(k, v, [1, 0, 0], off)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cache.write(k, v, [1, 0, 0], off)
+    mine = int(cache.block_table[0, 0])
+    others = [p for p in range(8) if p != mine]
+    before = [x[others].clone() for x in (cache.k, cache.v, cache.k_scale, cache.v_scale) if x is not None]
+    g.replay()                          # row 15, the last of its page
+    torch.cuda.synchronize()
+    assert int(cache.dev_status) == 0 and int(cache.seq_len[0]) == 16
+    for _ in range(3):
+        g.replay()
+    torch.cuda.synchronize()
+    assert int(cache.dev_status) == P.PMPE_DEV_CACHE_RANGE
+    after = [x[others] for x in (cache.k, cache.v, cache.k_scale, cache.v_scale) if x is not None]
+    assert all(torch.equal(a, b) for a, b in zip(before, after))
