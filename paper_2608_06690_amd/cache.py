@@ -155,6 +155,7 @@ class PagedCache:
                 req_offset = request_offsets(counts, self.seq_len.device)
             elif req_offset.shape != (self.requests + 1,) or req_offset.dtype != torch.int32 or req_offset.device != self.k.device:
                 raise ValueError(f"req_offset must be [{self.requests + 1}] of torch.int32 on {self.k.device}")
+            had = [len(p) for p in self._pages]
             self._reserve(counts)
             more = counts[0] if all(n == counts[0] for n in counts) else req_offset[1:] - req_offset[:-1]
             self.seq_len.add_(more)
@@ -163,8 +164,8 @@ class PagedCache:
                                 self.v, self.k_scale, self.v_scale, self.dev_status)
             except Exception:  # nothing was written: a length ahead of the rows would show what the pages held before
                 self.seq_len.sub_(more)
-                for r, n in enumerate(self.lengths):
-                    self._give_back(r, -(-n // self.desc.page_size))
+                for r, n in enumerate(had):  # (no others: pages reserved ahead may hold rows of replays)
+                    self._give_back(r, n)
                 raise
             self.lengths = [a + b for a, b in zip(self.lengths, counts)]
             if stream is not None:
