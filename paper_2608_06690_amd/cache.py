@@ -125,18 +125,21 @@ class PagedCache:
             raise ValueError(f"{len(need)} pages are needed, {len(self._free)} are free")
         if not need:
             return
-        rows, cols, pages, tags = [], [], [], []
-        for r in need:
-            p = self._free.pop()
+        if self.k.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise ValueError("a captured write cannot take pages: they have to be reserved before")
+        rows, cols, pages, tags, n = [], [], [], [], [len(p) for p in self._pages]
+        for r, p in zip(need, reversed(self._free)):
             rows.append(r)
-            cols.append(len(self._pages[r]))
+            cols.append(n[r])
             pages.append(p)
             tags.append(_as_int32(N.PMPE_POLICY_ALLOW if self.decision[r] else N.PMPE_POLICY_DENY))
-            self._pages[r].append(p)
+            n[r] += 1
+        i = torch.tensor([rows, cols, pages, tags], dtype=torch.int64).to(self.page_tag.device)
+        self.block_table[i[0], i[1]] = i[2].int()
+        self.page_tag[i[2]] = i[3].int()
+        for r, p in zip(rows, pages):  # (the books last: where the device's part fails, they are as they were)
+            self._pages[r].append(self._free.pop())
             self._users[p] = 1
-        rows, cols, pages, tags = torch.tensor([rows, cols, pages, tags], dtype=torch.int64).to(self.page_tag.device)
-        self.block_table[rows, cols] = pages.int()
-        self.page_tag[pages] = tags.int()
 
     def write(self, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int], req_offset: Optional[torch.Tensor] = None,
               stream=None) -> None:

@@ -43,3 +43,23 @@ def test_replays_past_the_pages_leave_other_requests_alone(fp8):
     assert int(cache.dev_status) == P.PMPE_DEV_CACHE_RANGE
     after = [x[others] for x in (cache.k, cache.v, cache.k_scale, cache.v_scale) if x is not None]
     assert all(torch.equal(a, b) for a, b in zip(before, after))
+
+
+def test_a_captured_write_that_needs_pages_is_refused():
+    log("captured write without pages")
+    cache = P.PagedCache(2, 8, 16, KV, DIM, 4, REV, FP)
+    for r in range(2):
+        cache.open(r, None)
+    cache.write(rows(20, 1), rows(20, 2), [16, 4])
+    k, v, off = rows(2, 3), rows(2, 4), torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    books = [list(p) for p in cache._pages], list(cache._free), list(cache.lengths)
+    x, g = torch.zeros(4, device="cuda"), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        with pytest.raises(ValueError):
+            cache.write(k, v, [1, 1], off)
+        x.add_(1)                       # (the capture goes on)
+    assert books == (cache._pages, cache._free, cache.lengths) and cache.seq_len.tolist() == [16, 4]
+    g.replay()
+    cache.write(k, v, [1, 1], off)
+    got, _ = cache.read([17, 5])
+    assert torch.equal(got[16], k[0]) and torch.equal(got[21], k[1]) and x.tolist() == [1.0] * 4 and int(cache.dev_status) == 0

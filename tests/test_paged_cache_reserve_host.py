@@ -27,3 +27,32 @@ def test_a_refused_write_keeps_the_pages_that_were_there(monkeypatch):
             c.write(k, k, counts)
         assert c._pages == mine and sorted(c._free) == sorted(free) and c.block_table.tolist() == owned(c)
         assert c.lengths == [4, 0, 16] and all(int(c.page_tag[p]) == 0 for p in sum(mine, []))
+
+
+class Broken:
+    """A tensor that cannot be written (as in a capture that allows no copies)."""
+
+    def __init__(self, t):
+        self.t, self.device = t, t.device
+
+    def __setitem__(self, at, value):
+        raise RuntimeError("not now")
+
+
+@pytest.mark.parametrize("name", ["block_table", "page_tag"])
+def test_pages_that_the_device_does_not_learn_of_are_not_taken(name):
+    c = cache()
+    for r in range(3):
+        c.open(r, None)
+    grow(c, [20, 0, 1])
+    mine, free, users = [list(p) for p in c._pages], list(c._free), list(c._users)
+    whole = getattr(c, name)
+    setattr(c, name, Broken(whole))
+    k = torch.zeros(40, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(RuntimeError):
+        c.write(k, k, [20, 20, 0])
+    assert c._pages == mine and c._free == free and c._users == users and c.lengths == [20, 0, 1]
+    setattr(c, name, whole)
+    grow(c, [20, 20, 0])
+    assert [len(p) for p in c._pages] == [3, 2, 1] and c.block_table.tolist() == owned(c)
+    assert all(int(c.page_tag[p]) == 0 for p in sum(c._pages, []))
