@@ -95,8 +95,8 @@ class PagedCache:
         raises PmpeError where the tags differ."""
         if rows < 0:
             raise ValueError(f"{rows} rows cannot be shared")
-        if self.lengths[r] or r == source:
-            raise ValueError(f"request {r} must be empty and another than its source")
+        if self.lengths[r] or self._pages[r] or r == source:
+            raise ValueError(f"request {r} must be empty, without pages, and another than its source")
         if not N.pmpe_cache_tag_check(self.tag(source) if tag is None else tag, self.tag(r)):
             raise N.PmpeError(N.PMPE_ERR_TAG_MISMATCH, "pmpe_cache_tag_check")
         if self.decision[source] != self.decision[r]:  # (whatever tag was given: the pages are the source's)
@@ -110,6 +110,28 @@ class PagedCache:
         self._pages[r], self.lengths[r] = list(pages), n * self.desc.page_size
         self.seq_len[r] = self.lengths[r]
         return self.lengths[r]
+
+    def _counts(self, counts: Sequence[int]) -> List[int]:
+        counts = [int(n) for n in counts]
+        if len(counts) != self.requests:
+            raise ValueError(f"{self.requests} counts are needed, not {len(counts)}")
+        return counts
+
+    def reserve(self, counts: Sequence[int], stream=None) -> None:
+        """Pages for counts[r] rows of each request behind those that it has, or none at all (ValueError): a captured
+        write takes none itself, so its replays go as far as pages are reserved and are refused behind that."""
+        counts = self._counts(counts)
+        with torch.cuda.stream(stream):
+            self._reserve(counts)
+
+    def advance(self, counts: Sequence[int]) -> None:
+        """The rows that replays of captured writes have added to each request, which only the device has counted: after
+        them, and before the next call that needs the requests' lengths (write, read, share, reserve)."""
+        counts = self._counts(counts)
+        for r, n in enumerate(counts):
+            if n < 0 or self.lengths[r] + n > len(self._pages[r]) * self.desc.page_size:
+                raise ValueError(f"request {r} has no pages for {n} rows more than {self.lengths[r]}")
+        self.lengths = [a + b for a, b in zip(self.lengths, counts)]
 
     def _reserve(self, counts: Sequence[int]) -> None:
         """Pages for counts[r] more rows of each request, or none at all."""
@@ -145,10 +167,11 @@ class PagedCache:
               stream=None) -> None:
         """The rows k and v [sum(counts), n_kv_heads, head_dim] (slices of a projection will do) behind those that the
         requests have: counts[r] of request r, in order. req_offset: request_offsets(counts) on the device, if the
-        caller has it. With a stream, the books' small copies are made on it, too."""
-        counts = [int(n) for n in counts]
-        if len(counts) != self.requests or sum(counts) != k.shape[0]:
-            raise ValueError(f"{self.requests} counts are needed, with a sum of {k.shape[0]}")
+        caller has it (a captured write needs it). With a stream, the books' small copies are made on it, too. Nothing is
+        written while a graph captures the call, so the host's lengths stay: `reserve` before, `advance` after replays."""
+        counts = self._counts(counts)
+        if sum(counts) != k.shape[0]:
+            raise ValueError(f"the counts must have a sum of {k.shape[0]}")
         act = torch.bfloat16 if self.desc.act_dtype == N.PMPE_BF16 else torch.float32
         for t in (k, v):  # (before the books change)
             if t.shape != (k.shape[0], self.desc.n_kv_heads, self.desc.head_dim) or t.dtype != act or t.device != self.k.device:
@@ -170,7 +193,8 @@ class PagedCache:
                 for r, n in enumerate(had):  # (no others: pages reserved ahead may hold rows of replays)
                     self._give_back(r, n)
                 raise
-            self.lengths = [a + b for a, b in zip(self.lengths, counts)]
+            if not (self.k.is_cuda and torch.cuda.is_current_stream_capturing()):
+                self.lengths = [a + b for a, b in zip(self.lengths, counts)]
             if stream is not None:
                 req_offset.record_stream(stream)
 

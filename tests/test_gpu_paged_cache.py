@@ -63,3 +63,38 @@ def test_a_captured_write_that_needs_pages_is_refused():
     cache.write(k, v, [1, 1], off)
     got, _ = cache.read([17, 5])
     assert torch.equal(got[16], k[0]) and torch.equal(got[21], k[1]) and x.tolist() == [1.0] * 4 and int(cache.dev_status) == 0
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_captured_steps_through_the_public_calls(fp8):
+    log(f"captured steps fp8 {fp8}")
+    cache, eager = (P.PagedCache(3, 16, 16, KV, DIM, 5, REV, FP, fp8=fp8) for _ in range(2))
+    k0, v0 = rows(60, 1), rows(60, 2)
+    for c in (cache, eager):
+        for r in range(3):
+            c.open(r, {"allow_private": r == 1})
+        c.write(k0, v0, [30, 10, 20])
+    off = torch.tensor([0, 1, 2, 3], dtype=torch.int32, device="cuda")
+    k, v, q = rows(3, 3), rows(3, 4), randn((3, HEADS, DIM), 5, 1.0, BF16).cuda()
+    cache.reserve([20, 20, 20])
+    cache.attend(q, 0.125)              # (its workspace)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cache.write(k, v, [1, 1, 1], off)
+        out = cache.attend(q, 0.125)
+    assert cache.lengths == [30, 10, 20] and cache.seq_len.tolist() == [30, 10, 20]
+    for i in range(6):
+        for n, t in enumerate((k, v)):
+            t.copy_(rows(3, 10 + 2 * i + n))
+        q.copy_(randn(q.shape, 40 + i, 1.0, BF16))
+        g.replay()
+        eager.write(k, v, [1, 1, 1], off)
+        assert torch.equal(out, eager.attend(q, 0.125))
+    cache.advance([6, 6, 6])
+    assert cache.lengths == eager.lengths == cache.seq_len.tolist() == [36, 16, 26]
+    more = rows(5, 60), rows(5, 61)     # eager rows go on from the replays'
+    for c in (cache, eager):
+        c.write(*more, [0, 5, 0])
+    for a, b in zip(cache.read([36, 21, 26]), eager.read([36, 21, 26])):
+        assert torch.equal(a, b)
+    assert int(cache.dev_status) == 0 and cache.lengths == [36, 21, 26]

@@ -56,3 +56,43 @@ def test_pages_that_the_device_does_not_learn_of_are_not_taken(name):
     grow(c, [20, 20, 0])
     assert [len(p) for p in c._pages] == [3, 2, 1] and c.block_table.tolist() == owned(c)
     assert all(int(c.page_tag[p]) == 0 for p in sum(c._pages, []))
+
+
+def test_reserved_pages_and_rows_of_replays():
+    c = cache()
+    for r in range(3):
+        c.open(r, {"allow_private": r == 1})
+    grow(c, [4, 0, 16])
+    c.reserve([13, 16, 0])
+    assert [len(p) for p in c._pages] == [2, 1, 1] and c.lengths == [4, 0, 16] and c.block_table.tolist() == owned(c)
+    c.reserve([28, 3, 0])         # inside what it has
+    assert [len(p) for p in c._pages] == [2, 1, 1]
+    for counts in ([64, 0, 0], [0, 0, 64], [0, 65, 0], [1, 0], [0, 0, -1], [44, 64, 33]):
+        with pytest.raises(ValueError):
+            c.reserve(counts)
+    for counts in ([29, 0, 0], [0, 17, 0], [0, 0, 1], [-1, 0, 0], [1, 1], [1, 1, 0, 0]):
+        with pytest.raises(ValueError):
+            c.advance(counts)
+    assert c.lengths == [4, 0, 16] and [len(p) for p in c._pages] == [2, 1, 1]
+    c.advance([28, 0, 0])
+    c.advance([0, 16, 0])
+    assert c.lengths == [32, 16, 16]
+    with pytest.raises(ValueError):
+        c.advance([1, 0, 0])
+    c.close(0)
+    with pytest.raises(ValueError):
+        c.advance([1, 0, 0])      # not open: no pages
+    with pytest.raises(ValueError):
+        c.reserve([1, 0, 0])
+
+
+def test_a_request_with_reserved_pages_does_not_share():
+    c = cache()
+    for r in range(3):
+        c.open(r, None)
+    grow(c, [40, 0, 0])
+    c.reserve([0, 20, 0])
+    with pytest.raises(ValueError):
+        c.share(1, 0, 40)         # its own two pages would be lost
+    assert sum(map(len, c._pages)) + len(c._free) == 8
+    assert c.share(2, 0, 40) == 32
