@@ -26,8 +26,9 @@ class PagedCache:
     `open` gives a request its decision, which its pages carry from then on; `write` adds rows to the requests of a
     batch (the new token of each in a decoding step, a prompt before it), `attend` is the attention of each request's
     newest token, `share` lets a request begin with another's first pages where their cache tags are equal. The
-    kernels refuse a page of the other decision whatever the block table says (`dev_status`). The books are the
-    host's: pages come and go between calls on one stream."""
+    kernels refuse a page of the other decision whatever the block table says: the bits of `dev_status`, which the
+    caller reads when it likes, tell. The books are the host's, their device copies follow on the stream of each call (the
+    current one without `stream`): an object's calls go to one stream, or the caller orders its streams."""
 
     def __init__(self, requests: int, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, max_pages: int,
                  model_revision: bytes, checkpoint_fingerprint: bytes, bf16: bool = True, fp8: bool = False, device="cuda"):
@@ -60,19 +61,21 @@ class PagedCache:
             raise ValueError(f"request {r} is not open")
         return N.make_cache_tag(self.decision[r], self.revision, self.fingerprint)
 
-    def open(self, r: int, meta: Any) -> None:
+    def open(self, r: int, meta: Any, stream=None) -> None:
         """Request r begins anew, with the decision that its trusted metadata resolve to (missing or malformed: deny)."""
-        self.close(r)
+        self.close(r, stream)
         word = policy_word(meta)
-        self.decision[r] = int(word == N.PMPE_POLICY_ALLOW)
-        self.words[r] = _as_int32(word)
+        with torch.cuda.stream(stream):
+            self.decision[r] = int(word == N.PMPE_POLICY_ALLOW)
+            self.words[r] = _as_int32(word)
 
-    def close(self, r: int) -> None:
+    def close(self, r: int, stream=None) -> None:
         """Request r gives its pages back; those that no other request has belong to no decision then."""
-        self._give_back(r, 0)
-        self.lengths[r], self.decision[r] = 0, None
-        self.words[r] = 0
-        self.seq_len[r] = 0
+        with torch.cuda.stream(stream):
+            self._give_back(r, 0)
+            self.lengths[r], self.decision[r] = 0, None
+            self.words[r] = 0
+            self.seq_len[r] = 0
 
     def _give_back(self, r: int, keep: int) -> None:
         """The pages of request r but the first `keep`. Their columns of the table name none from then on: a length that
@@ -89,7 +92,7 @@ class PagedCache:
             self.page_tag[torch.tensor(free, device=self.page_tag.device)] = _FREE
         del self._pages[r][keep:]
 
-    def share(self, r: int, source: int, rows: int, tag: Optional[N.CacheTag] = None) -> int:
+    def share(self, r: int, source: int, rows: int, tag: Optional[N.CacheTag] = None, stream=None) -> int:
         """Request r, open and empty, begins with the rows of the whole pages among the first `rows` of `source`. tag:
         the cache tag that these rows were made under (default: the source's). Returns the number of rows it has then;
         raises PmpeError where the tags differ."""
@@ -105,10 +108,11 @@ class PagedCache:
         pages = self._pages[source][:n]
         for p in pages:
             self._users[p] += 1
-        if n:
-            self.block_table[r, :n] = self.block_table[source, :n]
         self._pages[r], self.lengths[r] = list(pages), n * self.desc.page_size
-        self.seq_len[r] = self.lengths[r]
+        with torch.cuda.stream(stream):
+            if n:
+                self.block_table[r, :n] = self.block_table[source, :n]
+            self.seq_len[r] = self.lengths[r]
         return self.lengths[r]
 
     def _counts(self, counts: Sequence[int]) -> List[int]:

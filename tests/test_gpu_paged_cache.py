@@ -98,3 +98,49 @@ def test_captured_steps_through_the_public_calls(fp8):
     for a, b in zip(cache.read([36, 21, 26]), eager.read([36, 21, 26])):
         assert torch.equal(a, b)
     assert int(cache.dev_status) == 0 and cache.lengths == [36, 21, 26]
+
+
+def serve(cache, q, stream, reads):
+    """Requests that come, share, end and come again, with the kernels' outputs after every change."""
+    out, at = [], 0
+
+    def put(counts):
+        nonlocal at
+        n = sum(counts)
+        cache.write(reads[0][at:at + n], reads[1][at:at + n], counts, stream=stream)
+        out.append(cache.attend(q, 0.125, stream=stream))
+        at += n
+    for r in range(4):
+        cache.open(r, {"allow_private": r % 2 == 1}, stream=stream)
+    put([20, 33, 5, 1])
+    for turn in range(6):
+        cache.close(turn % 3, stream=stream)
+        cache.open(turn % 3, {"allow_private": turn % 2 == 0}, stream=stream)
+        put([3 + 5 * (turn % 3 == r) for r in range(4)])
+        cache.open(3, {"allow_private": cache.decision[1] == 1}, stream=stream)
+        got = cache.share(3, 1, 40, stream=stream)
+        assert got == min(40, cache.lengths[1]) // 16 * 16
+        cache.reserve([17, 0, 17, 2], stream=stream)
+        put([1, 1, 1, 1])
+        out += cache.read([1, 2, 3, 1], stream=stream)
+    return out
+
+
+def test_every_call_on_a_side_stream_with_the_current_one_busy():
+    log("all calls on a side stream")
+    kv, q = (rows(300, 1), rows(300, 2)), randn((4, HEADS, DIM), 3, 1.0, BF16).cuda()
+    results = []
+    busy = torch.randn(4096, 4096, device="cuda")
+    for side in (False, True):
+        cache = P.PagedCache(4, 24, 16, KV, DIM, 6, REV, FP)
+        torch.cuda.synchronize()
+        s = torch.cuda.Stream() if side else None
+        if side:
+            for _ in range(40):         # what is put on the current stream comes tens of milliseconds later
+                busy = torch.mm(busy, busy).clamp_(-1.0, 1.0)
+        out = serve(cache, q, s, kv)
+        if side:
+            s.synchronize()
+        results.append([x.cpu() for x in out] + [cache.seq_len.cpu(), cache.dev_status.cpu()])
+        torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and int(results[1][-1]) == 0
