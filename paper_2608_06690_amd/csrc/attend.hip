@@ -32,6 +32,7 @@ constexpr int TILE = 32;        // cache rows of a wave's step
 constexpr int PARTS = 1536;       // parts that all tiles would make: two rounds of the blocks that fit the card
 constexpr int WHOLE_TILES = 32;   // tables of at most so many tiles: no head is cut (8 steps, about as long as the search and the join)
 constexpr int MOST_HEADS = 8192;  // virtual heads from which none is cut
+constexpr int MOST_BLOCKS = 1 << 22;  // of a launch: 2^30 threads (2^32 are more than one can have)
 constexpr float LOG2E = 1.4426950408889634f;
 
 enum { BF16 = 0, FP8 = 1, F32 = 2 };
@@ -681,25 +682,42 @@ bool direct(int64_t vheads, int max_pages, int page_size) {
   return (int64_t)max_pages * page_size <= WHOLE_TILES * TILE || vheads >= MOST_HEADS;
 }
 
+// Requests [r0, r0 + n) of a call whose heads are not cut.
+AttnArgs part_of_call(const AttnArgs& a, int r0, int n) {
+  const size_t el = a.c.act_bf16 ? 2 : 4, row = (size_t)a.heads * a.c.dim;
+  AttnArgs p = a;
+  p.c.R = n;
+  p.c.table += (size_t)r0 * a.c.max_pages;
+  if (a.c.words) p.c.words += r0;
+  p.q = (const char*)a.q + (size_t)r0 * a.q_stride * el;
+  if (a.first) p.first += r0;
+  p.len += r0;
+  p.out = (char*)a.out + r0 * row * el;
+  if (a.lse) p.lse += (size_t)r0 * a.heads;
+  return p;
+}
+
 template <int T, int NB>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
   const Split sp = split_of(a.heads, a.c.kv);
   const int64_t vheads = (int64_t)a.c.R * sp.vheads, rows = (int64_t)a.c.max_pages * a.c.page_size;
-  const bool d = direct(vheads, a.c.max_pages, a.c.page_size);
-  const int grid = (int)(d ? vheads : vheads + PARTS);
-  if (sp.rows <= 8) {
-    if (d) attn_kernel<T, NB, true, true><<<grid, 64 * WAVES, 0, s>>>(a);
-    else attn_kernel<T, NB, true, false><<<grid, 64 * WAVES, 0, s>>>(a);
-  } else {
-    if (d) attn_kernel<T, NB, false, true><<<grid, 64 * WAVES, 0, s>>>(a);
-    else attn_kernel<T, NB, false, false><<<grid, 64 * WAVES, 0, s>>>(a);
+  if (direct(vheads, a.c.max_pages, a.c.page_size)) {
+    // (more than the threads that one launch may have: so many requests at a time)
+    const int most = MOST_BLOCKS / sp.vheads;
+    for (int r0 = 0; r0 < a.c.R; r0 += most) {
+      const AttnArgs p = part_of_call(a, r0, std::min(most, a.c.R - r0));
+      if (sp.rows <= 8) attn_kernel<T, NB, true, true><<<p.c.R * sp.vheads, 64 * WAVES, 0, s>>>(p);
+      else attn_kernel<T, NB, false, true><<<p.c.R * sp.vheads, 64 * WAVES, 0, s>>>(p);
+    }
+    return hipGetLastError();
   }
-  if (!d) {
-    // places that can be in use
-    const int slots = (int)std::min<int64_t>(SLOTS, vheads * ((rows + 8 * TILE - 1) / (8 * TILE) + 1));
-    if (vheads > 64) attn_join_kernel<T != F32, 1><<<(slots * sp.rows + 3) / 4, 256, 0, s>>>(a);
-    else attn_join_kernel<T != F32, 4><<<slots * sp.rows, 256, 0, s>>>(a);
-  }
+  const int grid = (int)vheads + PARTS;
+  if (sp.rows <= 8) attn_kernel<T, NB, true, false><<<grid, 64 * WAVES, 0, s>>>(a);
+  else attn_kernel<T, NB, false, false><<<grid, 64 * WAVES, 0, s>>>(a);
+  // places that can be in use
+  const int slots = (int)std::min<int64_t>(SLOTS, vheads * ((rows + 8 * TILE - 1) / (8 * TILE) + 1));
+  if (vheads > 64) attn_join_kernel<T != F32, 1><<<(slots * sp.rows + 3) / 4, 256, 0, s>>>(a);
+  else attn_join_kernel<T != F32, 4><<<slots * sp.rows, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
