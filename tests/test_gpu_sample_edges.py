@@ -75,3 +75,19 @@ def test_uniform_numbers_of_one_and_more_take_the_last_token(V):
             for par in ({}, dict(top_k=[V - 30] * 8), dict(min_p=[1e-35] * 8), dict(top_p=[0.9] * 8), dict(top_k=[5] * 8),
                         dict(temperature=[0.3] * 8, top_k=[V // 2] * 8, min_p=[1e-38] * 8)):
                 check(z, par, [u] * 8)
+
+
+@pytest.mark.parametrize("V", [8192, 30011])
+@pytest.mark.parametrize("top", [131072.0, -131200.0, 5e5, -5e5, 1e7])
+def test_rows_of_several_pieces_at_and_beyond_the_border(V, top):
+    log(f"several pieces V {V} top {top}")
+    rows, at = [], torch.arange(V)
+    for off in (-70.0, -1.0, 0.0, 1.0, 60.0):
+        for step in (0.5, 40.0, -40.0, 500.0):
+            rows.append((top + off + 4.0 * torch.randn(V, generator=gen(len(rows))) - step * (at >= V // 2)).float())
+    z = torch.stack(rows)
+    B = len(rows)
+    u = torch.rand(B, generator=gen(8)).tolist()
+    for par in ({}, dict(top_k=[V // 2] * B), dict(top_p=[0.9] * B), dict(min_p=[0.02] * B), dict(top_k=[50] * B, top_p=[0.5] * B)):
+        check(z, par, u)
+        check(z * 0.001, dict(par, temperature=[0.001] * B), u)
