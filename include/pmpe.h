@@ -868,7 +868,8 @@ pmpe_status pmpe_expert_ffn_mx(const pmpe_layer_desc* d, int32_t T, const uint8_
  *                     s = 2^ceil(log2(amax / 448)) of 32 consecutive values of a head, stored as its
  *                     biased exponent; a block with a value that is not finite becomes NaN
  *   block_table       [R, max_pages] int32: position p of request r is row p % page_size of page
- *                     block_table[r, p / page_size]. Entries past a request's length are not read
+ *                     block_table[r, p / page_size]. Entries past a request's length are not read;
+ *                     a negative one names no page, whatever the length says
  *   page_tag          [n_pages] uint32 or NULL (no check): PMPE_POLICY_ALLOW or PMPE_POLICY_DENY. A
  *                     request may use a page only if its tag is the request's resolved decision; any
  *                     other tag is refused to every request
@@ -927,7 +928,9 @@ pmpe_status pmpe_kv_read(const pmpe_cache_desc* c, int32_t T, int32_t R, void* k
  *   s_j = scale q . k_j for positions j in [seq_first[r], seq_len[r]) whose page the request may use
  *   out = sum_j exp(s_j - max s) v_j / sum_j exp(s_j - max s);  lse = max s + ln sum_j exp(s_j - max s)
  *   query head i reads kv head i / (n_heads / n_kv_heads). A request without such a position has out 0
- *   and lse -inf. Products, softmax statistics and sums are fp32, also of values cached in 8 bits.
+ *   and lse -inf. Products, softmax statistics and sums are fp32, also of values cached in 8 bits (a
+ *   weight meets bf16 values as a sum of three bf16 parts, right to 2^-27). A value that is not finite
+ *   makes the outputs that it enters not finite, an infinite one NaN as well as infinite.
  *
  *   q, out       [R, n_heads, head_dim] of act_dtype, requests of q q_stride elements apart; n_heads a
  *                multiple of n_kv_heads, up to 1024

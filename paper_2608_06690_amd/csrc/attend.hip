@@ -10,15 +10,16 @@
 // the second product without leaving their lane, and V^T's pairs of rows are one byte permutation each.
 //
 // A block has a request's virtual head (a kv head and up to 16 of its query heads), its four waves every fourth tile.
-// Where requests are long, a head's tiles are cut into equal parts of a length that all requests share, found from
-// their lengths by every block: PARTS parts in all, and one more at most for each head. A second kernel joins the
-// parts in order. No atomics: equal calls have equal bits.
+// Where tables are long, a head's tiles are cut into equal parts of a length that all requests share, found from
+// their lengths by every block: 32 tiles, fewer (8 at least) where CUs would be left without a part, more where there
+// would be over PARTS parts and one for each head. A second kernel joins the parts in order. No atomics: equal calls
+// have equal bits.
 //
-// Bound by HBM, and by the pattern in which it is read: 256 requests of up to 4096 rows over 4 kv heads of 128 in 8 bits
-// (1.1 GB) take 213 us, 5.0 TB/s, and as long with all products left out; 64 of 8000 rows in bf16 324 us, 6.4 TB/s. A K
+// Bound by HBM, and by the pattern in which it is read: 256 requests of up to 8149 rows (4047 in the mean) over 4 kv heads of
+// 128 in 8 bits (1.1 GB) take 205 us, 5.4 TB/s; 64 of 8000 rows over 8 kv heads of 128 in bf16 (2.1 GB) 323 us, 6.5 TB/s. A K
 // operand of 8-bit rows is 64 bytes at a time, half a line, and scales are lines of their own; plain reads of whole
-// lines reach 6.6 to 7.1 TB/s, of half lines 5.7 to 6.0. Single requests are bound by latency: 700 rows 10.5 us,
-// 131,000 rows 43 us in 1,536 parts and 11 us to join them. Loads are never under a branch (a row that may not
+// lines reach 6.6 to 7.1 TB/s, of half lines 5.7 to 6.0. Single requests over 4 kv heads are bound by latency: 700 rows 10.6
+// us, 131,000 rows 43 us in 512 parts and 11 us to join them. Loads are never under a branch (a row that may not
 // be used is read from page 0 and dropped): with branches each step waited for all loads of the one before it.
 #include <algorithm>
 
@@ -29,7 +30,7 @@ namespace {
 
 constexpr int WAVES = 4;
 constexpr int TILE = 32;        // cache rows of a wave's step
-constexpr int PARTS = 1536;       // parts that all tiles would make: two rounds of the blocks that fit the card
+constexpr int PARTS = 1536;       // parts of all tiles at most, but for one of each head: two rounds of the blocks that fit the card
 constexpr int WHOLE_TILES = 32;   // tables of at most so many tiles: no head is cut (8 steps, about as long as the search and the join)
 constexpr int MOST_HEADS = 8192;  // virtual heads from which none is cut
 constexpr int MOST_BLOCKS = 1 << 22;  // of a launch: 2^30 threads (2^32 are more than one can have)
@@ -326,7 +327,7 @@ struct Wave {
     } else {
       // A weight as the sum of three bf16 values, which leaves 2^-27 of it (two leave 2^-18, and four times as many
       // outputs rounded to the other side as fp32 weights do). With up to 8 heads the second parts are columns 8 .. 15 of
-      // the first parts' product.
+      // the first parts' product. The third takes 2 to 7 % of a single request of up to 1000 rows, nothing of long ones.
       u32x4 hi, lo, rest;
       float x[8], y[8];
 #pragma unroll

@@ -8,9 +8,10 @@
 // the token's heads, so a block of 32 values lies in 4 neighbouring lanes: its largest magnitude takes two exchanges
 // and no LDS. One kernel serves both directions and k and v together, as a launch costs more than a small batch's rows.
 //
-// Bound by HBM in large batches: 16384 tokens of 4 heads of 128 written in 8 bits take 13.2 to 13.7 us for 50.9 MB
-// (3.8 TB/s; a large copy's rate would give 9.8), 16000 read 9.6 to 9.9 us (5.0). 8 tokens take 3.2 us, a launch;
-// the call then costs 10 to 14 us of checks on the host.
+// Bound by a wave's chain of loads up to its first row (request, position, page, tag), by HBM in large batches: 16417
+// tokens of 4 heads of 128 written in 8 bits take 13.1 to 13.7 us for 51.0 MB (3.8 TB/s; a large copy's rate would give
+// 9.8), 8289 read 9.3 to 9.9 us for 25.7 MB (2.7 TB/s; 5.0 at that rate). 8 tokens take 3.2 us, a launch; the call then
+// costs 10 to 14 us of checks on the host.
 #include "kvcache.h"
 #include "mx.h"
 
