@@ -128,14 +128,20 @@ class PagedCache:
         with torch.cuda.stream(stream):
             self._reserve(counts)
 
-    def advance(self, counts: Sequence[int]) -> None:
-        """The rows that replays of captured writes have added to each request, which only the device has counted: after
-        them, and before the next call that needs the requests' lengths (write, read, share, reserve)."""
-        counts = self._counts(counts)
-        for r, n in enumerate(counts):
-            if n < 0 or self.lengths[r] + n > len(self._pages[r]) * self.desc.page_size:
-                raise ValueError(f"request {r} has no pages for {n} rows more than {self.lengths[r]}")
-        self.lengths = [a + b for a, b in zip(self.lengths, counts)]
+    def advance(self, stream=None) -> List[int]:
+        """Brings the host's lengths to the device's, which alone has counted the rows of replayed writes: after replays,
+        and before the next call that goes by the requests' lengths (write, read, share, reserve). Rows that were refused
+        because no page was there are in neither then. Waits for the stream; returns the rows that each request gained."""
+        with torch.cuda.stream(stream):
+            torch.minimum(self.seq_len, self._most(self.seq_len.device), out=self.seq_len)
+            have = self.seq_len.tolist()
+        gained = [a - b for a, b in zip(have, self.lengths)]
+        self.lengths = have
+        return gained
+
+    def _most(self, device) -> torch.Tensor:
+        """[requests] int32: rows that the pages of each request hold."""
+        return torch.tensor([len(p) * self.desc.page_size for p in self._pages], dtype=torch.int32).to(device)
 
     def _reserve(self, counts: Sequence[int]) -> None:
         """Pages for counts[r] more rows of each request, or none at all."""
@@ -161,6 +167,9 @@ class PagedCache:
             tags.append(_as_int32(N.PMPE_POLICY_ALLOW if self.decision[r] else N.PMPE_POLICY_DENY))
             n[r] += 1
         i = torch.tensor([rows, cols, pages, tags], dtype=torch.int64).to(self.page_tag.device)
+        # (a length that replays have taken past the pages of now counts rows that were refused: the new pages, and what
+        # they held before, must not stand in for them)
+        torch.minimum(self.seq_len, self._most(self.seq_len.device), out=self.seq_len)
         self.block_table[i[0], i[1]] = i[2].int()
         self.page_tag[i[2]] = i[3].int()
         for r, p in zip(rows, pages):  # (the books last: where the device's part fails, they are as they were)

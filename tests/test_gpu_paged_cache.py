@@ -90,7 +90,7 @@ def test_captured_steps_through_the_public_calls(fp8):
         g.replay()
         eager.write(k, v, [1, 1, 1], off)
         assert torch.equal(out, eager.attend(q, 0.125))
-    cache.advance([6, 6, 6])
+    assert cache.advance() == [6, 6, 6]
     assert cache.lengths == eager.lengths == cache.seq_len.tolist() == [36, 16, 26]
     more = rows(5, 60), rows(5, 61)     # eager rows go on from the replays'
     for c in (cache, eager):
@@ -144,3 +144,38 @@ def test_every_call_on_a_side_stream_with_the_current_one_busy():
         results.append([x.cpu() for x in out] + [cache.seq_len.cpu(), cache.dev_status.cpu()])
         torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(*results)) and int(results[1][-1]) == 0
+
+
+def test_replays_past_the_pages_go_on_once_more_are_reserved():
+    log("replays past the pages, then more pages")
+    cache = P.PagedCache(2, 8, 16, KV, DIM, 4, REV, FP)
+    cache.open(0, {"allow_private": True})
+    cache.write(rows(60, 1), rows(60, 2), [60, 0])
+    cache.close(0)                      # the pages to come hold rows of an allowed request
+    for r in range(2):
+        cache.open(r, None)
+    k0, v0 = rows(14, 3), rows(14, 4)
+    cache.write(k0, v0, [14, 0])
+    k, v, q = rows(1, 5), rows(1, 6), randn((2, HEADS, DIM), 7, 1.0, BF16).cuda()
+    off = torch.tensor([0, 1, 1], dtype=torch.int32, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cache.write(k, v, [1, 0], off)
+    ks, vs = [k0], [v0]
+    for i in range(9):
+        k.copy_(rows(1, 20 + i))
+        v.copy_(rows(1, 40 + i))
+        if i < 2 or i >= 5:             # the third to fifth meet no page
+            ks.append(k.clone())
+            vs.append(v.clone())
+        if i == 5:
+            assert int(cache.dev_status) == P.PMPE_DEV_CACHE_RANGE
+            cache.reserve([10, 0])
+        g.replay()
+    assert cache.advance() == [6, 0] and cache.lengths == [20, 0] == cache.seq_len.tolist()
+    got = cache.read([20, 0])
+    assert torch.equal(got[0], torch.cat(ks)) and torch.equal(got[1], torch.cat(vs))
+    fresh = P.PagedCache(2, 8, 16, KV, DIM, 4, REV, FP)
+    fresh.open(0, None)
+    fresh.write(torch.cat(ks), torch.cat(vs), [20, 0])
+    assert torch.equal(cache.attend(q, 0.125), fresh.attend(q, 0.125))

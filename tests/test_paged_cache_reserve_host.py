@@ -58,11 +58,17 @@ def test_pages_that_the_device_does_not_learn_of_are_not_taken(name):
     assert all(int(c.page_tag[p]) == 0 for p in sum(c._pages, []))
 
 
+def replay(c, counts):
+    """What replays of a captured write do to the device's lengths."""
+    c.seq_len += torch.tensor(counts, dtype=torch.int32)
+
+
 def test_reserved_pages_and_rows_of_replays():
     c = cache()
     for r in range(3):
         c.open(r, {"allow_private": r == 1})
     grow(c, [4, 0, 16])
+    replay(c, [4, 0, 16])
     c.reserve([13, 16, 0])
     assert [len(p) for p in c._pages] == [2, 1, 1] and c.lengths == [4, 0, 16] and c.block_table.tolist() == owned(c)
     c.reserve([28, 3, 0])         # inside what it has
@@ -70,20 +76,31 @@ def test_reserved_pages_and_rows_of_replays():
     for counts in ([64, 0, 0], [0, 0, 64], [0, 65, 0], [1, 0], [0, 0, -1], [44, 64, 33]):
         with pytest.raises(ValueError):
             c.reserve(counts)
-    for counts in ([29, 0, 0], [0, 17, 0], [0, 0, 1], [-1, 0, 0], [1, 1], [1, 1, 0, 0]):
-        with pytest.raises(ValueError):
-            c.advance(counts)
-    assert c.lengths == [4, 0, 16] and [len(p) for p in c._pages] == [2, 1, 1]
-    c.advance([28, 0, 0])
-    c.advance([0, 16, 0])
-    assert c.lengths == [32, 16, 16]
-    with pytest.raises(ValueError):
-        c.advance([1, 0, 0])
+    assert c.advance() == [0, 0, 0] and c.lengths == [4, 0, 16] and [len(p) for p in c._pages] == [2, 1, 1]
+    replay(c, [28, 5, 0])
+    assert c.advance() == [28, 5, 0] and c.lengths == [32, 5, 16] == c.seq_len.tolist()
     c.close(0)
-    with pytest.raises(ValueError):
-        c.advance([1, 0, 0])      # not open: no pages
+    replay(c, [3, 0, 0])          # not open
+    assert c.advance() == [0, 0, 0] and c.lengths == [0, 5, 16] == c.seq_len.tolist()
     with pytest.raises(ValueError):
         c.reserve([1, 0, 0])
+
+
+@pytest.mark.parametrize("late", [False, True])
+def test_refused_rows_of_replays_are_counted_nowhere(late):
+    # (a page that is reserved after them holds what another request left in it)
+    c = cache()
+    for r in range(3):
+        c.open(r, None)
+    grow(c, [14, 3, 0])
+    replay(c, [14, 3, 0])
+    replay(c, [5, 5, 0])          # request 0 has a page for two of its five
+    if not late:
+        assert c.advance() == [2, 5, 0] and c.seq_len.tolist() == [16, 8, 0]
+    c.reserve([20, 0, 0])
+    assert c.seq_len.tolist() == [16, 8, 0] and len(c._pages[0]) >= 2
+    replay(c, [1, 1, 0])
+    assert c.advance() == ([3, 6, 0] if late else [1, 1, 0]) and c.lengths == [17, 9, 0] == c.seq_len.tolist()
 
 
 def test_a_request_with_reserved_pages_does_not_share():
