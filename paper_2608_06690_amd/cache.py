@@ -133,18 +133,18 @@ class PagedCache:
         and before the next call that goes by the requests' lengths (write, read, share, reserve). Rows that were refused
         because no page was there are in neither then. Waits for the stream; returns the rows that each request gained."""
         with torch.cuda.stream(stream):
-            torch.minimum(self.seq_len, self._most(self.seq_len.device), out=self.seq_len)
+            torch.minimum(self.seq_len, torch.tensor(self._most(), dtype=torch.int32).to(self.seq_len.device), out=self.seq_len)
             have = self.seq_len.tolist()
         gained = [a - b for a, b in zip(have, self.lengths)]
         self.lengths = have
         return gained
 
-    def _most(self, device) -> torch.Tensor:
-        """[requests] int32: rows that the pages of each request hold."""
-        return torch.tensor([len(p) * self.desc.page_size for p in self._pages], dtype=torch.int32).to(device)
+    def _most(self) -> List[int]:
+        """Rows that the pages of each request hold."""
+        return [len(p) * self.desc.page_size for p in self._pages]
 
-    def _reserve(self, counts: Sequence[int]) -> None:
-        """Pages for counts[r] more rows of each request, or none at all."""
+    def _reserve(self, counts: Sequence[int]) -> List[int]:
+        """Pages for counts[r] more rows of each request, or none at all. Returns the request of each page taken."""
         size, need = self.desc.page_size, []
         for r, n in enumerate(counts):
             if n < 0 or (n > 0 and self.decision[r] is None):
@@ -156,7 +156,7 @@ class PagedCache:
         if len(need) > len(self._free):
             raise ValueError(f"{len(need)} pages are needed, {len(self._free)} are free")
         if not need:
-            return
+            return need
         if self.k.is_cuda and torch.cuda.is_current_stream_capturing():
             raise ValueError("a captured write cannot take pages: they have to be reserved before")
         rows, cols, pages, tags, n = [], [], [], [], [len(p) for p in self._pages]
@@ -166,15 +166,16 @@ class PagedCache:
             pages.append(p)
             tags.append(_as_int32(N.PMPE_POLICY_ALLOW if self.decision[r] else N.PMPE_POLICY_DENY))
             n[r] += 1
-        i = torch.tensor([rows, cols, pages, tags], dtype=torch.int64).to(self.page_tag.device)
+        n, i = len(need), torch.tensor(rows + cols + pages + tags + self._most(), dtype=torch.int64).to(self.page_tag.device)
         # (a length that replays have taken past the pages of now counts rows that were refused: the new pages, and what
         # they held before, must not stand in for them)
-        torch.minimum(self.seq_len, self._most(self.seq_len.device), out=self.seq_len)
-        self.block_table[i[0], i[1]] = i[2].int()
-        self.page_tag[i[2]] = i[3].int()
+        torch.minimum(self.seq_len, i[4 * n:].int(), out=self.seq_len)
+        self.block_table[i[:n], i[n:2 * n]] = i[2 * n:3 * n].int()
+        self.page_tag[i[2 * n:3 * n]] = i[3 * n:4 * n].int()
         for r, p in zip(rows, pages):  # (the books last: where the device's part fails, they are as they were)
             self._pages[r].append(self._free.pop())
             self._users[p] = 1
+        return need
 
     def write(self, k: torch.Tensor, v: torch.Tensor, counts: Sequence[int], req_offset: Optional[torch.Tensor] = None,
               stream=None) -> None:
@@ -194,8 +195,7 @@ class PagedCache:
                 req_offset = request_offsets(counts, self.seq_len.device)
             elif req_offset.shape != (self.requests + 1,) or req_offset.dtype != torch.int32 or req_offset.device != self.k.device:
                 raise ValueError(f"req_offset must be [{self.requests + 1}] of torch.int32 on {self.k.device}")
-            had = [len(p) for p in self._pages]
-            self._reserve(counts)
+            taken = self._reserve(counts)
             more = counts[0] if all(n == counts[0] for n in counts) else req_offset[1:] - req_offset[:-1]
             self.seq_len.add_(more)
             try:
@@ -203,8 +203,8 @@ class PagedCache:
                                 self.v, self.k_scale, self.v_scale, self.dev_status)
             except Exception:  # nothing was written: a length ahead of the rows would show what the pages held before
                 self.seq_len.sub_(more)
-                for r, n in enumerate(had):  # (no others: pages reserved ahead may hold rows of replays)
-                    self._give_back(r, n)
+                for r in set(taken):  # (no others: pages reserved ahead may hold rows of replays)
+                    self._give_back(r, len(self._pages[r]) - taken.count(r))
                 raise
             if not (self.k.is_cuda and torch.cuda.is_current_stream_capturing()):
                 self.lengths = [a + b for a, b in zip(self.lengths, counts)]
